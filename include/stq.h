@@ -7,7 +7,9 @@
  * decoupled-weight-decay update), the per-layer statistics the Score Engine of
  * Section 3.3 consumes, the conversion of stored codes when Map (Section 3.4)
  * changes a layer's bit-width, the host-side decision itself, and the same loop
- * with the decision and the bit plan resident on the device (stq_engine_*).
+ * with the decision and the bit plan resident on the device (stq_engine_*).  Beside
+ * it stand the operators of a layer whose weights and activations are held in 8 bits
+ * (stq_quantize_rows ... stq_matmul_grad_weight), which make the step's gradients.
  *
  * Conventions
  *   - Every function returns STQ_OK (0) or a negative STQ_E* code.  Nothing
@@ -78,7 +80,9 @@ enum {
   STQ_EDEVICE = -5, /* no such device, or not a gfx950 GPU */
   STQ_EHIP = -6,    /* a HIP runtime call failed */
   STQ_ESTATE = -7,  /* stq_stats called with nothing accumulated for that many tensors */
-  STQ_ELIMIT = -8   /* stq_step_static: more tensors than its static table holds */
+  STQ_ELIMIT = -8,  /* stq_step_static: more tensors than its static table holds */
+  STQ_ESHAPE = -9,  /* matrices whose sizes do not fit each other, or a size outside an operator's range */
+  STQ_EDTYPE = -10  /* a matrix of a type that the operator does not take there */
 };
 
 typedef struct stq_ctx stq_ctx; /* opaque, owned by the library */
@@ -329,6 +333,99 @@ int stq_engine_read(stq_engine* e, stq_bits* stored, stq_bits* next, stq_codes* 
 
 /* Synchronise the device and free what the engine owns (not the caller's buffers). */
 int stq_engine_destroy(stq_engine* e);
+
+/* ---- Operators of an 8-bit layer -----------------------------------------------------
+ * What trains the parameters that stq_step updates: a layer whose activations and weights are held in
+ * 8 bits, in the forward pass and for the backward pass, and whose gradients come out as stq_step reads
+ * them (fp32 or bf16).  All calls are asynchronous on hip_stream, allocate nothing, upload nothing, wait for
+ * nothing and keep nothing from one call to the next; they can be recorded into a HIP graph.  They use no
+ * buffer of the context, so calls on several streams may overlap.  Results do not depend on the launch
+ * (no atomics): the same inputs give the same bits.
+ *
+ * A matrix is row-major; `stride` elements lie between the starts of two rows (>= cols; a view into a wider
+ * matrix is fine).  Element alignment is enough for data; rows of 16-byte multiples are faster in places.  rows
+ * may be 0: the call then writes nothing (a weight gradient is all zeros).  cols is 1 at least; rows and cols are
+ * below 2^31.  Unless said otherwise an output may not overlap an input or another output.
+ *
+ * 8 bits (STQ_Q8): int8 codes q and fp32 scales s, value s * q.  block = 0: one scale for each row, at
+ * scales[row]; block = 64, 128 or 256: one for each `block` columns of a row (the last may cover fewer), at
+ * scales[row * ceil(cols / block) + col / block].  Written codes are q = rint(x * (127 / a)), s = a / 127 with
+ * a = max(max|x|, 2^-100) over the scale's elements (ties to even; -127 <= q <= 127).  Where one of these
+ * elements is not finite, s is NaN and the codes are 0: everything computed from them is NaN then.
+ *
+ * Gradients pass through the conversion as if it were the identity; they are those of the values that the
+ * codes stand for. */
+#define STQ_F32 0u
+#define STQ_BF16 1u
+#define STQ_Q8 2u
+typedef struct {
+  void* data;     /* device; float, bfloat16 or int8 */
+  float* scales;  /* device; of an 8-bit matrix (else ignored) */
+  uint64_t rows, cols;
+  uint64_t stride; /* elements from row to row */
+  uint32_t dtype;  /* STQ_F32, STQ_BF16, STQ_Q8 */
+  uint32_t block;  /* columns per scale of an 8-bit matrix: 0 (the whole row), 64, 128 or 256 */
+} stq_matrix;
+
+/* Columns of stq_matmul's operands at most: their products are summed in int32. */
+#define STQ_MAX_INNER 131071u
+
+/* x (fp32 or bf16) to codes and scales: activations for a checkpoint (any block), or weights for stq_matmul
+ * (block 0: a scale for each output channel of w[out][in], for instance straight from stq_step's fp32 parameters). */
+int stq_quantize_rows(stq_ctx* ctx, const stq_matrix* x, const stq_matrix* codes, void* hip_stream);
+
+/* The values that codes stand for, as fp32 or bf16. */
+int stq_dequantize_rows(stq_ctx* ctx, const stq_matrix* codes, const stq_matrix* out, void* hip_stream);
+
+/* Root-mean-square norm behind the residual's addition:
+ *   sum = x + residual, rounded to x's type (residual NULL: sum = x)
+ *   rstd[row] = 1 / sqrt(mean(sum^2) + eps),  y = sum * rstd * weight, written as codes with a scale for each row
+ *   (scale = rstd * a / 127 with a the largest |sum * weight| of the row, at least 2^-100).
+ * x, residual: fp32 or bf16, one type.  weight: device, fp32[cols].  eps > 0, finite.  sum: x's type, may be NULL, and may be
+ * x's or residual's own buffer.  y: STQ_Q8, block 0.  saved (may be NULL): the sum in 8 bits, any block, for
+ * stq_rms_norm_grad.  rstd: device, fp32[rows], may be NULL.  A row whose squares add up to more than fp32 holds counts as not
+ * finite: its scale and rstd are NaN. */
+int stq_rms_norm(stq_ctx* ctx, const stq_matrix* x, const stq_matrix* residual, const float* weight, float eps,
+                 const stq_matrix* sum, const stq_matrix* y, const stq_matrix* saved, float* rstd, void* hip_stream);
+
+/* Its gradients.  sum: as it was left by the forward pass, fp32, bf16 or 8 bits; rstd: the forward pass's.  With
+ * n = sum * rstd and u = dy * weight:
+ *   dx = rstd * (u - n * mean(u * n)) + dresidual,  dweight[col] = sum over the rows of dy * n
+ * (the gradient of x and of residual alike).  dresidual (may be NULL): the gradient that reaches sum on its other way.
+ * dy, dresidual, dx: fp32 or bf16, one type; dx may be dy's or dresidual's own buffer.  dweight: device, fp32[cols], overwritten.
+ * workspace: device, 16-byte aligned, of at least stq_rms_norm_grad_bytes bytes, free again when the call's work is done. */
+int stq_rms_norm_grad(stq_ctx* ctx, const stq_matrix* sum, const float* weight, const float* rstd, const stq_matrix* dy,
+                      const stq_matrix* dresidual, const stq_matrix* dx, float* dweight, void* workspace,
+                      uint64_t workspace_bytes, void* hip_stream);
+int stq_rms_norm_grad_bytes(uint64_t rows, uint64_t cols, uint64_t* bytes); /* host only */
+
+/* Gated activation y = silu(gate) * up, silu(g) = g / (1 + exp(-g)), written as codes with a scale for each row (y: STQ_Q8,
+ * block 0).  gate, up: fp32 or bf16, one type, the same size (two halves of one matrix, for instance).  saved_gate,
+ * saved_up (NULL both, or neither): gate and up in 8 bits, one block, for stq_gated_silu_grad. */
+int stq_gated_silu(stq_ctx* ctx, const stq_matrix* gate, const stq_matrix* up, const stq_matrix* y,
+                   const stq_matrix* saved_gate, const stq_matrix* saved_up, void* hip_stream);
+
+/* Its gradients: dgate = dy * up * (s + gate * s * (1 - s)), s = 1 / (1 + exp(-gate)), and dup = dy * gate * s.  gate, up: one
+ * type and block, fp32, bf16 or 8 bits.  dy, dgate, dup: fp32 or bf16, one type; dgate or dup may be dy's own buffer. */
+int stq_gated_silu_grad(stq_ctx* ctx, const stq_matrix* gate, const stq_matrix* up, const stq_matrix* dy,
+                        const stq_matrix* dgate, const stq_matrix* dup, void* hip_stream);
+
+/* Product over codes: out[token][o] = x.scales[token] * w.scales[o] * sum over i of x.q[token][i] * w.q[o][i], the sum exact
+ * in int32.  x: [tokens][in], w: [outputs][in], both STQ_Q8 with block 0, in <= STQ_MAX_INNER.  out: fp32 or bf16. */
+int stq_matmul(stq_ctx* ctx, const stq_matrix* x, const stq_matrix* w, const stq_matrix* out, void* hip_stream);
+
+/* Gradient of x: dx[token][i] = sum over o of dy[token][o] * w.scales[o] * w.q[o][i].  dy, dx: fp32 or bf16.  The factors
+ * dy * scale enter the matrix cores as bfloat16, and as the sum of two bfloat16 (16 bits of each) where dx is fp32; sums are
+ * fp32. */
+int stq_matmul_grad_input(stq_ctx* ctx, const stq_matrix* dy, const stq_matrix* w, const stq_matrix* dx, void* hip_stream);
+
+/* Gradient of w: dw[o][i] = sum over tokens of dy[token][o] * x.scales[token] * x.q[token][i], from the activations' codes as
+ * they are.  dy, dw: fp32 or bf16; rounding as in stq_matmul_grad_input.  dw is overwritten, and can be stq_step's gradient.
+ * workspace: device, 16-byte aligned, of at least stq_matmul_grad_weight_bytes bytes (which may be 0: then NULL will do), free
+ * again when the call's work is done. */
+int stq_matmul_grad_weight(stq_ctx* ctx, const stq_matrix* dy, const stq_matrix* x, const stq_matrix* dw, void* workspace,
+                           uint64_t workspace_bytes, void* hip_stream);
+int stq_matmul_grad_weight_bytes(uint64_t tokens, uint64_t outputs, uint64_t inputs, uint64_t* bytes); /* host only */
 
 /* The library's own quantizer tables, for inspection (host only, no context):
  *   which 0: G[j] = fl32(2^(-j/32)), j < 511 (bits ignored)

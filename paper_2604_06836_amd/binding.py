@@ -20,6 +20,8 @@ STQ_FLAG_STATS_GRAD = 2
 STQ_DECIDE_R_ALG1 = 1
 STQ_DECIDE_NO_DUAL, STQ_DECIDE_NO_TEMPORAL, STQ_DECIDE_NO_SPATIAL = 2, 4, 8
 STQ_ENGINE_ALG1_ORDER = 1
+STQ_F32, STQ_BF16, STQ_Q8 = 0, 1, 2
+STQ_MAX_INNER = 131071
 
 
 class StqError(RuntimeError):
@@ -80,9 +82,16 @@ class Codes(C.Structure):
     _fields_ = [("m_codes", C.c_void_p), ("v_codes", C.c_void_p)]
 
 
+class Matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64),
+                ("stride", C.c_uint64), ("dtype", C.c_uint32), ("block", C.c_uint32)]
+
+
 EXPORTS = ["stq_init", "stq_set_schedule", "stq_destroy", "stq_state_bytes", "stq_zero_state", "stq_step", "stq_step_static", "stq_step_transition", "stq_grad_stats", "stq_stats",
            "stq_repack", "stq_repack_many", "stq_decide", "stq_decide_due", "stq_engine_create", "stq_engine_set_next", "stq_engine_step",
-           "stq_engine_read", "stq_engine_destroy", "stq_table", "stq_strerror"]
+           "stq_engine_read", "stq_engine_destroy", "stq_quantize_rows", "stq_dequantize_rows", "stq_rms_norm", "stq_rms_norm_grad",
+           "stq_rms_norm_grad_bytes", "stq_gated_silu", "stq_gated_silu_grad", "stq_matmul", "stq_matmul_grad_input",
+           "stq_matmul_grad_weight", "stq_matmul_grad_weight_bytes", "stq_table", "stq_strerror"]
 
 _lib = None
 
@@ -124,6 +133,18 @@ def load_library():
     L.stq_engine_read.argtypes = [vp, C.POINTER(Bits), C.POINTER(Bits), C.POINTER(Codes), C.POINTER(C.c_double),
                                   C.POINTER(DecideState), vp]
     L.stq_engine_destroy.argtypes = [vp]
+    mat = C.POINTER(Matrix)
+    L.stq_quantize_rows.argtypes = [vp, mat, mat, vp]
+    L.stq_dequantize_rows.argtypes = [vp, mat, mat, vp]
+    L.stq_rms_norm.argtypes = [vp, mat, mat, vp, C.c_float, mat, mat, mat, vp, vp]
+    L.stq_rms_norm_grad.argtypes = [vp, mat, vp, vp, mat, mat, mat, vp, vp, u64, vp]
+    L.stq_rms_norm_grad_bytes.argtypes = [u64, u64, C.POINTER(u64)]
+    L.stq_gated_silu.argtypes = [vp, mat, mat, mat, mat, mat, vp]
+    L.stq_gated_silu_grad.argtypes = [vp, mat, mat, mat, mat, mat, vp]
+    L.stq_matmul.argtypes = [vp, mat, mat, mat, vp]
+    L.stq_matmul_grad_input.argtypes = [vp, mat, mat, mat, vp]
+    L.stq_matmul_grad_weight.argtypes = [vp, mat, mat, mat, vp, u64, vp]
+    L.stq_matmul_grad_weight_bytes.argtypes = [u64, u64, u64, C.POINTER(u64)]
     for name in EXPORTS[:-1]:
         getattr(L, name).restype = C.c_int
     L.stq_strerror.argtypes = [C.c_int]
@@ -176,6 +197,27 @@ def make_plan(plan: Sequence) -> "C.Array":
     for a, p in zip(arr, plan):
         a.m_bits, a.v_bits = int(p[0]), int(p[1])
     return arr
+
+
+def make_matrix(data: Optional[int], rows: int, cols: int, dtype: int, *, stride: Optional[int] = None,
+                scales: Optional[int] = None, block: int = 0) -> Matrix:
+    """An stq_matrix: the address of a row-major matrix of dtype STQ_F32, STQ_BF16 or STQ_Q8 (then with its scales' address and
+    the columns per scale), `stride` elements from row to row (default: cols).  A program makes one for each buffer and keeps it."""
+    return Matrix(data, scales, rows, cols, cols if stride is None else stride, dtype, block)
+
+
+def rms_norm_grad_bytes(rows: int, cols: int) -> int:
+    """Bytes of workspace that Context.rms_norm_grad needs."""
+    n = C.c_uint64()
+    _check(load_library().stq_rms_norm_grad_bytes(rows, cols, C.byref(n)), "stq_rms_norm_grad_bytes")
+    return n.value
+
+
+def matmul_grad_weight_bytes(tokens: int, outputs: int, inputs: int) -> int:
+    """Bytes of workspace that Context.matmul_grad_weight needs (0: none)."""
+    n = C.c_uint64()
+    _check(load_library().stq_matmul_grad_weight_bytes(tokens, outputs, inputs, C.byref(n)), "stq_matmul_grad_weight_bytes")
+    return n.value
 
 
 def decide_due(step: int, update_every: int) -> bool:
@@ -266,6 +308,40 @@ class Context:
                stream: int = 0):
         _check(self._lib.stq_repack(self._h, numel, block, state, C.c_void_p(src), src_bits,
                                     C.c_void_p(dst), dst_bits, C.c_void_p(stream)), "stq_repack")
+
+    # operators of an 8-bit layer: the arguments are Matrix records (None where the C call takes NULL) and device addresses
+    def quantize_rows(self, x: Matrix, codes: Matrix, stream: int = 0):
+        _check(self._lib.stq_quantize_rows(self._h, x, codes, stream), "stq_quantize_rows")
+
+    def dequantize_rows(self, codes: Matrix, out: Matrix, stream: int = 0):
+        _check(self._lib.stq_dequantize_rows(self._h, codes, out, stream), "stq_dequantize_rows")
+
+    def rms_norm(self, x: Matrix, residual: Optional[Matrix], weight: int, eps: float, total: Optional[Matrix], y: Matrix,
+                 saved: Optional[Matrix] = None, rstd: Optional[int] = None, stream: int = 0):
+        """total: where x + residual goes (the C call's `sum`)."""
+        _check(self._lib.stq_rms_norm(self._h, x, residual, weight, eps, total, y, saved, rstd, stream), "stq_rms_norm")
+
+    def rms_norm_grad(self, total: Matrix, weight: int, rstd: int, dy: Matrix, dresidual: Optional[Matrix], dx: Matrix,
+                      dweight: int, workspace: int, workspace_bytes: int, stream: int = 0):
+        _check(self._lib.stq_rms_norm_grad(self._h, total, weight, rstd, dy, dresidual, dx, dweight, workspace,
+                                           workspace_bytes, stream), "stq_rms_norm_grad")
+
+    def gated_silu(self, gate: Matrix, up: Matrix, y: Matrix, saved_gate: Optional[Matrix] = None,
+                   saved_up: Optional[Matrix] = None, stream: int = 0):
+        _check(self._lib.stq_gated_silu(self._h, gate, up, y, saved_gate, saved_up, stream), "stq_gated_silu")
+
+    def gated_silu_grad(self, gate: Matrix, up: Matrix, dy: Matrix, dgate: Matrix, dup: Matrix, stream: int = 0):
+        _check(self._lib.stq_gated_silu_grad(self._h, gate, up, dy, dgate, dup, stream), "stq_gated_silu_grad")
+
+    def matmul(self, x: Matrix, w: Matrix, out: Matrix, stream: int = 0):
+        _check(self._lib.stq_matmul(self._h, x, w, out, stream), "stq_matmul")
+
+    def matmul_grad_input(self, dy: Matrix, w: Matrix, dx: Matrix, stream: int = 0):
+        _check(self._lib.stq_matmul_grad_input(self._h, dy, w, dx, stream), "stq_matmul_grad_input")
+
+    def matmul_grad_weight(self, dy: Matrix, x: Matrix, dw: Matrix, workspace: Optional[int] = None,
+                           workspace_bytes: int = 0, stream: int = 0):
+        _check(self._lib.stq_matmul_grad_weight(self._h, dy, x, dw, workspace, workspace_bytes, stream), "stq_matmul_grad_weight")
 
     def engine(self, tensors, second, plan, capacity_bits: int, block: int, *, alpha=0.1, tau=1000.0, phi=7.2,
                eps=1e-12, v_offset=0.0, flags=0, thr=(6.8, 12.0, 24.0), bits=(4, 8, 16, 32),

@@ -97,6 +97,8 @@ const char* stq_strerror(int code) {
     case STQ_EHIP: return "HIP runtime error";
     case STQ_ESTATE: return "no statistics accumulated";
     case STQ_ELIMIT: return "more tensors than the static scratch of stq_step_static holds";
+    case STQ_ESHAPE: return "matrix sizes that do not fit, or out of range";
+    case STQ_EDTYPE: return "matrix of a type that the operator does not take there";
     default: return "unknown error";
   }
 }
