@@ -14,6 +14,7 @@ namespace stq {
 namespace {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef int v16i __attribute__((ext_vector_type(16)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 typedef short v4s __attribute__((ext_vector_type(4)));
@@ -39,15 +40,146 @@ __device__ __forceinline__ Vec<N, T> load_vec(const T* row, uint32_t c, uint32_t
   return r;
 }
 
+// Four neighbouring elements of an output's row, as many as are there.
+template <uint32_t TO>
+__device__ __forceinline__ void store4(const Mat& out, uint32_t row, uint32_t col, uint32_t end, const float (&v)[4]) {
+  using T = typename Elem<TO>::type;
+  STQ_GLOBAL T* p = as_global(static_cast<T*>(out.p)) + row * out.stride + col;
+  Vec<4, T> r;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) r.e[e] = static_cast<T>(v[e]);
+  if (col + 4 <= end) {
+    __builtin_memcpy(p, &r, sizeof(r));
+  } else {
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e)
+      if (col + e < end) p[e] = r.e[e];
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- order of the tiles
+// Workgroups go to the card's eight dies in turn, each of which has an L2 of its own: a die takes a run of tiles, in an order that
+// goes through patches of up to eight rows of tiles, column by column, so that those at work together share rows and columns.
+constexpr uint32_t kDies = 8, kPatch = 8;
+struct TileAt { uint32_t row, col; };
+__device__ __forceinline__ TileAt tile_at(uint32_t id, uint32_t rows, uint32_t cols) {
+  const uint32_t total = rows * cols, each = total / kDies, more = total % kDies;
+  const uint32_t die = id % kDies, t = die * each + min(die, more) + id / kDies;
+  const uint32_t patch = t / (kPatch * cols), first = patch * kPatch, high = min(kPatch, rows - first);
+  const uint32_t in = t - first * cols;
+  return {first + in % high, in / high};
+}
+
 // ---------------------------------------------------------------------------------------------- codes by codes
-// A workgroup's 128 x 128 of the result, its four waves 64 x 64 each; 64 codes of the inner dimension at a time through LDS.
-constexpr int kTileM = 128, kTileN = 128, kStepK = 64, kRowI8 = kStepK + 16;
+// A workgroup's TM x TN of the result, its WM x WN waves a part each.  128 codes of the inner dimension at a time are loaded
+// straight into LDS, into one of two buffers while the other is worked on.  A row is 128 bytes there, eight pieces of 16, which lie at
+// the places that their number and the row's give by exclusive or, so that the reads of a fragment meet every bank once.
+// Rows beyond the matrix' end repeat its last one; a step that goes beyond the rows' end comes through registers, with zeros there.
+constexpr uint32_t kStepK = 128;
+
+template <uint32_t TO, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64) void matmul_tile_kernel(const MatmulArgs a, uint32_t tiles_m, uint32_t tiles_n) {
+#ifdef __HIP_DEVICE_COMPILE__  // (the host's compiler has no buffer descriptors)
+  constexpr uint32_t FM = TM / WM / 32, FN = TN / WN / 32;  // fragments of 32 of a wave
+  constexpr uint32_t kAtOnce = WM * WN * 8;                 // rows that a load of all waves fills
+  __shared__ __align__(1024) int8_t a0[TM * kStepK], b0[TN * kStepK], a1[TM * kStepK], b1[TN * kStepK];
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const TileAt at = tile_at(blockIdx.x, tiles_m, tiles_n);
+  const uint32_t m0 = at.row * TM, n0 = at.col * TN;
+  int8_t* const pa = static_cast<int8_t*>(a.a.p) + m0 * a.a.stride;
+  int8_t* const pb = static_cast<int8_t*>(a.b.p) + n0 * a.b.stride;
+  const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(pa, 0, 0x7FFFFFFF, 0x00020000);
+  const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(pb, 0, 0x7FFFFFFF, 0x00020000);
+  // load i of a wave fills rows kAtOnce i + 8 wave .. + 7 of LDS, in lane order
+  const uint32_t load_row = wave * 8 + (lane >> 3), piece = ((lane & 7) ^ (load_row >> 1)) & 7;
+  uint32_t oa[TM / kAtOnce], ob[TN / kAtOnce];
+#pragma unroll
+  for (uint32_t i = 0; i < TM / kAtOnce; ++i) oa[i] = min(load_row + kAtOnce * i, a.m - 1 - m0) * static_cast<uint32_t>(a.a.stride) + piece * 16;
+#pragma unroll
+  for (uint32_t i = 0; i < TN / kAtOnce; ++i) ob[i] = min(load_row + kAtOnce * i, a.n - 1 - n0) * static_cast<uint32_t>(a.b.stride) + piece * 16;
+  const auto load = [&](uint32_t k, int8_t* la, int8_t* lb) {
+    if (k + kStepK <= a.k) {
+#pragma unroll
+      for (uint32_t i = 0; i < TM / kAtOnce; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (STQ_LDS void*)(la + (i * kAtOnce + wave * 8) * kStepK), 16, oa[i], k, 0, 0);
+#pragma unroll
+      for (uint32_t i = 0; i < TN / kAtOnce; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (STQ_LDS void*)(lb + (i * kAtOnce + wave * 8) * kStepK), 16, ob[i], k, 0, 0);
+    } else if (k < a.k) {
+      const auto rest = [&](const int8_t* p, uint64_t stride, uint32_t last, int8_t* to, uint32_t rows) {
+#pragma unroll 1
+        for (uint32_t r = load_row; r < rows; r += kAtOnce) {
+          const Vec<16, int8_t> v = load_vec<16>(p + min(r, last) * stride, k + piece * 16, a.k, true);
+          __builtin_memcpy(to + r * kStepK + (lane & 7) * 16, &v, 16);
+        }
+      };
+      rest(pa, a.a.stride, a.m - 1 - m0, la, TM);
+      rest(pb, a.b.stride, a.n - 1 - n0, lb, TN);
+    }
+  };
+  v16i acc[FM][FN] = {};
+  const uint32_t wm = wave / WN * (TM / WM), wn = wave % WN * (TN / WN);
+  const auto work = [&](const int8_t* la, const int8_t* lb) {
+#pragma unroll
+    for (uint32_t s = 0; s < kStepK / 32; ++s) {
+      v4i fa[FM], fb[FN];
+      const uint32_t r = lane & 31, place = ((2 * s + (lane >> 5)) ^ (r >> 1)) & 7;
+#pragma unroll
+      for (uint32_t i = 0; i < FM; ++i) fa[i] = *reinterpret_cast<const v4i*>(la + (wm + i * 32 + r) * kStepK + place * 16);
+#pragma unroll
+      for (uint32_t j = 0; j < FN; ++j) fb[j] = *reinterpret_cast<const v4i*>(lb + (wn + j * 32 + r) * kStepK + place * 16);
+#pragma unroll
+      for (uint32_t i = 0; i < FM; ++i)
+#pragma unroll
+        for (uint32_t j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
+    }
+  };
+  load(0, a0, b0);
+  for (uint32_t k = 0;; k += 2 * kStepK) {
+    __syncthreads();
+    load(k + kStepK, a1, b1);
+    work(a0, b0);
+    if (k + kStepK >= a.k) break;
+    __syncthreads();
+    load(k + 2 * kStepK, a0, b0);
+    work(a1, b1);
+    if (k + 2 * kStepK >= a.k) break;
+  }
+  // w's rows along the fragments' rows: a lane has four neighbouring outputs of one token at a time
+  // the scales by way of LDS, into which nothing is loaded any more
+  __syncthreads();
+  float* const sm = reinterpret_cast<float*>(a0);
+  float* const sn = reinterpret_cast<float*>(b0);
+  for (uint32_t i = threadIdx.x; i < TM; i += WM * WN * 64) sm[i] = as_global(a.a.s)[min(m0 + i, a.m - 1)];
+  for (uint32_t i = threadIdx.x; i < TN; i += WM * WN * 64) sn[i] = as_global(a.b.s)[min(n0 + i, a.n - 1)];
+  __syncthreads();
+#pragma unroll
+  for (uint32_t i = 0; i < FM; ++i) {
+    const uint32_t r = wm + i * 32 + (lane & 31), m = m0 + r;
+    const float s = sm[r];
+#pragma unroll
+    for (uint32_t j = 0; j < FN; ++j)
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q) {
+        const uint32_t c = wn + j * 32 + q * 8 + (lane >> 5) * 4;
+        float v[4];
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) v[e] = static_cast<float>(acc[i][j][q * 4 + e]) * s * sn[c + e];
+        if (m < a.m) store4<TO>(a.out, m, n0 + c, a.n, v);
+      }
+  }
+#endif
+}
+
+// The same for operands of any alignment and inner size, through registers: 128 x 128 of the result, 64 codes at a time.
+constexpr uint32_t kAnyM = 128, kAnyN = 128, kAnyK = 64, kAnyRow = kAnyK + 16;
 
 template <uint32_t TO>
-__global__ __launch_bounds__(256) void matmul_kernel(const MatmulArgs a) {
-  __shared__ __align__(16) int8_t sa[kTileM * kRowI8], sb[kTileN * kRowI8];
+__global__ __launch_bounds__(256) void matmul_any_kernel(const MatmulArgs a, uint32_t tiles_m, uint32_t tiles_n) {
+  __shared__ __align__(16) int8_t sa[kAnyM * kAnyRow], sb[kAnyN * kAnyRow];
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t m0 = blockIdx.y * kTileM, n0 = blockIdx.x * kTileN;
+  const TileAt at = tile_at(blockIdx.x, tiles_m, tiles_n);
+  const uint32_t m0 = at.row * kAnyM, n0 = at.col * kAnyN;
   const uint32_t row = threadIdx.x >> 2, col = (threadIdx.x & 3) * 16;  // of a thread's two vectors of either tile, 64 rows apart
   const int8_t* pa = static_cast<const int8_t*>(a.a.p);
   const int8_t* pb = static_cast<const int8_t*>(a.b.p);
@@ -63,42 +195,105 @@ __global__ __launch_bounds__(256) void matmul_kernel(const MatmulArgs a) {
   v4i acc[4][4] = {};
   const uint32_t wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
   load(0);
-  for (uint32_t k = 0; k < a.k; k += kStepK) {
+  for (uint32_t k = 0; k < a.k; k += kAnyK) {
     __syncthreads();
 #pragma unroll
     for (uint32_t h = 0; h < 2; ++h) {
-      __builtin_memcpy(sa + (row + 64 * h) * kRowI8 + col, &va[h], 16);
-      __builtin_memcpy(sb + (row + 64 * h) * kRowI8 + col, &vb[h], 16);
+      __builtin_memcpy(sa + (row + 64 * h) * kAnyRow + col, &va[h], 16);
+      __builtin_memcpy(sb + (row + 64 * h) * kAnyRow + col, &vb[h], 16);
     }
     __syncthreads();
-    if (k + kStepK < a.k) load(k + kStepK);
+    if (k + kAnyK < a.k) load(k + kAnyK);
     v4i fa[4], fb[4];
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) {
-      fa[i] = *reinterpret_cast<const v4i*>(sa + (wm + i * 16 + (lane & 15)) * kRowI8 + (lane >> 4) * 16);
-      fb[i] = *reinterpret_cast<const v4i*>(sb + (wn + i * 16 + (lane & 15)) * kRowI8 + (lane >> 4) * 16);
+      fa[i] = *reinterpret_cast<const v4i*>(sa + (wm + i * 16 + (lane & 15)) * kAnyRow + (lane >> 4) * 16);
+      fb[i] = *reinterpret_cast<const v4i*>(sb + (wn + i * 16 + (lane & 15)) * kAnyRow + (lane >> 4) * 16);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[i], fb[j], acc[i][j], 0, 0, 0);
+      for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
   }
-  using T = typename Elem<TO>::type;
 #pragma unroll
-  for (uint32_t i = 0; i < 4; ++i)
+  for (uint32_t i = 0; i < 4; ++i) {
+    const uint32_t m = m0 + wm + i * 16 + (lane & 15);
+    const float s = as_global(a.a.s)[min(m, a.m - 1)];
 #pragma unroll
-    for (uint32_t r = 0; r < 4; ++r) {
-      const uint32_t m = m0 + wm + i * 16 + (lane >> 4) * 4 + r;
-      if (m >= a.m) continue;
-      const float s = as_global(a.a.s)[m];
+    for (uint32_t j = 0; j < 4; ++j) {
+      const uint32_t n = n0 + wn + j * 16 + (lane >> 4) * 4;
+      float v[4];
 #pragma unroll
-      for (uint32_t j = 0; j < 4; ++j) {
-        const uint32_t n = n0 + wn + j * 16 + (lane & 15);
-        if (n < a.n)
-          as_global(static_cast<T*>(a.out.p))[m * a.out.stride + n] =
-              static_cast<T>(static_cast<float>(acc[i][j][r]) * s * as_global(a.b.s)[n]);
+      for (uint32_t e = 0; e < 4; ++e) v[e] = static_cast<float>(acc[i][j][e]) * s * as_global(a.b.s)[min(n + e, a.n - 1)];
+      if (m < a.m) store4<TO>(a.out, m, n, a.n, v);
+    }
+  }
+}
+
+__device__ __forceinline__ v4i load_fragment(const int8_t* p) {
+  v4i v;
+  __builtin_memcpy(&v, as_global(p), 16);
+  return v;
+}
+
+// Few tokens: what counts is how fast w's codes arrive.  A workgroup has 16 of w's rows and up to 16 G tokens; its eight waves share
+// the inner dimension, a run of 128 codes each in turn, read straight into the fragments, and add up at the end.
+template <uint32_t TO, int G>
+__global__ __launch_bounds__(512) void matmul_few_kernel(const MatmulArgs a) {
+  __shared__ __align__(16) v4i part[8][G][64];
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * G;
+  const uint32_t row = lane & 15, piece = (lane >> 4) * 16;
+  const int8_t* pw = static_cast<const int8_t*>(a.b.p) + min(n0 + row, a.n - 1) * a.b.stride;
+  const int8_t* px[G];
+#pragma unroll
+  for (uint32_t g = 0; g < G; ++g) px[g] = static_cast<const int8_t*>(a.a.p) + min(m0 + g * 16 + row, a.m - 1) * a.a.stride;
+  v4i acc[G] = {};
+  uint32_t k = wave * 128 + piece;
+  constexpr uint32_t kAhead = 4;  // runs whose loads are under way together
+  for (; (k & ~127u) + (kAhead - 1) * 1024 + 128 <= a.k; k += kAhead * 1024) {
+    v4i fw[2 * kAhead], fx[G][2 * kAhead];
+#pragma unroll
+    for (uint32_t h = 0; h < 2 * kAhead; ++h) {
+      const uint32_t c = k + (h >> 1) * 1024 + (h & 1) * 64;
+      fw[h] = load_fragment(pw + c);
+#pragma unroll
+      for (uint32_t g = 0; g < G; ++g) fx[g][h] = load_fragment(px[g] + c);
+    }
+#pragma unroll
+    for (uint32_t h = 0; h < 2 * kAhead; ++h)
+#pragma unroll
+      for (uint32_t g = 0; g < G; ++g) acc[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[h], fx[g][h], acc[g], 0, 0, 0);
+  }
+  for (; (k & ~127u) < a.k; k += 1024) {
+#pragma unroll
+    for (uint32_t h = 0; h < 2; ++h) {
+      const Vec<16, int8_t> w = load_vec<16>(pw, k + h * 64, a.k, true);
+      v4i fw;
+      __builtin_memcpy(&fw, &w, 16);
+#pragma unroll
+      for (uint32_t g = 0; g < G; ++g) {
+        const Vec<16, int8_t> x = load_vec<16>(px[g], k + h * 64, a.k, true);
+        v4i fx;
+        __builtin_memcpy(&fx, &x, 16);
+        acc[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw, fx, acc[g], 0, 0, 0);
       }
     }
+  }
+#pragma unroll
+  for (uint32_t g = 0; g < G; ++g) part[wave][g][lane] = acc[g];
+  __syncthreads();
+  if (wave >= G) return;
+  v4i sum = part[0][wave][lane];
+#pragma unroll
+  for (uint32_t w = 1; w < 8; ++w) sum += part[w][wave][lane];
+  const uint32_t m = m0 + wave * 16 + row, n = n0 + (lane >> 4) * 4;
+  if (m >= a.m) return;
+  const float s = as_global(a.a.s)[m];
+  float v[4];
+#pragma unroll
+  for (uint32_t e = 0; e < 4; ++e) v[e] = static_cast<float>(sum[e]) * s * as_global(a.b.s)[min(n + e, a.n - 1)];
+  store4<TO>(a.out, m, n, a.n, v);
 }
 
 // ---------------------------------------------------------------------------------------------- gradients
@@ -203,6 +398,32 @@ __global__ __launch_bounds__(256) void grad_kernel(const MatmulArgs a, uint32_t 
     }
 }
 
+uint32_t tiles_of(uint32_t size, uint32_t tile) { return (size - 1) / tile + 1; }
+
+// Whether a matrix' rows can be loaded straight into LDS: 16-byte pieces, a tile's rows within reach of a 31-bit offset.
+bool in_pieces(const Mat& x) { return (reinterpret_cast<uintptr_t>(x.p) & 15) == 0 && x.stride % 16 == 0 && x.stride < (1u << 22); }
+
+template <uint32_t TO>
+void run_matmul(const MatmulArgs& a, uint32_t n_cu, hipStream_t st) {
+  if (a.m <= 64) {
+    const uint32_t groups = tiles_of(a.n, 16);
+    if (a.m <= 16) matmul_few_kernel<TO, 1><<<groups, 512, 0, st>>>(a);
+    else if (a.m <= 32) matmul_few_kernel<TO, 2><<<groups, 512, 0, st>>>(a);
+    else matmul_few_kernel<TO, 4><<<groups, 512, 0, st>>>(a);
+    return;
+  }
+  if (!in_pieces(a.a) || !in_pieces(a.b)) {
+    const uint32_t rows = tiles_of(a.m, kAnyM), cols = tiles_of(a.n, kAnyN);
+    matmul_any_kernel<TO><<<rows * cols, 256, 0, st>>>(a, rows, cols);
+    return;
+  }
+  const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(a.m, t)) * tiles_of(a.n, t); };
+  const uint32_t t = count(256) >= n_cu ? 256 : (count(128) >= n_cu ? 128 : 64), rows = tiles_of(a.m, t), cols = tiles_of(a.n, t);
+  if (t == 256) matmul_tile_kernel<TO, 256, 256, 2, 4><<<rows * cols, 512, 0, st>>>(a, rows, cols);
+  else if (t == 128) matmul_tile_kernel<TO, 128, 128, 2, 2><<<rows * cols, 256, 0, st>>>(a, rows, cols);
+  else matmul_tile_kernel<TO, 64, 64, 2, 2><<<rows * cols, 256, 0, st>>>(a, rows, cols);
+}
+
 template <class F>
 void with_type(uint32_t type, F f) {
   if (type == kF32) f(std::integral_constant<uint32_t, kF32>{});
@@ -212,8 +433,8 @@ void with_type(uint32_t type, F f) {
 }  // namespace
 
 int launch_matmul(const MatmulArgs& a, uint32_t out_type, uint32_t n_cu, void* stream) {
-  const dim3 grid((a.n - 1) / kTileN + 1, (a.m - 1) / kTileM + 1);
-  with_type(out_type, [&](auto to) { matmul_kernel<to()><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a); });
+  if (out_type == kF32) run_matmul<kF32>(a, n_cu, static_cast<hipStream_t>(stream));
+  else run_matmul<kBF16>(a, n_cu, static_cast<hipStream_t>(stream));
   return hipGetLastError();
 }
 int launch_matmul_grad_input(const MatmulArgs& a, uint32_t dy_type, uint32_t out_type, uint32_t n_cu, void* stream) {
