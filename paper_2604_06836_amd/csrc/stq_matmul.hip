@@ -3,7 +3,6 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
-#include <type_traits>
 
 #include "stq_operators.h"
 #include "stq_wave.h"
@@ -15,7 +14,7 @@ namespace {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v16i __attribute__((ext_vector_type(16)));
-typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 #define STQ_LDS __attribute__((address_space(3)))
@@ -55,6 +54,13 @@ __device__ __forceinline__ void store4(const Mat& out, uint32_t row, uint32_t co
     for (uint32_t e = 0; e < 4; ++e)
       if (col + e < end) p[e] = r.e[e];
   }
+}
+
+template <int N, class T>
+__device__ __forceinline__ Vec<N, T> load_whole(const T* p) {
+  Vec<N, T> r;
+  __builtin_memcpy(&r, as_global(p), sizeof(r));
+  return r;
 }
 
 // ---------------------------------------------------------------------------------------------- order of the tiles
@@ -299,103 +305,196 @@ __global__ __launch_bounds__(512) void matmul_few_kernel(const MatmulArgs a) {
 // ---------------------------------------------------------------------------------------------- gradients
 // out[i][j] = sum over c of dy(i, c) * s(c) * q(c, j): with respect to the input (WEIGHT false) i is the token and c the output, and
 // dy's rows run along c; with respect to the weight i is the output and c the token, and dy's rows run along i.  The codes' rows run
-// along j.  Codes are whole numbers below 2^8 and exact in bf16.  dy * s is rounded to bf16, or with TERMS = 2 to the sum of two, for
-// results in fp32: what is left out is then at most 2^-16 of it.  Operands whose rows run along the result's rows or columns are read
-// out of LDS transposed, four rows of 16 columns at a time.
-constexpr int kTileI = 128, kTileJ = 128, kStepC = 32;
-constexpr int kRowC = kStepC + 8;    // LDS row of an operand that runs along c
-constexpr int kRowX = kTileI + 16;   // LDS row of one that runs along i or j
+// along j.  Codes are whole numbers below 2^8 and exact in bf16.  dy * s is rounded to bf16, or for results in fp32 to the sum of
+// three, which hold all 24 bits of it.
+// A workgroup has TI x TJ of the result, its WI x WJ waves a part each, and takes STEP of c at a time: what a step needs is loaded
+// into registers two steps ahead, turned into bf16 and put into one of two LDS buffers one step ahead.  Operands whose rows run along
+// i or j are read out of LDS transposed, four rows of 16 columns at a time.
+template <uint32_t TO> constexpr int kTerms = TO == kF32 ? 3 : 1;
 
-// a fragment of 16 columns from x0 on and 32 rows of a [c][x] tile: eight neighbouring rows of one column to a lane
-__device__ __forceinline__ v8b transposed(const __bf16* tile, uint32_t x0, uint32_t lane) {
-  const __bf16* p = tile + ((lane >> 4) * 8 + ((lane & 15) >> 2)) * kRowX + x0 + (lane & 3) * 4;
+// A [c][x] tile: rows of X elements, 64 bytes more apart than that, so that the four rows of a transposed read meet every bank once.
+template <uint32_t X> constexpr uint32_t kRowX = X + 32;
+// A [i][c] tile of C = 32 or 64 elements a row, in pieces of eight which lie at the places that their number and the row's give by
+// exclusive or, for the same reason.
+template <uint32_t C>
+__device__ __forceinline__ uint32_t place_c(uint32_t row, uint32_t piece) {
+  return row * C + (C == 32 ? piece ^ ((row >> 2) & 3) : piece ^ ((row >> 1) & 7)) * 8;
+}
+
+// The fragment of columns x0 .. x0+31 and rows c0 .. c0+15 of a [c][x] tile: eight neighbouring rows of one column to a lane.
+template <uint32_t X>
+__device__ __forceinline__ v8b transposed(const __bf16* tile, uint32_t c0, uint32_t x0, uint32_t lane) {
+  const __bf16* p = tile + (c0 + (lane >> 5) * 8 + ((lane & 15) >> 2)) * kRowX<X> + x0 + (lane & 16) + (lane & 3) * 4;
   const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((STQ_LDS v4s*)(p));
-  const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((STQ_LDS v4s*)(p + 4 * kRowX));
+  const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((STQ_LDS v4s*)(p + 4 * kRowX<X>));
   v8b r;
   __builtin_memcpy(&r, &lo, 8);
   __builtin_memcpy(reinterpret_cast<char*>(&r) + 8, &hi, 8);
   return r;
 }
 
-template <bool WEIGHT, uint32_t TY, uint32_t TO>
-__global__ __launch_bounds__(256) void grad_kernel(const MatmulArgs a, uint32_t ni, uint32_t nj, uint32_t nc) {
-  constexpr int kTerms = TO == kF32 ? 2 : 1;
-  constexpr int kSizeA = WEIGHT ? kStepC * kRowX : kTileI * kRowC;
-  __shared__ __align__(16) __bf16 sa[kTerms][kSizeA], sb[kStepC * kRowX];
-  using T = typename Elem<TY>::type;
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t i0 = blockIdx.y * kTileI, j0 = blockIdx.x * kTileJ;
-  const T* dy = static_cast<const T*>(a.a.p);
-  const int8_t* q = static_cast<const int8_t*>(a.b.p);
-  // a thread's two vectors of eight: of a tile along x rows 16 apart, of one along c rows 64 apart
-  const uint32_t xr = threadIdx.x >> 4, xc = (threadIdx.x & 15) * 8, cr = threadIdx.x >> 2, cc = (threadIdx.x & 3) * 8;
-  Vec<8, T> va[2];
-  Vec<8, int8_t> vb[2];
-  Vec<8, float> vs;
-  auto load = [&](uint32_t c) {
+// Elements x .. x+7 of a row of `size`: what lies beyond its end is anything that the row holds (it meets zeros, or results that are
+// not stored).  EIGHTS: sizes and x are multiples of eight, so that a vector is there or is not.
+template <bool EIGHTS, class T>
+__device__ __forceinline__ Vec<8, T> load_eight(const T* row, uint32_t x, uint32_t size) {
+  if constexpr (EIGHTS) return load_whole<8>(row + min(x, size - 8));
+  Vec<8, T> r;
 #pragma unroll
-    for (uint32_t h = 0; h < 2; ++h) {
-      const uint32_t row = c + xr + 16 * h;
-      vb[h] = load_vec<8>(q + row * a.b.stride, j0 + xc, nj, row < nc);
+  for (uint32_t e = 0; e < 8; ++e) r.e[e] = as_global(row)[min(x + e, size - 1)];
+  return r;
+}
+
+struct GradShape {
+  uint32_t ni, nj, nc;      // sizes of the sum
+  uint32_t tiles_i, tiles_j;
+  uint32_t splits, each;    // parts of c, and their length (a multiple of the step)
+  float* partial;           // [splits][ni][nj] where there are several
+};
+
+template <bool WEIGHT, bool EIGHTS, uint32_t TY, uint32_t TO, int TI, int TJ, int WI, int WJ, int STEP>
+__global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, const GradShape g) {
+  constexpr uint32_t kThreads = WI * WJ * 64, FI = TI / WI / 32, FJ = TJ / WJ / 32, T = kTerms<TO>;
+  constexpr uint32_t kSizeA = WEIGHT ? STEP * kRowX<TI> : TI * STEP, kSizeB = STEP * kRowX<TJ>;
+  constexpr uint32_t VA = TI * STEP / 8 / kThreads, VB = TJ * STEP / 8 / kThreads;  // vectors of eight of a thread
+  __shared__ __align__(16) __bf16 sa0[T][kSizeA], sb0[kSizeB], sa1[T][kSizeA], sb1[kSizeB];
+  using D = typename Elem<TY>::type;
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const TileAt at = tile_at(blockIdx.x, g.tiles_i, g.tiles_j);
+  const uint32_t i0 = at.row * TI, j0 = at.col * TJ;
+  const uint32_t first = blockIdx.y * g.each, end = min(g.nc, first + g.each);
+  const D* const dy = static_cast<const D*>(a.a.p);
+  const int8_t* const q = static_cast<const int8_t*>(a.b.p);
+  const float* const scales = a.b.s;
+  // where a thread's vectors lie: of a [c][x] tile kThreads / (X / 8) rows apart, of the [i][c] one kThreads / (STEP / 8)
+  constexpr uint32_t kApartB = kThreads / (TJ / 8), kApartA = WEIGHT ? kThreads / (TI / 8) : kThreads / (STEP / 8);
+  const uint32_t br = threadIdx.x / (TJ / 8), bc = threadIdx.x % (TJ / 8) * 8;
+  const uint32_t ar = threadIdx.x / (WEIGHT ? TI / 8 : STEP / 8), ac = threadIdx.x % (WEIGHT ? TI / 8 : STEP / 8) * 8;
+
+  Vec<8, D> va[VA];
+  Vec<8, int8_t> vb[VB];
+  Vec<8, float> vs;
+  const auto load = [&](uint32_t c) {
+#pragma unroll
+    for (uint32_t h = 0; h < VB; ++h) vb[h] = load_eight<EIGHTS>(q + min(c + br + kApartB * h, end - 1) * a.b.stride, j0 + bc, g.nj);
+#pragma unroll
+    for (uint32_t h = 0; h < VA; ++h) {
       if (WEIGHT) {
-        va[h] = load_vec<8>(dy + row * a.a.stride, i0 + xc, ni, row < nc);
-        vs.e[h] = row < nc ? as_global(a.b.s)[row] : 0.0f;
+        const uint32_t row = min(c + ar + kApartA * h, end - 1);
+        va[h] = load_eight<EIGHTS>(dy + row * a.a.stride, i0 + ac, g.ni);
+        vs.e[h] = as_global(scales)[row];
       } else {
-        const uint32_t i = i0 + cr + 64 * h;
-        va[h] = load_vec<8>(dy + i * a.a.stride, c + cc, nc, i < ni);
+        va[h] = load_eight<EIGHTS>(dy + min(i0 + ar + kApartA * h, g.ni - 1) * a.a.stride, c + ac, end);
       }
     }
-    if (!WEIGHT) vs = load_vec<8>(a.b.s, c + cc, nc, true);
-  };
-  v4f acc[4][4] = {};
-  const uint32_t wi = (wave >> 1) * 64, wj = (wave & 1) * 64;
-  load(0);
-  for (uint32_t c = 0; c < nc; c += kStepC) {
-    __syncthreads();
+    if (!WEIGHT) vs = load_eight<EIGHTS>(scales, c + ac, end);
+    if (c + STEP <= end) return;
+    // the last step of a sum whose length is no multiple: zeros in place of what comes after it
 #pragma unroll
-    for (uint32_t h = 0; h < 2; ++h) {
-      v8b t[kTerms], b;
+    for (uint32_t h = 0; h < VA; ++h)
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e)
+        if ((WEIGHT ? c + ar + kApartA * h : c + ac + e) >= end) {
+          va[h].e[e] = static_cast<D>(0.0f);
+          vs.e[WEIGHT ? h : e] = 0.0f;
+        }
+  };
+  const auto put = [&](__bf16 (*ta)[kSizeA], __bf16* tb) {
+#pragma unroll
+    for (uint32_t h = 0; h < VA; ++h) {
+      v8b t[T];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float x = static_cast<float>(va[h].e[e]) * (WEIGHT ? vs.e[h] : vs.e[e]);
-        t[0][e] = static_cast<__bf16>(x);
-        if (kTerms == 2) t[kTerms - 1][e] = static_cast<__bf16>(x - static_cast<float>(t[0][e]));
-        b[e] = static_cast<__bf16>(static_cast<float>(vb[h].e[e]));
+        float x = static_cast<float>(va[h].e[e]) * (WEIGHT ? vs.e[h] : vs.e[e]);
+#pragma unroll
+        for (uint32_t k = 0; k < T; ++k) {
+          t[k][e] = static_cast<__bf16>(x);
+          x -= static_cast<float>(t[k][e]);
+        }
       }
-      const uint32_t at = WEIGHT ? (xr + 16 * h) * kRowX + xc : (cr + 64 * h) * kRowC + cc;
+      const uint32_t row = ar + kApartA * h, to = WEIGHT ? row * kRowX<TI> + ac : place_c<STEP>(row, ac / 8);
 #pragma unroll
-      for (int k = 0; k < kTerms; ++k) __builtin_memcpy(&sa[k][at], &t[k], 16);
-      __builtin_memcpy(&sb[(xr + 16 * h) * kRowX + xc], &b, 16);
+      for (uint32_t k = 0; k < T; ++k) __builtin_memcpy(&ta[k][to], &t[k], 16);
     }
+#pragma unroll
+    for (uint32_t h = 0; h < VB; ++h) {
+      v8b t;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = static_cast<__bf16>(static_cast<float>(vb[h].e[e]));
+      __builtin_memcpy(&tb[(br + kApartB * h) * kRowX<TJ> + bc], &t, 16);
+    }
+  };
+  v16f acc[FI][FJ] = {};
+  const uint32_t wi = wave / WJ * (TI / WI), wj = wave % WJ * (TJ / WJ);
+  const auto work = [&](const __bf16 (*ta)[kSizeA], const __bf16* tb) {
+#pragma unroll
+    for (uint32_t c = 0; c < STEP; c += 16) {
+      v8b fb[FJ];
+#pragma unroll
+      for (uint32_t j = 0; j < FJ; ++j) fb[j] = transposed<TJ>(tb, c, wj + j * 32, lane);
+#pragma unroll
+      for (uint32_t k = 0; k < T; ++k)
+#pragma unroll
+        for (uint32_t i = 0; i < FI; ++i) {
+          v8b fa;
+          if (WEIGHT) fa = transposed<TI>(ta[k], c, wi + i * 32, lane);
+          else __builtin_memcpy(&fa, &ta[k][place_c<STEP>(wi + i * 32 + (lane & 31), c / 8 + (lane >> 5))], 16);
+#pragma unroll
+          for (uint32_t j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa, acc[i][j], 0, 0, 0);
+        }
+    }
+  };
+  // (loads and puts beyond the last step repeat its rows and are not used)
+  load(first);
+  put(sa0, sb0);
+  load(first + STEP);
+  for (uint32_t c = first;; c += 2 * STEP) {
     __syncthreads();
-    if (c + kStepC < nc) load(c + kStepC);
-    v8b fb[4];
+    put(sa1, sb1);
+    load(c + 2 * STEP);
+    work(sa0, sb0);
+    if (c + STEP >= end) break;
+    __syncthreads();
+    put(sa0, sb0);
+    load(c + 3 * STEP);
+    work(sa1, sb1);
+    if (c + 2 * STEP >= end) break;
+  }
+  // the codes' columns along the fragments' rows: a lane has four neighbouring columns of one row at a time
+  const Mat part{g.partial + static_cast<uint64_t>(blockIdx.y) * g.ni * g.nj, nullptr, g.nj, 0, 0};
 #pragma unroll
-    for (uint32_t j = 0; j < 4; ++j) fb[j] = transposed(sb, wj + j * 16, lane);
+  for (uint32_t i = 0; i < FI; ++i) {
+    const uint32_t row = i0 + wi + i * 32 + (lane & 31);
+    if (row >= g.ni) continue;
 #pragma unroll
-    for (int k = 0; k < kTerms; ++k)
+    for (uint32_t j = 0; j < FJ; ++j)
 #pragma unroll
-      for (uint32_t i = 0; i < 4; ++i) {
-        v8b fa;
-        if (WEIGHT) fa = transposed(sa[k], wi + i * 16, lane);
-        else __builtin_memcpy(&fa, &sa[k][(wi + i * 16 + (lane & 15)) * kRowC + (lane >> 4) * 8], 16);
+      for (uint32_t p = 0; p < 4; ++p) {
+        const uint32_t col = j0 + wj + j * 32 + p * 8 + (lane >> 5) * 4;
+        float v[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
+        for (uint32_t e = 0; e < 4; ++e) v[e] = acc[i][j][p * 4 + e];
+        if (col >= g.nj) continue;
+        if (g.splits > 1) store4<kF32>(part, row, col, g.nj, v);
+        else store4<TO>(a.out, row, col, g.nj, v);
       }
   }
-  using O = typename Elem<TO>::type;
+}
+
+// The parts of a sum that was taken in parts, in one order.
+template <uint32_t TO>
+__global__ __launch_bounds__(256) void join_kernel(const Mat out, const float* partial, uint32_t splits, uint32_t ni, uint32_t nj) {
+  const uint32_t per_row = (nj + 3) / 4;
+  const uint64_t total = static_cast<uint64_t>(ni) * per_row, size = static_cast<uint64_t>(ni) * nj;
+  for (uint64_t t = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; t < total; t += static_cast<uint64_t>(gridDim.x) * 256) {
+    const uint32_t row = static_cast<uint32_t>(t / per_row), col = static_cast<uint32_t>(t % per_row) * 4;
+    float v[4] = {0, 0, 0, 0};
+    for (uint32_t k = 0; k < splits; ++k) {
+      const Vec<4, float> p = load_vec<4>(partial + k * size + static_cast<uint64_t>(row) * nj, col, nj, true);
 #pragma unroll
-  for (uint32_t i = 0; i < 4; ++i)
-#pragma unroll
-    for (uint32_t r = 0; r < 4; ++r) {
-      const uint32_t row = i0 + wi + i * 16 + (lane >> 4) * 4 + r;
-      if (row >= ni) continue;
-#pragma unroll
-      for (uint32_t j = 0; j < 4; ++j) {
-        const uint32_t col = j0 + wj + j * 16 + (lane & 15);
-        if (col < nj) as_global(static_cast<O*>(a.out.p))[row * a.out.stride + col] = static_cast<O>(acc[i][j][r]);
-      }
+      for (int e = 0; e < 4; ++e) v[e] += p.e[e];
     }
+    store4<TO>(out, row, col, nj, v);
+  }
 }
 
 uint32_t tiles_of(uint32_t size, uint32_t tile) { return (size - 1) / tile + 1; }
@@ -424,10 +523,51 @@ void run_matmul(const MatmulArgs& a, uint32_t n_cu, hipStream_t st) {
   else matmul_tile_kernel<TO, 64, 64, 2, 2><<<rows * cols, 256, 0, st>>>(a, rows, cols);
 }
 
-template <class F>
-void with_type(uint32_t type, F f) {
-  if (type == kF32) f(std::integral_constant<uint32_t, kF32>{});
-  else f(std::integral_constant<uint32_t, kBF16>{});
+// Parts of the tokens for a weight gradient of few tiles: as many as give every CU a workgroup, of 512 tokens at least (a part
+// costs a write and a read of the result in fp32).
+constexpr uint32_t kCus = 256, kLeastPart = 512;
+uint32_t splits_of(uint64_t m, uint64_t n, uint64_t k) {
+  const uint64_t tiles = ((n + 127) / 128) * ((k + 127) / 128);
+  if (tiles * 2 > kCus || m < 2 * kLeastPart) return 1;
+  const uint64_t s = kCus / tiles, most = m / kLeastPart;
+  return static_cast<uint32_t>(s < most ? s : most);
+}
+
+template <bool WEIGHT, uint32_t TY, uint32_t TO>
+void run_grad(const MatmulArgs& a, GradShape g, uint32_t n_cu, hipStream_t st) {
+  constexpr int kStepC = 32;
+  const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(g.ni, t)) * tiles_of(g.nj, t); };
+  const bool eights = g.nj % 8 == 0 && (WEIGHT ? g.ni : g.nc) % 8 == 0;
+  const uint32_t t = eights && g.splits == 1 && count(256) >= n_cu ? 256 : 128;
+  g.tiles_i = tiles_of(g.ni, t);
+  g.tiles_j = tiles_of(g.nj, t);
+  const auto join = [&] {
+    const uint64_t groups = (static_cast<uint64_t>(g.ni) * ((g.nj + 3) / 4) + 255) / 256;
+    join_kernel<TO><<<static_cast<uint32_t>(groups < 4096 ? groups : 4096), 256, 0, st>>>(a.out, g.partial, g.splits, g.ni, g.nj);
+  };
+  if (g.nc == 0) {  // no tokens: a sum of nothing
+    g.splits = 0;
+    return join();
+  }
+  g.each = tiles_of(g.nc, g.splits * 64) * 64;
+  g.splits = tiles_of(g.nc, g.each);
+  const dim3 grid(g.tiles_i * g.tiles_j, g.splits);
+  if (!eights) grad_kernel<WEIGHT, false, TY, TO, 128, 128, 2, 2, kStepC><<<grid, 256, 0, st>>>(a, g);
+  else if (t == 256) grad_kernel<WEIGHT, true, TY, TO, 256, 256, 2, 4, kStepC><<<grid, 512, 0, st>>>(a, g);
+  else grad_kernel<WEIGHT, true, TY, TO, 128, 128, 2, 2, kStepC><<<grid, 256, 0, st>>>(a, g);
+  if (g.splits > 1) join();
+}
+template <bool WEIGHT>
+int run_grads(const MatmulArgs& a, const GradShape& g, uint32_t dy_type, uint32_t out_type, uint32_t n_cu, void* stream) {
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dy_type == kF32) {
+    if (out_type == kF32) run_grad<WEIGHT, kF32, kF32>(a, g, n_cu, st);
+    else run_grad<WEIGHT, kF32, kBF16>(a, g, n_cu, st);
+  } else {
+    if (out_type == kF32) run_grad<WEIGHT, kBF16, kF32>(a, g, n_cu, st);
+    else run_grad<WEIGHT, kBF16, kBF16>(a, g, n_cu, st);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -438,19 +578,14 @@ int launch_matmul(const MatmulArgs& a, uint32_t out_type, uint32_t n_cu, void* s
   return hipGetLastError();
 }
 int launch_matmul_grad_input(const MatmulArgs& a, uint32_t dy_type, uint32_t out_type, uint32_t n_cu, void* stream) {
-  const dim3 grid((a.k - 1) / kTileJ + 1, (a.m - 1) / kTileI + 1);
-  with_type(dy_type, [&](auto ty) { with_type(out_type, [&](auto to) {
-    grad_kernel<false, ty(), to()><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, a.m, a.k, a.n);
-  }); });
-  return hipGetLastError();
+  return run_grads<false>(a, GradShape{a.m, a.k, a.n, 0, 0, 1, 0, nullptr}, dy_type, out_type, n_cu, stream);
 }
 int launch_matmul_grad_weight(const MatmulArgs& a, uint32_t dy_type, uint32_t out_type, float* workspace, uint32_t n_cu, void* stream) {
-  const dim3 grid((a.k - 1) / kTileJ + 1, (a.n - 1) / kTileI + 1);
-  with_type(dy_type, [&](auto ty) { with_type(out_type, [&](auto to) {
-    grad_kernel<true, ty(), to()><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, a.n, a.k, a.m);
-  }); });
-  return hipGetLastError();
+  return run_grads<true>(a, GradShape{a.n, a.k, a.m, 0, 0, splits_of(a.m, a.n, a.k), 0, workspace}, dy_type, out_type, n_cu, stream);
 }
-uint64_t grad_weight_bytes(uint64_t m, uint64_t n, uint64_t k) { return 0; }
+uint64_t grad_weight_bytes(uint64_t m, uint64_t n, uint64_t k) {
+  const uint64_t s = splits_of(m, n, k);
+  return s > 1 ? 4 * s * n * k : 0;
+}
 
 }  // namespace stq
