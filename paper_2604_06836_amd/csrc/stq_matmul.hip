@@ -333,17 +333,6 @@ __device__ __forceinline__ v8b transposed(const __bf16* tile, uint32_t c0, uint3
   return r;
 }
 
-// Elements x .. x+7 of a row of `size`: what lies beyond its end is anything that the row holds (it meets zeros, or results that are
-// not stored).  EIGHTS: sizes and x are multiples of eight, so that a vector is there or is not.
-template <bool EIGHTS, class T>
-__device__ __forceinline__ Vec<8, T> load_eight(const T* row, uint32_t x, uint32_t size) {
-  if constexpr (EIGHTS) return load_whole<8>(row + min(x, size - 8));
-  Vec<8, T> r;
-#pragma unroll
-  for (uint32_t e = 0; e < 8; ++e) r.e[e] = as_global(row)[min(x + e, size - 1)];
-  return r;
-}
-
 struct GradShape {
   uint32_t ni, nj, nc;      // sizes of the sum
   uint32_t tiles_i, tiles_j;
@@ -351,6 +340,18 @@ struct GradShape {
   float* partial;           // [splits][ni][nj] where there are several
 };
 
+// Elements x .. x+7 of a row of `size`; what lies beyond its end is anything that the row holds (it meets zeros, or results that are
+// not stored).
+template <class T>
+__device__ __forceinline__ Vec<8, T> load_each(const T* row, uint32_t x, uint32_t size) {
+  Vec<8, T> r;
+#pragma unroll
+  for (uint32_t e = 0; e < 8; ++e) r.e[e] = as_global(row)[min(x + e, size - 1)];
+  return r;
+}
+
+// EIGHTS: the sizes along the operands' rows are multiples of eight, so that a vector is there or is not, and a tile's offsets fit 32
+// bits.
 template <bool WEIGHT, bool EIGHTS, uint32_t TY, uint32_t TO, int TI, int TJ, int WI, int WJ, int STEP>
 __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, const GradShape g) {
   constexpr uint32_t kThreads = WI * WJ * 64, FI = TI / WI / 32, FJ = TJ / WJ / 32, T = kTerms<TO>;
@@ -361,7 +362,7 @@ __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, 
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const TileAt at = tile_at(blockIdx.x, g.tiles_i, g.tiles_j);
   const uint32_t i0 = at.row * TI, j0 = at.col * TJ;
-  const uint32_t first = blockIdx.y * g.each, end = min(g.nc, first + g.each);
+  const uint32_t first = blockIdx.y * g.each, end = min(g.nc, first + g.each), last = first + (end - 1 - first) / STEP * STEP;
   const D* const dy = static_cast<const D*>(a.a.p);
   const int8_t* const q = static_cast<const int8_t*>(a.b.p);
   const float* const scales = a.b.s;
@@ -369,42 +370,65 @@ __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, 
   constexpr uint32_t kApartB = kThreads / (TJ / 8), kApartA = WEIGHT ? kThreads / (TI / 8) : kThreads / (STEP / 8);
   const uint32_t br = threadIdx.x / (TJ / 8), bc = threadIdx.x % (TJ / 8) * 8;
   const uint32_t ar = threadIdx.x / (WEIGHT ? TI / 8 : STEP / 8), ac = threadIdx.x % (WEIGHT ? TI / 8 : STEP / 8) * 8;
+  // EIGHTS: offsets of the vectors and scales from the start of a step, [1]: of the last one, where rows (or, along c, vectors) that
+  // are not there repeat the last that is
+  uint32_t oa[2][VA], ob[2][VB], os[2][WEIGHT ? VA : 1];
+  if (EIGHTS) {
+#pragma unroll
+    for (uint32_t l = 0; l < 2; ++l) {
+      const uint32_t rows = l ? end - 1 - last : STEP - 1;
+#pragma unroll
+      for (uint32_t h = 0; h < VB; ++h) ob[l][h] = min(br + kApartB * h, rows) * static_cast<uint32_t>(a.b.stride) + min(j0 + bc, g.nj - 8);
+#pragma unroll
+      for (uint32_t h = 0; h < VA; ++h) {
+        const uint32_t r = ar + kApartA * h;
+        if (WEIGHT) {
+          os[l][h] = min(r, rows);
+          oa[l][h] = os[l][h] * static_cast<uint32_t>(a.a.stride) + min(i0 + ac, g.ni - 8);
+        } else {
+          oa[l][h] = min(r, g.ni - 1 - i0) * static_cast<uint32_t>(a.a.stride) + min(ac, rows - 7);
+        }
+      }
+      if (!WEIGHT) os[l][0] = min(ac, rows - 7);
+    }
+  }
 
   Vec<8, D> va[VA];
   Vec<8, int8_t> vb[VB];
   Vec<8, float> vs;
-  const auto load = [&](uint32_t c) {
-#pragma unroll
-    for (uint32_t h = 0; h < VB; ++h) vb[h] = load_eight<EIGHTS>(q + min(c + br + kApartB * h, end - 1) * a.b.stride, j0 + bc, g.nj);
-#pragma unroll
-    for (uint32_t h = 0; h < VA; ++h) {
-      if (WEIGHT) {
+  // The loads of piece p, a vector of dy or of the codes, of step c (beyond the last step: of that).
+  const auto load = [&](uint32_t c, uint32_t p) {
+    c = min(c, last);
+    const bool l = c == last;
+    if (p < VA) {
+      const uint32_t h = p;
+      if (EIGHTS) {
+        va[h] = load_whole<8>(dy + (WEIGHT ? c : i0) * a.a.stride + (WEIGHT ? 0 : c) + (l ? oa[1][h] : oa[0][h]));
+        if (WEIGHT) vs.e[h] = as_global(scales + c)[l ? os[1][h] : os[0][h]];
+        else if (h == VA - 1) vs = load_whole<8>(scales + c + (l ? os[1][0] : os[0][0]));
+      } else if (WEIGHT) {
         const uint32_t row = min(c + ar + kApartA * h, end - 1);
-        va[h] = load_eight<EIGHTS>(dy + row * a.a.stride, i0 + ac, g.ni);
+        va[h] = load_each(dy + row * a.a.stride, i0 + ac, g.ni);
         vs.e[h] = as_global(scales)[row];
       } else {
-        va[h] = load_eight<EIGHTS>(dy + min(i0 + ar + kApartA * h, g.ni - 1) * a.a.stride, c + ac, end);
+        va[h] = load_each(dy + min(i0 + ar + kApartA * h, g.ni - 1) * a.a.stride, c + ac, end);
+        if (h == VA - 1) vs = load_each(scales, c + ac, end);
       }
+    } else {
+      const uint32_t h = p - VA;
+      if (EIGHTS) vb[h] = load_whole<8>(q + c * a.b.stride + (l ? ob[1][h] : ob[0][h]));
+      else vb[h] = load_each(q + min(c + br + kApartB * h, end - 1) * a.b.stride, j0 + bc, g.nj);
     }
-    if (!WEIGHT) vs = load_eight<EIGHTS>(scales, c + ac, end);
-    if (c + STEP <= end) return;
-    // the last step of a sum whose length is no multiple: zeros in place of what comes after it
-#pragma unroll
-    for (uint32_t h = 0; h < VA; ++h)
-#pragma unroll
-      for (uint32_t e = 0; e < 8; ++e)
-        if ((WEIGHT ? c + ar + kApartA * h : c + ac + e) >= end) {
-          va[h].e[e] = static_cast<D>(0.0f);
-          vs.e[WEIGHT ? h : e] = 0.0f;
-        }
   };
-  const auto put = [&](__bf16 (*ta)[kSizeA], __bf16* tb) {
-#pragma unroll
-    for (uint32_t h = 0; h < VA; ++h) {
+  // Piece p, which was loaded for step c, into LDS.  What lies beyond the sum's end is zero, whatever was read in its place.
+  const auto put = [&](uint32_t c, uint32_t p, __bf16 (*ta)[kSizeA], __bf16* tb) {
+    if (p < VA) {
+      const uint32_t h = p;
       v8b t[T];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float x = static_cast<float>(va[h].e[e]) * (WEIGHT ? vs.e[h] : vs.e[e]);
+      for (uint32_t e = 0; e < 8; ++e) {
+        const bool there = (WEIGHT ? c + ar + kApartA * h : c + ac + (EIGHTS ? 0 : e)) < end;
+        float x = (there ? static_cast<float>(va[h].e[e]) : 0.0f) * (WEIGHT ? vs.e[h] : (there ? vs.e[e] : 0.0f));
 #pragma unroll
         for (uint32_t k = 0; k < T; ++k) {
           t[k][e] = static_cast<__bf16>(x);
@@ -414,9 +438,8 @@ __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, 
       const uint32_t row = ar + kApartA * h, to = WEIGHT ? row * kRowX<TI> + ac : place_c<STEP>(row, ac / 8);
 #pragma unroll
       for (uint32_t k = 0; k < T; ++k) __builtin_memcpy(&ta[k][to], &t[k], 16);
-    }
-#pragma unroll
-    for (uint32_t h = 0; h < VB; ++h) {
+    } else {
+      const uint32_t h = p - VA;
       v8b t;
 #pragma unroll
       for (int e = 0; e < 8; ++e) t[e] = static_cast<__bf16>(static_cast<float>(vb[h].e[e]));
@@ -425,38 +448,58 @@ __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, 
   };
   v16f acc[FI][FJ] = {};
   const uint32_t wi = wave / WJ * (TI / WI), wj = wave % WJ * (TJ / WJ);
-  const auto work = [&](const __bf16 (*ta)[kSizeA], const __bf16* tb) {
+  // One step out of ta, tb, and on the way, between the matrix instructions, so that the vector unit and LDS work beside the matrix
+  // cores: what was loaded for the next step into na, nb, and the loads of the step after that.
+  const auto work = [&](uint32_t c, const __bf16 (*ta)[kSizeA], const __bf16* tb, __bf16 (*na)[kSizeA], __bf16* nb) {
+    constexpr uint32_t kUnits = STEP / 16 * T * FI, kPieces = VA + VB;
+    const auto read_a = [&](uint32_t u) {
+      const uint32_t at_c = u / (T * FI) * 16, k = u / FI % T, i = u % FI;
+      v8b f;
+      if (WEIGHT) f = transposed<TI>(ta[k], at_c, wi + i * 32, lane);
+      else __builtin_memcpy(&f, &ta[k][place_c<STEP>(wi + i * 32 + (lane & 31), at_c / 8 + (lane >> 5))], 16);
+      return f;
+    };
+    v8b fa = read_a(0), fb[FJ];
 #pragma unroll
-    for (uint32_t c = 0; c < STEP; c += 16) {
-      v8b fb[FJ];
+    for (uint32_t j = 0; j < FJ; ++j) fb[j] = transposed<TJ>(tb, 0, wj + j * 32, lane);
 #pragma unroll
-      for (uint32_t j = 0; j < FJ; ++j) fb[j] = transposed<TJ>(tb, c, wj + j * 32, lane);
+    for (uint32_t u = 0; u < kUnits; ++u) {
+      v8b next_a = fa, next_b[FJ];
 #pragma unroll
-      for (uint32_t k = 0; k < T; ++k)
+      for (uint32_t j = 0; j < FJ; ++j) next_b[j] = fb[j];
+      if (u + 1 < kUnits) next_a = read_a(u + 1);
+      if ((u + 1) % (T * FI) == 0 && u + 1 < kUnits) {
 #pragma unroll
-        for (uint32_t i = 0; i < FI; ++i) {
-          v8b fa;
-          if (WEIGHT) fa = transposed<TI>(ta[k], c, wi + i * 32, lane);
-          else __builtin_memcpy(&fa, &ta[k][place_c<STEP>(wi + i * 32 + (lane & 31), c / 8 + (lane >> 5))], 16);
+        for (uint32_t j = 0; j < FJ; ++j) next_b[j] = transposed<TJ>(tb, (u + 1) / (T * FI) * 16, wj + j * 32, lane);
+      }
 #pragma unroll
-          for (uint32_t j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa, acc[i][j], 0, 0, 0);
+      for (uint32_t j = 0; j < FJ; ++j)
+        acc[u % FI][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa, acc[u % FI][j], 0, 0, 0);
+#pragma unroll
+      for (uint32_t p = 0; p < kPieces; ++p)
+        if (p * kUnits / kPieces == u) {
+          put(c + STEP, p, na, nb);
+          load(c + 2 * STEP, p);
         }
+      fa = next_a;
+#pragma unroll
+      for (uint32_t j = 0; j < FJ; ++j) fb[j] = next_b[j];
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
-  // (loads and puts beyond the last step repeat its rows and are not used)
-  load(first);
-  put(sa0, sb0);
-  load(first + STEP);
+  // (what is put beyond the last step is not used)
+#pragma unroll
+  for (uint32_t p = 0; p < VA + VB; ++p) load(first, p);
+#pragma unroll
+  for (uint32_t p = 0; p < VA + VB; ++p) put(first, p, sa0, sb0);
+#pragma unroll
+  for (uint32_t p = 0; p < VA + VB; ++p) load(first + STEP, p);
   for (uint32_t c = first;; c += 2 * STEP) {
     __syncthreads();
-    put(sa1, sb1);
-    load(c + 2 * STEP);
-    work(sa0, sb0);
+    work(c, sa0, sb0, sa1, sb1);
     if (c + STEP >= end) break;
     __syncthreads();
-    put(sa0, sb0);
-    load(c + 3 * STEP);
-    work(sa1, sb1);
+    work(c + STEP, sa1, sb1, sa0, sb0);
     if (c + 2 * STEP >= end) break;
   }
   // the codes' columns along the fragments' rows: a lane has four neighbouring columns of one row at a time
@@ -537,7 +580,7 @@ template <bool WEIGHT, uint32_t TY, uint32_t TO>
 void run_grad(const MatmulArgs& a, GradShape g, uint32_t n_cu, hipStream_t st) {
   constexpr int kStepC = 32;
   const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(g.ni, t)) * tiles_of(g.nj, t); };
-  const bool eights = g.nj % 8 == 0 && (WEIGHT ? g.ni : g.nc) % 8 == 0;
+  const bool eights = g.nj % 8 == 0 && (WEIGHT ? g.ni : g.nc) % 8 == 0 && a.a.stride < (1u << 22) && a.b.stride < (1u << 22);
   const uint32_t t = eights && g.splits == 1 && count(256) >= n_cu ? 256 : 128;
   g.tiles_i = tiles_of(g.ni, t);
   g.tiles_j = tiles_of(g.nj, t);
