@@ -125,33 +125,46 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul_tile_kernel(const MatmulA
   };
   v16i acc[FM][FN] = {};
   const uint32_t wm = wave / WN * (TM / WM), wn = wave % WN * (TN / WN);
-  const auto work = [&](const int8_t* la, const int8_t* lb) {
+  // A step out of la, lb, in units of one fragment of the tokens.  A unit's fragments are read two units ahead, so that those of the
+  // last two are there when the workgroup meets: from then on the next step's buffers are full and this step's are free.
+  constexpr uint32_t kUnits = kStepK / 32 * FM;
+  v4i fa[2], fb[2][FN];
+  const uint32_t r = lane & 31;
+  const auto at_piece = [&](uint32_t row, uint32_t s) { return row * kStepK + (((2 * s + (lane >> 5)) ^ (r >> 1)) & 7) * 16; };
+  const auto read = [&](uint32_t u, const int8_t* la, const int8_t* lb) {
+    const uint32_t s = u / FM, i = u % FM;
+    fa[u & 1] = *reinterpret_cast<const v4i*>(la + at_piece(wm + i * 32 + r, s));
+    if (i) return;
 #pragma unroll
-    for (uint32_t s = 0; s < kStepK / 32; ++s) {
-      v4i fa[FM], fb[FN];
-      const uint32_t r = lane & 31, place = ((2 * s + (lane >> 5)) ^ (r >> 1)) & 7;
+    for (uint32_t j = 0; j < FN; ++j) fb[s & 1][j] = *reinterpret_cast<const v4i*>(lb + at_piece(wn + j * 32 + r, s));
+  };
+  const auto work = [&](uint32_t k, int8_t* la, int8_t* lb, const int8_t* na, const int8_t* nb) {
 #pragma unroll
-      for (uint32_t i = 0; i < FM; ++i) fa[i] = *reinterpret_cast<const v4i*>(la + (wm + i * 32 + r) * kStepK + place * 16);
+    for (uint32_t u = 0; u < kUnits; ++u) {
+      if (u == kUnits - 2) {
+        __syncthreads();
+        load(k + 2 * kStepK, la, lb);
+      }
 #pragma unroll
-      for (uint32_t j = 0; j < FN; ++j) fb[j] = *reinterpret_cast<const v4i*>(lb + (wn + j * 32 + r) * kStepK + place * 16);
-#pragma unroll
-      for (uint32_t i = 0; i < FM; ++i)
-#pragma unroll
-        for (uint32_t j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
+      for (uint32_t j = 0; j < FN; ++j)
+        acc[u % FM][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[u / FM & 1][j], fa[u & 1], acc[u % FM][j], 0, 0, 0);
+      if (u + 2 < kUnits) read(u + 2, la, lb);
+      else read(u + 2 - kUnits, na, nb);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
   load(0, a0, b0);
+  __syncthreads();
+  load(kStepK, a1, b1);
+  read(0, a0, b0);
+  read(1, a0, b0);
+  // (the fragments that the last step reads ahead are not used)
   for (uint32_t k = 0;; k += 2 * kStepK) {
-    __syncthreads();
-    load(k + kStepK, a1, b1);
-    work(a0, b0);
+    work(k, a0, b0, a1, b1);
     if (k + kStepK >= a.k) break;
-    __syncthreads();
-    load(k + 2 * kStepK, a0, b0);
-    work(a1, b1);
+    work(k + kStepK, a1, b1, a0, b0);
     if (k + 2 * kStepK >= a.k) break;
   }
-  // w's rows along the fragments' rows: a lane has four neighbouring outputs of one token at a time
   // the scales by way of LDS, into which nothing is loaded any more
   __syncthreads();
   float* const sm = reinterpret_cast<float*>(a0);
@@ -448,57 +461,51 @@ __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, 
   };
   v16f acc[FI][FJ] = {};
   const uint32_t wi = wave / WJ * (TI / WI), wj = wave % WJ * (TJ / WJ);
-  // One step out of ta, tb, and on the way, between the matrix instructions, so that the vector unit and LDS work beside the matrix
-  // cores: what was loaded for the next step into na, nb, and the loads of the step after that.
-  const auto work = [&](uint32_t c, const __bf16 (*ta)[kSizeA], const __bf16* tb, __bf16 (*na)[kSizeA], __bf16* nb) {
-    constexpr uint32_t kUnits = STEP / 16 * T * FI, kPieces = VA + VB;
-    const auto read_a = [&](uint32_t u) {
-      const uint32_t at_c = u / (T * FI) * 16, k = u / FI % T, i = u % FI;
-      v8b f;
-      if (WEIGHT) f = transposed<TI>(ta[k], at_c, wi + i * 32, lane);
-      else __builtin_memcpy(&f, &ta[k][place_c<STEP>(wi + i * 32 + (lane & 31), at_c / 8 + (lane >> 5))], 16);
-      return f;
-    };
-    v8b fa = read_a(0), fb[FJ];
+  // A step out of ta, tb, in units of one fragment of dy.  A unit's fragments are read two units ahead; on the way, between the matrix
+  // instructions, so that the vector unit and LDS work beside the matrix cores, what was loaded for the next step goes into na, nb, and
+  // the loads of the step after that begin.  When the workgroup meets, before the last two units, all of this step has been read and all
+  // of the next is there.
+  constexpr uint32_t kUnits = STEP / 16 * T * FI, kPieces = VA + VB;
+  v8b fa[2], fb[2][FJ];
+  const auto read = [&](uint32_t u, const __bf16 (*ta)[kSizeA], const __bf16* tb) {
+    const uint32_t s = u / (T * FI), k = u / FI % T, i = u % FI;
+    if (WEIGHT) fa[u & 1] = transposed<TI>(ta[k], s * 16, wi + i * 32, lane);
+    else __builtin_memcpy(&fa[u & 1], &ta[k][place_c<STEP>(wi + i * 32 + (lane & 31), s * 2 + (lane >> 5))], 16);
+    if (u % (T * FI)) return;
 #pragma unroll
-    for (uint32_t j = 0; j < FJ; ++j) fb[j] = transposed<TJ>(tb, 0, wj + j * 32, lane);
+    for (uint32_t j = 0; j < FJ; ++j) fb[s & 1][j] = transposed<TJ>(tb, s * 16, wj + j * 32, lane);
+  };
+  const auto work = [&](uint32_t c, const __bf16 (*ta)[kSizeA], const __bf16* tb, __bf16 (*na)[kSizeA], __bf16* nb) {
 #pragma unroll
     for (uint32_t u = 0; u < kUnits; ++u) {
-      v8b next_a = fa, next_b[FJ];
-#pragma unroll
-      for (uint32_t j = 0; j < FJ; ++j) next_b[j] = fb[j];
-      if (u + 1 < kUnits) next_a = read_a(u + 1);
-      if ((u + 1) % (T * FI) == 0 && u + 1 < kUnits) {
-#pragma unroll
-        for (uint32_t j = 0; j < FJ; ++j) next_b[j] = transposed<TJ>(tb, (u + 1) / (T * FI) * 16, wj + j * 32, lane);
-      }
+      if (u == kUnits - 2) __syncthreads();
 #pragma unroll
       for (uint32_t j = 0; j < FJ; ++j)
-        acc[u % FI][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa, acc[u % FI][j], 0, 0, 0);
+        acc[u % FI][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[u / (T * FI) & 1][j], fa[u & 1], acc[u % FI][j], 0, 0, 0);
+      if (u + 2 < kUnits) read(u + 2, ta, tb);
+      else read(u + 2 - kUnits, na, nb);
 #pragma unroll
       for (uint32_t p = 0; p < kPieces; ++p)
-        if (p * kUnits / kPieces == u) {
+        if (p * (kUnits - 2) / kPieces == u) {
           put(c + STEP, p, na, nb);
           load(c + 2 * STEP, p);
         }
-      fa = next_a;
-#pragma unroll
-      for (uint32_t j = 0; j < FJ; ++j) fb[j] = next_b[j];
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  // (what is put beyond the last step is not used)
 #pragma unroll
-  for (uint32_t p = 0; p < VA + VB; ++p) load(first, p);
+  for (uint32_t p = 0; p < kPieces; ++p) load(first, p);
 #pragma unroll
-  for (uint32_t p = 0; p < VA + VB; ++p) put(first, p, sa0, sb0);
+  for (uint32_t p = 0; p < kPieces; ++p) put(first, p, sa0, sb0);
 #pragma unroll
-  for (uint32_t p = 0; p < VA + VB; ++p) load(first + STEP, p);
+  for (uint32_t p = 0; p < kPieces; ++p) load(first + STEP, p);
+  __syncthreads();
+  read(0, sa0, sb0);
+  read(1, sa0, sb0);
+  // (what is put and read beyond the last step is not used)
   for (uint32_t c = first;; c += 2 * STEP) {
-    __syncthreads();
     work(c, sa0, sb0, sa1, sb1);
     if (c + STEP >= end) break;
-    __syncthreads();
     work(c + STEP, sa1, sb1, sa0, sb0);
     if (c + 2 * STEP >= end) break;
   }
