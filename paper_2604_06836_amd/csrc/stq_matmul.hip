@@ -39,21 +39,72 @@ __device__ __forceinline__ Vec<N, T> load_vec(const T* row, uint32_t c, uint32_t
   return r;
 }
 
-// Four neighbouring elements of an output's row, as many as are there.
+// What a lane has of a wave's result at a time is four neighbouring columns of one row; 16 bytes of a row, as an output has them.
+struct Piece { uint32_t w[4]; };
+template <uint32_t TO>
+__device__ __forceinline__ void pack4(const float (&v)[4], void* to) {  // in LDS
+  if constexpr (TO == kF32) {
+    __builtin_memcpy(to, v, 16);
+  } else {
+    const __bf16 h[4] = {static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1]), static_cast<__bf16>(v[2]), static_cast<__bf16>(v[3])};
+    uint64_t w;
+    __builtin_memcpy(&w, h, 8);
+    __builtin_memcpy(to, &w, 8);
+  }
+}
+template <uint32_t TO>
+__device__ __forceinline__ void store_piece(const Mat& out, uint32_t row, uint32_t col, uint32_t end, const Piece& v) {
+  using T = typename Elem<TO>::type;
+  constexpr uint32_t kPer = 16 / sizeof(T);
+  STQ_GLOBAL T* p = as_global(static_cast<T*>(out.p)) + row * out.stride + col;
+  if (col + kPer <= end) {
+    __builtin_memcpy(p, &v, 16);
+  } else {
+    T e[kPer];
+    __builtin_memcpy(e, &v, 16);
+#pragma unroll
+    for (uint32_t i = 0; i < kPer; ++i)
+      if (col + i < end) p[i] = e[i];
+  }
+}
+// A wave's result, FI x FJ fragments of 32 x 32 from row0, col0 on, into an output of rows x cols, by way of 32 rows of LDS of its own
+// (`box`, 4096 FJ bytes for fp32), so that whole pieces of rows are stored, neighbouring ones together.  value(i, j, p, e): column
+// 8 p + 4 (lane / 32) + e of row lane % 32 of fragment i, j.  Pieces lie at the places that their number and the row's give by
+// exclusive or.
+template <uint32_t TO, uint32_t FI, uint32_t FJ, class F>
+__device__ __forceinline__ void store_tile(const Mat& out, uint32_t row0, uint32_t col0, uint32_t rows, uint32_t cols, char* box, uint32_t lane, F value) {
+  constexpr uint32_t kSize = TO == kF32 ? 4 : 2, kRow = FJ * 32 * kSize, kPieces = kRow / 16, kShift = kRow == 256 ? 0 : (kRow == 128 ? 1 : 2);
+  const auto place = [&](uint32_t row, uint32_t piece) { return row * kRow + ((piece ^ (row >> kShift)) & (kPieces - 1)) * 16; };
+#pragma unroll
+  for (uint32_t i = 0; i < FI; ++i) {
+#pragma unroll
+    for (uint32_t j = 0; j < FJ; ++j)
+#pragma unroll
+      for (uint32_t p = 0; p < 4; ++p) {
+        float v[4];
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) v[e] = value(i, j, p, e);
+        const uint32_t byte = (j * 32 + p * 8 + (lane >> 5) * 4) * kSize;
+        pack4<TO>(v, box + place(lane & 31, byte / 16) + byte % 16);
+      }
+#pragma unroll
+    for (uint32_t h = 0; h < 32 * kPieces / 64; ++h) {
+      const uint32_t row = h * (64 / kPieces) + lane / kPieces, piece = lane % kPieces;
+      Piece v;
+      __builtin_memcpy(&v, box + place(row, piece), 16);
+      const uint32_t r = row0 + i * 32 + row, c = col0 + piece * (16 / kSize);
+      if (r < rows && c < cols) store_piece<TO>(out, r, c, cols, v);
+    }
+  }
+}
+// Four elements where they are: for kernels whose results are few.
 template <uint32_t TO>
 __device__ __forceinline__ void store4(const Mat& out, uint32_t row, uint32_t col, uint32_t end, const float (&v)[4]) {
   using T = typename Elem<TO>::type;
   STQ_GLOBAL T* p = as_global(static_cast<T*>(out.p)) + row * out.stride + col;
-  Vec<4, T> r;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) r.e[e] = static_cast<T>(v[e]);
-  if (col + 4 <= end) {
-    __builtin_memcpy(p, &r, sizeof(r));
-  } else {
-#pragma unroll
-    for (uint32_t e = 0; e < 4; ++e)
-      if (col + e < end) p[e] = r.e[e];
-  }
+  for (uint32_t e = 0; e < 4; ++e)
+    if (col + e < end) p[e] = static_cast<T>(v[e]);
 }
 
 template <int N, class T>
@@ -111,7 +162,7 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul_tile_kernel(const MatmulA
 #pragma unroll
       for (uint32_t i = 0; i < TN / kAtOnce; ++i)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (STQ_LDS void*)(lb + (i * kAtOnce + wave * 8) * kStepK), 16, ob[i], k, 0, 0);
-    } else if (k < a.k) {
+    } else {
       const auto rest = [&](const int8_t* p, uint64_t stride, uint32_t last, int8_t* to, uint32_t rows) {
 #pragma unroll 1
         for (uint32_t r = load_row; r < rows; r += kAtOnce) {
@@ -125,15 +176,15 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul_tile_kernel(const MatmulA
   };
   v16i acc[FM][FN] = {};
   const uint32_t wm = wave / WN * (TM / WM), wn = wave % WN * (TN / WN);
-  // A step out of la, lb, in units of one fragment of the tokens.  A unit's fragments are read two units ahead, so that those of the
-  // last two are there when the workgroup meets: from then on the next step's buffers are full and this step's are free.
-  constexpr uint32_t kUnits = kStepK / 32 * FM;
-  v4i fa[2], fb[2][FN];
+  // A step out of la, lb, in units of one fragment of the tokens.  A unit's fragments are read kAhead units ahead, so that those of the
+  // last kAhead are there when the workgroup meets: from then on the next step's buffers are full and this step's are free.
+  constexpr uint32_t kUnits = kStepK / 32 * FM, kAhead = FM < 4 ? 2 : 4;
+  v4i fa[kAhead], fb[2][FN];
   const uint32_t r = lane & 31;
   const auto at_piece = [&](uint32_t row, uint32_t s) { return row * kStepK + (((2 * s + (lane >> 5)) ^ (r >> 1)) & 7) * 16; };
   const auto read = [&](uint32_t u, const int8_t* la, const int8_t* lb) {
     const uint32_t s = u / FM, i = u % FM;
-    fa[u & 1] = *reinterpret_cast<const v4i*>(la + at_piece(wm + i * 32 + r, s));
+    fa[u % kAhead] = *reinterpret_cast<const v4i*>(la + at_piece(wm + i * 32 + r, s));
     if (i) return;
 #pragma unroll
     for (uint32_t j = 0; j < FN; ++j) fb[s & 1][j] = *reinterpret_cast<const v4i*>(lb + at_piece(wn + j * 32 + r, s));
@@ -141,52 +192,42 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul_tile_kernel(const MatmulA
   const auto work = [&](uint32_t k, int8_t* la, int8_t* lb, const int8_t* na, const int8_t* nb) {
 #pragma unroll
     for (uint32_t u = 0; u < kUnits; ++u) {
-      if (u == kUnits - 2) {
+      if (u == kUnits - kAhead) {
         __syncthreads();
         load(k + 2 * kStepK, la, lb);
       }
 #pragma unroll
       for (uint32_t j = 0; j < FN; ++j)
-        acc[u % FM][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[u / FM & 1][j], fa[u & 1], acc[u % FM][j], 0, 0, 0);
-      if (u + 2 < kUnits) read(u + 2, la, lb);
-      else read(u + 2 - kUnits, na, nb);
+        acc[u % FM][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[u / FM & 1][j], fa[u % kAhead], acc[u % FM][j], 0, 0, 0);
+      if (u + kAhead < kUnits) read(u + kAhead, la, lb);
+      else read(u + kAhead - kUnits, na, nb);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
   load(0, a0, b0);
   __syncthreads();
   load(kStepK, a1, b1);
-  read(0, a0, b0);
-  read(1, a0, b0);
-  // (the fragments that the last step reads ahead are not used)
-  for (uint32_t k = 0;; k += 2 * kStepK) {
+#pragma unroll
+  for (uint32_t u = 0; u < kAhead; ++u) read(u, a0, b0);
+  // Two steps at a time, of which the second may lie beyond the rows' end and be one of zeros: with one way out of the loop the sums
+  // stay in their registers.  (What the last step reads ahead is not used.)
+  for (uint32_t k = 0; k < a.k; k += 2 * kStepK) {
     work(k, a0, b0, a1, b1);
-    if (k + kStepK >= a.k) break;
     work(k + kStepK, a1, b1, a0, b0);
-    if (k + 2 * kStepK >= a.k) break;
   }
-  // the scales by way of LDS, into which nothing is loaded any more
+  // the scales and the result by way of LDS, into which nothing is loaded any more
   __syncthreads();
-  float* const sm = reinterpret_cast<float*>(a0);
-  float* const sn = reinterpret_cast<float*>(b0);
+  float* const sm = reinterpret_cast<float*>(a1);
+  float* const sn = reinterpret_cast<float*>(b1);
   for (uint32_t i = threadIdx.x; i < TM; i += WM * WN * 64) sm[i] = as_global(a.a.s)[min(m0 + i, a.m - 1)];
   for (uint32_t i = threadIdx.x; i < TN; i += WM * WN * 64) sn[i] = as_global(a.b.s)[min(n0 + i, a.n - 1)];
   __syncthreads();
-#pragma unroll
-  for (uint32_t i = 0; i < FM; ++i) {
-    const uint32_t r = wm + i * 32 + (lane & 31), m = m0 + r;
-    const float s = sm[r];
-#pragma unroll
-    for (uint32_t j = 0; j < FN; ++j)
-#pragma unroll
-      for (uint32_t q = 0; q < 4; ++q) {
-        const uint32_t c = wn + j * 32 + q * 8 + (lane >> 5) * 4;
-        float v[4];
-#pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) v[e] = static_cast<float>(acc[i][j][q * 4 + e]) * s * sn[c + e];
-        if (m < a.m) store4<TO>(a.out, m, n0 + c, a.n, v);
-      }
-  }
+  constexpr uint32_t kBox = 32 * FN * 32 * 4, kHalf = WM * WN / 2;
+  static_assert(kHalf * kBox <= TM * kStepK && kHalf * kBox <= TN * kStepK, "a box for each wave");
+  char* const box = wave < kHalf ? reinterpret_cast<char*>(a0) + wave * kBox : reinterpret_cast<char*>(b0) + (wave - kHalf) * kBox;
+  store_tile<TO, FM, FN>(a.out, m0 + wm, n0 + wn, a.m, a.n, box, lane, [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) {
+    return static_cast<float>(acc[i][j][p * 4 + e]) * sm[wm + i * 32 + (lane & 31)] * sn[wn + j * 32 + p * 8 + (lane >> 5) * 4 + e];
+  });
 #endif
 }
 
@@ -370,7 +411,7 @@ __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, 
   constexpr uint32_t kThreads = WI * WJ * 64, FI = TI / WI / 32, FJ = TJ / WJ / 32, T = kTerms<TO>;
   constexpr uint32_t kSizeA = WEIGHT ? STEP * kRowX<TI> : TI * STEP, kSizeB = STEP * kRowX<TJ>;
   constexpr uint32_t VA = TI * STEP / 8 / kThreads, VB = TJ * STEP / 8 / kThreads;  // vectors of eight of a thread
-  __shared__ __align__(16) __bf16 sa0[T][kSizeA], sb0[kSizeB], sa1[T][kSizeA], sb1[kSizeB];
+  __shared__ __align__(16) struct { __bf16 a0[T][kSizeA], b0[kSizeB], a1[T][kSizeA], b1[kSizeB]; } tiles;
   using D = typename Elem<TY>::type;
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const TileAt at = tile_at(blockIdx.x, g.tiles_i, g.tiles_j);
@@ -496,37 +537,28 @@ __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, 
 #pragma unroll
   for (uint32_t p = 0; p < kPieces; ++p) load(first, p);
 #pragma unroll
-  for (uint32_t p = 0; p < kPieces; ++p) put(first, p, sa0, sb0);
+  for (uint32_t p = 0; p < kPieces; ++p) put(first, p, tiles.a0, tiles.b0);
 #pragma unroll
   for (uint32_t p = 0; p < kPieces; ++p) load(first + STEP, p);
   __syncthreads();
-  read(0, sa0, sb0);
-  read(1, sa0, sb0);
-  // (what is put and read beyond the last step is not used)
-  for (uint32_t c = first;; c += 2 * STEP) {
-    work(c, sa0, sb0, sa1, sb1);
-    if (c + STEP >= end) break;
-    work(c + STEP, sa1, sb1, sa0, sb0);
-    if (c + 2 * STEP >= end) break;
+  read(0, tiles.a0, tiles.b0);
+  read(1, tiles.a0, tiles.b0);
+  // Two steps at a time, of which the second may lie beyond the sum's end and be one of zeros: with one way out of the loop the sums
+  // stay in their registers.  (What the last step reads ahead is not used.)
+  for (uint32_t c = first; c < end; c += 2 * STEP) {
+    work(c, tiles.a0, tiles.b0, tiles.a1, tiles.b1);
+    work(c + STEP, tiles.a1, tiles.b1, tiles.a0, tiles.b0);
   }
-  // the codes' columns along the fragments' rows: a lane has four neighbouring columns of one row at a time
-  const Mat part{g.partial + static_cast<uint64_t>(blockIdx.y) * g.ni * g.nj, nullptr, g.nj, 0, 0};
-#pragma unroll
-  for (uint32_t i = 0; i < FI; ++i) {
-    const uint32_t row = i0 + wi + i * 32 + (lane & 31);
-    if (row >= g.ni) continue;
-#pragma unroll
-    for (uint32_t j = 0; j < FJ; ++j)
-#pragma unroll
-      for (uint32_t p = 0; p < 4; ++p) {
-        const uint32_t col = j0 + wj + j * 32 + p * 8 + (lane >> 5) * 4;
-        float v[4];
-#pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) v[e] = acc[i][j][p * 4 + e];
-        if (col >= g.nj) continue;
-        if (g.splits > 1) store4<kF32>(part, row, col, g.nj, v);
-        else store4<TO>(a.out, row, col, g.nj, v);
-      }
+  __syncthreads();
+  const auto value = [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return acc[i][j][p * 4 + e]; };
+  constexpr uint32_t kBox = 32 * FJ * 32 * (TI == 256 && TO != kF32 ? 2 : 4);
+  static_assert(sizeof(tiles) >= WI * WJ * kBox, "a box for each wave");
+  char* const box = reinterpret_cast<char*>(&tiles) + wave * kBox;
+  if (TI != 256 && g.splits > 1) {  // (sums taken in parts are of small tiles)
+    const Mat part{g.partial + static_cast<uint64_t>(blockIdx.y) * g.ni * g.nj, nullptr, g.nj, 0, 0};
+    store_tile<kF32, FI, FJ>(part, i0 + wi, j0 + wj, g.ni, g.nj, box, lane, value);
+  } else {
+    store_tile<TO, FI, FJ>(a.out, i0 + wi, j0 + wj, g.ni, g.nj, box, lane, value);
   }
 }
 
