@@ -107,13 +107,6 @@ __device__ __forceinline__ void store4(const Mat& out, uint32_t row, uint32_t co
     if (col + e < end) p[e] = static_cast<T>(v[e]);
 }
 
-template <int N, class T>
-__device__ __forceinline__ Vec<N, T> load_whole(const T* p) {
-  Vec<N, T> r;
-  __builtin_memcpy(&r, as_global(p), sizeof(r));
-  return r;
-}
-
 // ---------------------------------------------------------------------------------------------- order of the tiles
 // Workgroups go to the card's eight dies in turn, each of which has an L2 of its own: a die takes a run of tiles, in an order that
 // goes through patches of up to eight rows of tiles, column by column, so that those at work together share rows and columns.
@@ -154,6 +147,7 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul_tile_kernel(const MatmulA
   for (uint32_t i = 0; i < TM / kAtOnce; ++i) oa[i] = min(load_row + kAtOnce * i, a.m - 1 - m0) * static_cast<uint32_t>(a.a.stride) + piece * 16;
 #pragma unroll
   for (uint32_t i = 0; i < TN / kAtOnce; ++i) ob[i] = min(load_row + kAtOnce * i, a.n - 1 - n0) * static_cast<uint32_t>(a.b.stride) + piece * 16;
+  const uint32_t both_end = (a.k + 2 * kStepK - 1) / (2 * kStepK) * (2 * kStepK);  // of the steps, taken two at a time
   const auto load = [&](uint32_t k, int8_t* la, int8_t* lb) {
     if (k + kStepK <= a.k) {
 #pragma unroll
@@ -162,7 +156,7 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul_tile_kernel(const MatmulA
 #pragma unroll
       for (uint32_t i = 0; i < TN / kAtOnce; ++i)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (STQ_LDS void*)(lb + (i * kAtOnce + wave * 8) * kStepK), 16, ob[i], k, 0, 0);
-    } else {
+    } else if (k < both_end) {
       const auto rest = [&](const int8_t* p, uint64_t stride, uint32_t last, int8_t* to, uint32_t rows) {
 #pragma unroll 1
         for (uint32_t r = load_row; r < rows; r += kAtOnce) {
@@ -394,13 +388,37 @@ struct GradShape {
   float* partial;           // [splits][ni][nj] where there are several
 };
 
+// Eight elements as they were loaded, in whole words: a step's loads are under way while others are turned into bf16, and must not be
+// taken apart before they are needed.
+template <class T>
+struct Packed {
+  static constexpr int kWords = 8 * sizeof(T) / 4;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void keep(bool there) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = there ? w[i] : 0u;
+  }
+  __device__ __forceinline__ float at(uint32_t e) const {
+    if constexpr (sizeof(T) == 4) return u2f(w[e]);
+    else if constexpr (sizeof(T) == 2) return u2f(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);  // bf16
+    else return static_cast<float>(static_cast<int8_t>(w[e / 4] >> (e % 4 * 8)));
+  }
+};
+template <class T>
+__device__ __forceinline__ Packed<T> load_packed(const T* p) {
+  Packed<T> r;
+  __builtin_memcpy(&r, as_global(p), sizeof(r));
+  return r;
+}
 // Elements x .. x+7 of a row of `size`; what lies beyond its end is anything that the row holds (it meets zeros, or results that are
 // not stored).
 template <class T>
-__device__ __forceinline__ Vec<8, T> load_each(const T* row, uint32_t x, uint32_t size) {
-  Vec<8, T> r;
+__device__ __forceinline__ Packed<T> load_each(const T* row, uint32_t x, uint32_t size) {
+  T e[8];
 #pragma unroll
-  for (uint32_t e = 0; e < 8; ++e) r.e[e] = as_global(row)[min(x + e, size - 1)];
+  for (uint32_t i = 0; i < 8; ++i) e[i] = as_global(row)[min(x + i, size - 1)];
+  Packed<T> r;
+  __builtin_memcpy(&r, e, sizeof(r));
   return r;
 }
 
@@ -447,30 +465,28 @@ __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, 
     }
   }
 
-  Vec<8, D> va[VA];
-  Vec<8, int8_t> vb[VB];
-  Vec<8, float> vs;
+  Packed<D> va[VA];
+  Packed<int8_t> vb[VB];
+  float vs[8];  // scales: of each vector of dy's, or (along c) of its elements
   // The loads of piece p, a vector of dy or of the codes, of step c (beyond the last step: of that).
   const auto load = [&](uint32_t c, uint32_t p) {
     c = min(c, last);
     const bool l = c == last;
     if (p < VA) {
       const uint32_t h = p;
-      if (EIGHTS) {
-        va[h] = load_whole<8>(dy + (WEIGHT ? c : i0) * a.a.stride + (WEIGHT ? 0 : c) + (l ? oa[1][h] : oa[0][h]));
-        if (WEIGHT) vs.e[h] = as_global(scales + c)[l ? os[1][h] : os[0][h]];
-        else if (h == VA - 1) vs = load_whole<8>(scales + c + (l ? os[1][0] : os[0][0]));
-      } else if (WEIGHT) {
-        const uint32_t row = min(c + ar + kApartA * h, end - 1);
-        va[h] = load_each(dy + row * a.a.stride, i0 + ac, g.ni);
-        vs.e[h] = as_global(scales)[row];
-      } else {
-        va[h] = load_each(dy + min(i0 + ar + kApartA * h, g.ni - 1) * a.a.stride, c + ac, end);
-        if (h == VA - 1) vs = load_each(scales, c + ac, end);
+      if (EIGHTS) va[h] = load_packed(dy + (WEIGHT ? c : i0) * a.a.stride + (WEIGHT ? 0 : c) + (l ? oa[1][h] : oa[0][h]));
+      else if (WEIGHT) va[h] = load_each(dy + min(c + ar + kApartA * h, end - 1) * a.a.stride, i0 + ac, g.ni);
+      else va[h] = load_each(dy + min(i0 + ar + kApartA * h, g.ni - 1) * a.a.stride, c + ac, end);
+      if (WEIGHT) {
+        vs[h] = EIGHTS ? as_global(scales + c)[l ? os[1][h] : os[0][h]] : as_global(scales)[min(c + ar + kApartA * h, end - 1)];
+      } else if (h == VA - 1) {
+        const Packed<float> t = EIGHTS ? load_packed(scales + c + (l ? os[1][0] : os[0][0])) : load_each(scales, c + ac, end);
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) vs[e] = t.at(e);
       }
     } else {
       const uint32_t h = p - VA;
-      if (EIGHTS) vb[h] = load_whole<8>(q + c * a.b.stride + (l ? ob[1][h] : ob[0][h]));
+      if (EIGHTS) vb[h] = load_packed(q + c * a.b.stride + (l ? ob[1][h] : ob[0][h]));
       else vb[h] = load_each(q + min(c + br + kApartB * h, end - 1) * a.b.stride, j0 + bc, g.nj);
     }
   };
@@ -478,11 +494,18 @@ __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, 
   const auto put = [&](uint32_t c, uint32_t p, __bf16 (*ta)[kSizeA], __bf16* tb) {
     if (p < VA) {
       const uint32_t h = p;
+      if (WEIGHT) va[h].keep(c + ar + kApartA * h < end);
+      else if (EIGHTS) va[h].keep(c + ac < end);
       v8b t[T];
 #pragma unroll
       for (uint32_t e = 0; e < 8; ++e) {
-        const bool there = (WEIGHT ? c + ar + kApartA * h : c + ac + (EIGHTS ? 0 : e)) < end;
-        float x = (there ? static_cast<float>(va[h].e[e]) : 0.0f) * (WEIGHT ? vs.e[h] : (there ? vs.e[e] : 0.0f));
+        float x = va[h].at(e), s = vs[WEIGHT ? h : e];
+        if (!WEIGHT) {  // (the scales repeat, too, and need not be finite)
+          const bool there = c + ac + (EIGHTS ? 0 : e) < end;
+          x = EIGHTS || there ? x : 0.0f;
+          s = there ? s : 0.0f;
+        }
+        x *= s;
 #pragma unroll
         for (uint32_t k = 0; k < T; ++k) {
           t[k][e] = static_cast<__bf16>(x);
@@ -496,7 +519,7 @@ __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, 
       const uint32_t h = p - VA;
       v8b t;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) t[e] = static_cast<__bf16>(static_cast<float>(vb[h].e[e]));
+      for (uint32_t e = 0; e < 8; ++e) t[e] = static_cast<__bf16>(vb[h].at(e));
       __builtin_memcpy(&tb[(br + kApartB * h) * kRowX<TJ> + bc], &t, 16);
     }
   };
