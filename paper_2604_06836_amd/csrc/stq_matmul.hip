@@ -4,8 +4,7 @@
 
 #include <cstdint>
 
-#include "stq_operators.h"
-#include "stq_wave.h"
+#include "stq_vectors.h"
 
 #pragma clang fp contract(off)
 
@@ -18,10 +17,6 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 #define STQ_LDS __attribute__((address_space(3)))
-
-template <uint32_t TY> struct Elem;
-template <> struct Elem<kF32> { using type = float; };
-template <> struct Elem<kBF16> { using type = __bf16; };
 
 // N elements of a row from element c on; those at or beyond `end` are zeros and are not read (nor any, of a row that is not there).
 template <int N, class T>
@@ -388,28 +383,6 @@ struct GradShape {
   float* partial;           // [splits][ni][nj] where there are several
 };
 
-// Eight elements as they were loaded, in whole words: a step's loads are under way while others are turned into bf16, and must not be
-// taken apart before they are needed.
-template <class T>
-struct Packed {
-  static constexpr int kWords = 8 * sizeof(T) / 4;
-  uint32_t w[kWords];
-  __device__ __forceinline__ void keep(bool there) {
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) w[i] = there ? w[i] : 0u;
-  }
-  __device__ __forceinline__ float at(uint32_t e) const {
-    if constexpr (sizeof(T) == 4) return u2f(w[e]);
-    else if constexpr (sizeof(T) == 2) return u2f(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);  // bf16
-    else return static_cast<float>(static_cast<int8_t>(w[e / 4] >> (e % 4 * 8)));
-  }
-};
-template <class T>
-__device__ __forceinline__ Packed<T> load_packed(const T* p) {
-  Packed<T> r;
-  __builtin_memcpy(&r, as_global(p), sizeof(r));
-  return r;
-}
 // Elements x .. x+7 of a row of `size`; what lies beyond its end is anything that the row holds (it meets zeros, or results that are
 // not stored).
 template <class T>

@@ -85,7 +85,7 @@ int stq_dequantize_rows(stq_ctx* ctx, const stq_matrix* x, const stq_matrix* out
   if (!a.rows) return STQ_OK;
   DeviceGuard g(ctx->device);
   if (!g.ok) return STQ_EHIP;
-  return launched(launch_dequantize_rows(a, out->dtype, stream));
+  return launched(launch_dequantize_rows(a, out->dtype, ctx->n_cu, stream));
 }
 
 int stq_rms_norm(stq_ctx* ctx, const stq_matrix* x, const stq_matrix* residual, const float* weight, float eps,
@@ -189,7 +189,7 @@ int stq_gated_silu_grad(stq_ctx* ctx, const stq_matrix* gate, const stq_matrix* 
   if (!a.rows) return STQ_OK;
   DeviceGuard g(ctx->device);
   if (!g.ok) return STQ_EHIP;
-  return launched(launch_gated_grad(a, gate->dtype, dy->dtype, stream));
+  return launched(launch_gated_grad(a, gate->dtype, dy->dtype, ctx->n_cu, stream));
 }
 
 int stq_matmul(stq_ctx* ctx, const stq_matrix* x, const stq_matrix* w, const stq_matrix* out, void* stream) {

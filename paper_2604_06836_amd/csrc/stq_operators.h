@@ -32,7 +32,6 @@ struct NormGradArgs {
   const float* rstd;
   float* dweight;
   float* partial;   // [groups][cols]
-  uint32_t groups;  // set by the launcher: workgroups of the first kernel
   uint32_t rows, cols;
 };
 struct GatedArgs {
@@ -50,19 +49,18 @@ struct MatmulArgs {
 };
 
 constexpr uint32_t kNormGroups = 512;  // partial sums of dweight at most
-inline uint32_t rows_per_group(uint32_t cols) { return cols <= 1024 ? 4 : 1; }  // of the kernels that hold rows, see stq_rows.hip
 inline uint32_t norm_grad_groups(uint64_t rows, uint32_t cols) {
-  const uint64_t g = (rows + rows_per_group(cols) - 1) / rows_per_group(cols);
+  const uint64_t at_once = cols <= 512 ? 4 : 1, g = (rows + at_once - 1) / at_once;  // (rows of a workgroup, see with_rows)
   return g < kNormGroups ? static_cast<uint32_t>(g) : kNormGroups;
 }
 
 // Launchers; `stream` is a hipStream_t.  Return a hipError_t as int.  rows, m > 0.
 int launch_quantize_rows(const RowsArgs& a, uint32_t type, uint32_t n_cu, void* stream);
-int launch_dequantize_rows(const RowsArgs& a, uint32_t type, void* stream);
+int launch_dequantize_rows(const RowsArgs& a, uint32_t type, uint32_t n_cu, void* stream);
 int launch_rms_norm(const NormArgs& a, uint32_t type, uint32_t n_cu, void* stream);
 int launch_rms_norm_grad(NormGradArgs a, uint32_t sum_type, uint32_t type, void* stream);
 int launch_gated(const GatedArgs& a, uint32_t type, uint32_t n_cu, void* stream);
-int launch_gated_grad(const GatedGradArgs& a, uint32_t kept_type, uint32_t type, void* stream);
+int launch_gated_grad(const GatedGradArgs& a, uint32_t kept_type, uint32_t type, uint32_t n_cu, void* stream);
 int launch_matmul(const MatmulArgs& a, uint32_t out_type, uint32_t n_cu, void* stream);
 int launch_matmul_grad_input(const MatmulArgs& a, uint32_t dy_type, uint32_t out_type, uint32_t n_cu, void* stream);
 int launch_matmul_grad_weight(const MatmulArgs& a, uint32_t dy_type, uint32_t out_type, float* workspace, uint32_t n_cu, void* stream);

@@ -4,16 +4,15 @@
 // All are bound by memory: every matrix is read once and written once.  A thread owns vectors of eight neighbouring columns, so
 // that a vector has one scale (blocks are 64, 128 or 256 columns) and is one load of 8 (codes), 16 (bf16) or 32 bytes.  Kernels
 // that need a maximum or a sum over a row hold the row in registers between the two: a wave for a row of up to 1024 columns,
-// without any barrier, a workgroup of 256 to 1024 threads for longer ones, with one barrier for a row.  Unaligned vectors are the
-// hardware's to split; only the last vector of a row whose columns are no multiple of eight goes element by element.  Rows of over
-// 16384 columns are not held but read again, out of the caches.
+// without any barrier, a workgroup of just the waves that it takes for longer ones, with one barrier for a row.  They go through the
+// rows with the next row's loads under way.  Only the last vector of a row whose columns are no multiple of eight goes element by element.  Longer
+// rows (over 16384 columns; 8192 for the norm's gradients) are not held but read again, out of the caches.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
 #include <type_traits>
 
-#include "stq_operators.h"
-#include "stq_wave.h"
+#include "stq_vectors.h"
 
 #pragma clang fp contract(off)
 
@@ -23,64 +22,30 @@ namespace {
 constexpr float kLeast = 0x1p-100f;  // what a group's largest magnitude counts as at least
 constexpr uint32_t kInf = 0x7F800000u;
 
-// ---------------------------------------------------------------------------------------------- vectors of eight columns
-template <uint32_t TY> struct Elem;
-template <> struct Elem<kF32> { using type = float; };
-template <> struct Elem<kBF16> { using type = __bf16; };
-template <> struct Elem<kQ8> { using type = int8_t; };
-
-// Columns c .. c+7 of a row, as they are stored; beyond the row's end zeros, and nothing is read there.
-template <class T>
-struct Raw { T e[8]; };
-template <class T>
-__device__ __forceinline__ Raw<T> load_raw(const T* row, uint32_t c, uint32_t cols) {
-  Raw<T> r;
-  const STQ_GLOBAL T* p = as_global(row) + c;
-  if (c + 8 <= cols) {
-    __builtin_memcpy(&r, p, sizeof(r));
-  } else {
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) r.e[i] = c + i < cols ? p[i] : static_cast<T>(0);
-  }
-  return r;
-}
-template <class T>
-__device__ __forceinline__ void store_raw(T* row, uint32_t c, uint32_t cols, const Raw<T>& r) {
-  STQ_GLOBAL T* p = as_global(row) + c;
-  if (c + 8 <= cols) {
-    __builtin_memcpy(p, &r, sizeof(r));
-  } else {
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i)
-      if (c + i < cols) p[i] = r.e[i];
-  }
-}
+// ---------------------------------------------------------------------------------------------- rows and vectors
 template <class T>
 __device__ __forceinline__ T* row_of(const Mat& m, uint32_t row) { return static_cast<T*>(m.p) + static_cast<uint64_t>(row) * m.stride; }
 __device__ __forceinline__ float* scale_of(const Mat& m, uint32_t row, uint32_t c) {
   return m.s + static_cast<uint64_t>(row) * m.per_row + (m.lg ? c >> m.lg : 0u);
 }
-
+// A vector as it was loaded, with the scale of codes.
 template <uint32_t TY>
-__device__ __forceinline__ void load8(const Mat& m, uint32_t row, uint32_t c, uint32_t cols, float (&v)[8]) {
-  using T = typename Elem<TY>::type;
-  const Raw<T> r = load_raw(row_of<T>(m, row), c, cols);
-  if constexpr (TY == kQ8) {
-    const float s = c < cols ? as_global(scale_of(m, row, c))[0] : 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = s * static_cast<float>(r.e[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(r.e[i]);
+struct Loaded {
+  Packed<typename Elem<TY>::type> v;
+  float s;
+  __device__ __forceinline__ void from(const Mat& m, uint32_t row, uint32_t c, uint32_t cols) {
+    v = load_ending(row_of<typename Elem<TY>::type>(m, row), c, cols);
+    if constexpr (TY == kQ8) s = as_global(scale_of(m, row, min(c, cols - 1)))[0];
   }
-}
+  __device__ __forceinline__ float at(uint32_t e) const {
+    if constexpr (TY == kQ8) return s * v.at(e);
+    return v.at(e);
+  }
+};
 template <uint32_t TY>
 __device__ __forceinline__ void store8(const Mat& m, uint32_t row, uint32_t c, uint32_t cols, const float (&v)[8]) {
   using T = typename Elem<TY>::type;
-  Raw<T> r;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) r.e[i] = static_cast<T>(v[i]);
-  store_raw(row_of<T>(m, row), c, cols, r);
+  store_ending(row_of<T>(m, row), c, cols, pack<T>(v));
 }
 // v as the matrix' type holds it
 template <uint32_t TY>
@@ -115,10 +80,8 @@ __device__ __forceinline__ uint32_t codes4(const float* x, float inv, uint32_t k
   return (lo | hi) & keep;
 }
 __device__ __forceinline__ void store_codes(const Mat& m, uint32_t row, uint32_t c, uint32_t cols, const float (&v)[8], const Coder& k) {
-  const uint32_t w[2] = {codes4(v, k.inv, k.keep), codes4(v + 4, k.inv, k.keep)};
-  Raw<int8_t> r;
-  __builtin_memcpy(&r, w, 8);
-  store_raw(row_of<int8_t>(m, row), c, cols, r);
+  const Packed<int8_t> r = {{codes4(v, k.inv, k.keep), codes4(v + 4, k.inv, k.keep)}};
+  store_ending(row_of<int8_t>(m, row), c, cols, r);
 }
 // Codes with a scale for each block: the maximum over the block's 8, 16 or 32 neighbouring threads (all lanes take part).
 __device__ __forceinline__ void store_block_codes(const Mat& m, uint32_t row, uint32_t c, uint32_t cols, const float (&v)[8]) {
@@ -139,31 +102,58 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
   const uint32_t b = max(__builtin_amdgcn_readlane(x, 32), __builtin_amdgcn_readlane(x, 48));
   return max(a, b);
 }
-__device__ __forceinline__ float wave_sum(float x) {
+__device__ __forceinline__ float row_total(float x) {  // over each 16 lanes
   x += u2f(dpp_u32<kDppXor1>(f2u(x)));
   x += u2f(dpp_u32<kDppXor2>(f2u(x)));
   x += u2f(dpp_u32<kDppHalfMirror>(f2u(x)));
   x += u2f(dpp_u32<kDppMirror>(f2u(x)));
-  const uint32_t u = f2u(x);
+  return x;
+}
+__device__ __forceinline__ float first_of(float x) { return u2f(__builtin_amdgcn_readfirstlane(f2u(x))); }
+__device__ __forceinline__ float wave_sum(float x) {
+  const uint32_t u = f2u(row_total(x));
   const float a = u2f(__builtin_amdgcn_readlane(u, 0)) + u2f(__builtin_amdgcn_readlane(u, 16));
   const float b = u2f(__builtin_amdgcn_readlane(u, 32)) + u2f(__builtin_amdgcn_readlane(u, 48));
   return a + b;
 }
 
-// A sum and M maxima over the T threads of a row, left in all of them.  The T > 64 threads of a workgroup exchange them through
-// `box`: two sets in turn, so that one barrier a row is enough (a wave that is a row ahead writes the other set, and cannot be two
-// ahead).
-template <int T, int M>
+// The rows of a workgroup of kernels that go over a row twice.  WAVES: a wave for a row, else the workgroup, of up to 16 waves.  V: the
+// vectors of a thread, which are held, or 0: any number, which are not.
+constexpr uint32_t kMostWaves = 16;
+template <bool WAVES_, int V_>
+struct Rows {
+  static constexpr bool WAVES = WAVES_;
+  static constexpr int V = V_, kHeld = V ? V : 1;
+  static constexpr uint32_t kPerGroup = WAVES ? 4 : 1;
+  __device__ static __forceinline__ uint32_t first() { return blockIdx.x * kPerGroup + (WAVES ? threadIdx.x >> 6 : 0); }
+  __device__ static __forceinline__ uint32_t step() { return gridDim.x * kPerGroup; }
+  __device__ static __forceinline__ uint32_t thread() { return WAVES ? threadIdx.x & 63 : threadIdx.x; }
+  // f(first column, place in registers) for each vector of the thread.  All lanes of a wave take part in every call, also those beyond
+  // the row's end.
+  template <class F>
+  __device__ static __forceinline__ void each(uint32_t cols, F f) {
+    const uint32_t threads = WAVES ? 64 : blockDim.x;
+    if constexpr (V > 0) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) f((thread() + j * threads) * 8, j);
+    } else {
+      for (uint32_t base = 0; base < cols; base += threads * 8) f(base + thread() * 8, 0);
+    }
+  }
+};
+
+// A sum and M maxima over the threads of a row, left in all of them.  The waves of a workgroup exchange theirs through `box`: two sets in
+// turn, so that one barrier a row is enough (a wave that is a row ahead writes the other set, and cannot be two ahead).
+template <class R, int M>
 struct RowReducer {
-  static constexpr int kWaves = T / 64;
-  struct Box { float sum[kWaves]; uint32_t largest[M ? M : 1][kWaves]; };
-  Box* box;       // [2], in LDS
+  struct Box { float sum[kMostWaves]; uint32_t largest[M ? M : 1][kMostWaves]; };
+  Box* box;  // [2], in LDS
   uint32_t turn;
   __device__ __forceinline__ void reduce(float& sum, uint32_t* largest) {
     sum = wave_sum(sum);
 #pragma unroll
     for (int i = 0; i < M; ++i) largest[i] = wave_max(largest[i]);
-    if constexpr (T > 64) {
+    if constexpr (!R::WAVES) {
       Box& b = box[turn];
       turn ^= 1;
       if ((threadIdx.x & 63) == 0) {
@@ -172,49 +162,42 @@ struct RowReducer {
         for (int i = 0; i < M; ++i) b.largest[i][threadIdx.x >> 6] = largest[i];
       }
       __syncthreads();
-      sum = b.sum[0];
+      // a lane of sixteen for each wave
+      const uint32_t w = threadIdx.x & 15;
+      const bool there = w < blockDim.x >> 6;
+      sum = first_of(row_total(there ? b.sum[w] : 0.0f));
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) sum += b.sum[w];
-#pragma unroll
-      for (int i = 0; i < M; ++i) {
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) largest[i] = max(largest[i], b.largest[i][w]);
-      }
+      for (int i = 0; i < M; ++i) largest[i] = __builtin_amdgcn_readfirstlane(row_max(there ? b.largest[i][w] : 0u));
     }
   }
 };
-
-// The rows of a workgroup of kernels that go over a row twice: T threads for a row.
-template <int T> struct Rows {
-  static constexpr int kThreads = T < 256 ? 256 : T;
-  static constexpr uint32_t kPerGroup = kThreads / T;
-  __device__ static __forceinline__ uint32_t first() { return blockIdx.x * kPerGroup + (T < 256 ? threadIdx.x / T : 0); }
-  __device__ static __forceinline__ uint32_t step() { return gridDim.x * kPerGroup; }
-  __device__ static __forceinline__ uint32_t column() { return (threadIdx.x & (T - 1)) * 8; }
-};
-// f(first column, place in registers) for each vector of the thread: V of them that are held, or (V = 0) any number that are not.
-// All lanes of a wave take part in every call, also those beyond the row's end.
-template <int T, int V, class F>
-__device__ __forceinline__ void each_vector(uint32_t cols, F f) {
-  if constexpr (V > 0) {
-#pragma unroll
-    for (int j = 0; j < V; ++j) f(Rows<T>::column() + static_cast<uint32_t>(j) * T * 8, j);
-  } else {
-    for (uint32_t base = 0; base < cols; base += T * 8) f(base + Rows<T>::column(), 0);
-  }
-}
-template <int V> constexpr int kHeld = V ? V : 1;
+#define STQ_ROWS_KERNEL __global__ __launch_bounds__(R::WAVES ? 256 : 64 * kMostWaves) void
 
 // ---------------------------------------------------------------------------------------------- conversion
-template <uint32_t TY, int T, int V>
-__global__ __launch_bounds__(Rows<T>::kThreads) void quantize_kernel(const RowsArgs a) {
-  __shared__ typename RowReducer<T, 1>::Box box[2];
-  RowReducer<T, 1> red{box, 0};
-  for (uint32_t row = Rows<T>::first(); row < a.rows; row += Rows<T>::step()) {
-    float v[kHeld<V>][8];
+template <uint32_t TY, class R>
+STQ_ROWS_KERNEL quantize_kernel(const RowsArgs a) {
+  constexpr int V = R::V;
+  __shared__ typename RowReducer<R, 1>::Box box[2];
+  RowReducer<R, 1> red{box, 0};
+  Loaded<TY> next[R::kHeld];
+  const auto fetch = [&](uint32_t row) {
+    if (V && row < a.rows) R::each(a.cols, [&](uint32_t c, int at) { next[at].from(a.x, row, c, a.cols); });
+  };
+  fetch(R::first());
+  for (uint32_t row = R::first(); row < a.rows; row += R::step()) {
+    float v[R::kHeld][8];
     uint32_t largest = 0;
-    each_vector<T, V>(a.cols, [&](uint32_t c, int at) {
-      load8<TY>(a.x, row, c, a.cols, v[at]);
+    const auto take = [&](uint32_t c, int at) {
+      if (!V) next[at].from(a.x, row, c, a.cols);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[at][i] = next[at].at(i);
+    };
+    if (V) {
+      R::each(a.cols, take);
+      fetch(row + R::step());
+    }
+    R::each(a.cols, [&](uint32_t c, int at) {
+      if (!V) take(c, at);
       if (a.out.lg) store_block_codes(a.out, row, c, a.cols, v[at]);
       else largest = max(largest, largest8(v[at]));
     });
@@ -222,16 +205,18 @@ __global__ __launch_bounds__(Rows<T>::kThreads) void quantize_kernel(const RowsA
     float none = 0.0f;
     red.reduce(none, &largest);
     const Coder k = coder_of(largest);
-    each_vector<T, V>(a.cols, [&](uint32_t c, int at) {
+    R::each(a.cols, [&](uint32_t c, int at) {
       if (c >= a.cols) return;
-      if (!V) load8<TY>(a.x, row, c, a.cols, v[at]);
+      if (!V) take(c, at);
       store_codes(a.out, row, c, a.cols, v[at], k);
     });
-    if (Rows<T>::column() == 0) as_global(a.out.s)[row] = k.scale;
+    if (R::thread() == 0) as_global(a.out.s)[row] = k.scale;
   }
 }
 
-// Elementwise kernels: 2^lg_t threads for a row, blockIdx.x along the row, blockIdx.y over the rows.
+// Elementwise kernels: 2^lg_t threads for a row, blockIdx.x along the row, blockIdx.y over the rows, four of which a thread has under
+// way together.
+constexpr uint32_t kTogether = 4;
 struct Flat {
   uint32_t c, row, step;
   __device__ __forceinline__ explicit Flat(uint32_t lg_t) {
@@ -245,40 +230,65 @@ template <uint32_t TY>
 __global__ __launch_bounds__(256) void dequantize_kernel(const RowsArgs a, uint32_t lg_t) {
   const Flat f(lg_t);
   if (f.c >= a.cols) return;
-  for (uint32_t row = f.row; row < a.rows; row += f.step) {
-    float v[8];
-    load8<kQ8>(a.x, row, f.c, a.cols, v);
-    store8<TY>(a.out, row, f.c, a.cols, v);
+  for (uint32_t row = f.row; row < a.rows; row += kTogether * f.step) {
+    Loaded<kQ8> x[kTogether];
+#pragma unroll
+    for (uint32_t k = 0; k < kTogether; ++k)
+      if (row + k * f.step < a.rows) x[k].from(a.x, row + k * f.step, f.c, a.cols);
+#pragma unroll
+    for (uint32_t k = 0; k < kTogether; ++k) {
+      if (row + k * f.step >= a.rows) break;
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = x[k].at(i);
+      store8<TY>(a.out, row + k * f.step, f.c, a.cols, v);
+    }
   }
 }
 
 // ---------------------------------------------------------------------------------------------- norm
 // One pass: with h the sum, the scale of y is rstd * max|h w| / 127 and its codes are rint(h w * (127 / max|h w|)), free of rstd, so
 // that the sum of squares and the maxima are reduced together.
-template <uint32_t TY, int T, int V>
-__global__ __launch_bounds__(Rows<T>::kThreads) void rms_norm_kernel(const NormArgs a) {
-  __shared__ typename RowReducer<T, 2>::Box box[2];
-  RowReducer<T, 2> red{box, 0};
-  for (uint32_t row = Rows<T>::first(); row < a.rows; row += Rows<T>::step()) {
-    float h[kHeld<V>][8];
+template <uint32_t TY, class R>
+STQ_ROWS_KERNEL rms_norm_kernel(const NormArgs a) {
+  constexpr int V = R::V;
+  __shared__ typename RowReducer<R, 2>::Box box[2];
+  RowReducer<R, 2> red{box, 0};
+  Loaded<TY> next[R::kHeld], next_r[R::kHeld];
+  Loaded<kF32> w[R::kHeld];
+  const Mat weight{const_cast<float*>(a.weight), nullptr, 0, 0, 0};
+  const auto load = [&](uint32_t row, uint32_t c, int at) {
+    next[at].from(a.x, row, c, a.cols);
+    if (a.residual.p) next_r[at].from(a.residual, row, c, a.cols);
+  };
+  const auto fetch = [&](uint32_t row) {
+    if (V && row < a.rows) R::each(a.cols, [&](uint32_t c, int at) { load(row, c, at); });
+  };
+  fetch(R::first());
+  if (V) R::each(a.cols, [&](uint32_t c, int at) { w[at].from(weight, 0, c, a.cols); });
+  for (uint32_t row = R::first(); row < a.rows; row += R::step()) {
+    float h[R::kHeld][8];
     float squares = 0.0f;
     uint32_t largest[2] = {0, 0};  // of h * weight, of h
-    auto add = [&](uint32_t c, float (&v)[8]) {  // h of a vector
-      load8<TY>(a.x, row, c, a.cols, v);
-      if (!a.residual.p) return;
-      float r[8];
-      load8<TY>(a.residual, row, c, a.cols, r);
+    const auto add = [&](uint32_t c, int at) {  // h of a vector
+      if (!V) {
+        load(row, c, at);
+        w[at].from(weight, 0, c, a.cols);
+      }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = rounded<TY>(v[i] + r[i]);
+      for (int i = 0; i < 8; ++i) h[at][i] = a.residual.p ? rounded<TY>(next[at].at(i) + next_r[at].at(i)) : next[at].at(i);
     };
-    each_vector<T, V>(a.cols, [&](uint32_t c, int at) {
-      add(c, h[at]);
+    if (V) {
+      R::each(a.cols, add);
+      fetch(row + R::step());
+    }
+    R::each(a.cols, [&](uint32_t c, int at) {
+      if (!V) add(c, at);
       if (a.sum.p && c < a.cols) store8<TY>(a.sum, row, c, a.cols, h[at]);
-      const Raw<float> w = load_raw(a.weight, c, a.cols);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         squares = fmaf(h[at][i], h[at][i], squares);
-        largest[0] = max(largest[0], magnitude(h[at][i] * w.e[i]));
+        largest[0] = max(largest[0], magnitude(h[at][i] * w[at].at(i)));
         largest[1] = max(largest[1], magnitude(h[at][i]));
       }
       if (a.saved.p && a.saved.lg) store_block_codes(a.saved, row, c, a.cols, h[at]);
@@ -288,20 +298,26 @@ __global__ __launch_bounds__(Rows<T>::kThreads) void rms_norm_kernel(const NormA
     const bool finite = magnitude(squares) < kInf;
     const float rstd = finite ? 1.0f / __fsqrt_rn(squares / static_cast<float>(a.cols) + a.eps) : __builtin_nanf("");
     const Coder k = coder_of(finite ? largest[0] : kInf), ks = coder_of(largest[1]);
-    each_vector<T, V>(a.cols, [&](uint32_t c, int at) {
+    R::each(a.cols, [&](uint32_t c, int at) {
       if (c >= a.cols) return;
-      if (!V) {  // sum may have taken x's or residual's place
-        if (a.sum.p) load8<TY>(a.sum, row, c, a.cols, h[at]);
-        else add(c, h[at]);
+      if (!V) {  // the sum may have taken x's or residual's place
+        if (a.sum.p) {
+          Loaded<TY> t;
+          t.from(a.sum, row, c, a.cols);
+          w[at].from(weight, 0, c, a.cols);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) h[at][i] = t.at(i);
+        } else {
+          add(c, at);
+        }
       }
-      const Raw<float> w = load_raw(a.weight, c, a.cols);
       float y[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = h[at][i] * w.e[i];
+      for (int i = 0; i < 8; ++i) y[i] = h[at][i] * w[at].at(i);
       store_codes(a.y, row, c, a.cols, y, k);
       if (a.saved.p && !a.saved.lg) store_codes(a.saved, row, c, a.cols, h[at], ks);
     });
-    if (Rows<T>::column() == 0) {
+    if (R::thread() == 0) {
       as_global(a.y.s)[row] = k.scale * rstd;
       if (a.rstd) as_global(a.rstd)[row] = rstd;
       if (a.saved.p && !a.saved.lg) as_global(a.saved.s)[row] = ks.scale;
@@ -311,66 +327,80 @@ __global__ __launch_bounds__(Rows<T>::kThreads) void rms_norm_kernel(const NormA
 
 // Gradients of the norm.  A workgroup goes through rows of its own and adds up its part of dweight, in registers (for rows that are
 // not held: in `partial` itself, each of whose columns has one thread); the second kernel sums the parts in one order.
-template <uint32_t TS, uint32_t TY, int T, int V>
-__global__ __launch_bounds__(Rows<T>::kThreads) void rms_norm_grad_kernel(const NormGradArgs a) {
-  __shared__ typename RowReducer<T, 0>::Box box[2];
-  RowReducer<T, 0> red{box, 0};
+template <uint32_t TS, uint32_t TY, class R>
+STQ_ROWS_KERNEL rms_norm_grad_kernel(const NormGradArgs a) {
+  constexpr int V = R::V;
+  __shared__ typename RowReducer<R, 0>::Box box[2];
+  RowReducer<R, 0> red{box, 0};
   float* const part = a.partial + static_cast<uint64_t>(blockIdx.x) * a.cols;
-  float dw[kHeld<V>][8];
+  const Mat to_part{part, nullptr, 0, 0, 0}, weight{const_cast<float*>(a.weight), nullptr, 0, 0, 0};
+  float dw[R::kHeld][8];
 #pragma unroll
-  for (int j = 0; j < kHeld<V>; ++j)
+  for (int j = 0; j < R::kHeld; ++j)
 #pragma unroll
     for (int i = 0; i < 8; ++i) dw[j][i] = 0.0f;
-  for (uint32_t row = Rows<T>::first(); row < a.rows; row += Rows<T>::step()) {
+  Loaded<TS> next_n[R::kHeld];
+  Loaded<TY> next_g[R::kHeld], next_r[R::kHeld];
+  Loaded<kF32> w[R::kHeld];
+  const auto load = [&](uint32_t row, uint32_t c, int at) {
+    next_n[at].from(a.sum, row, c, a.cols);
+    next_g[at].from(a.dy, row, c, a.cols);
+    if (a.dres.p) next_r[at].from(a.dres, row, c, a.cols);
+  };
+  const auto fetch = [&](uint32_t row) {
+    if (V && row < a.rows) R::each(a.cols, [&](uint32_t c, int at) { load(row, c, at); });
+  };
+  fetch(R::first());
+  if (V) R::each(a.cols, [&](uint32_t c, int at) { w[at].from(weight, 0, c, a.cols); });
+  for (uint32_t row = R::first(); row < a.rows; row += R::step()) {
     const float rstd = as_global(a.rstd)[row];
-    float n[kHeld<V>][8], g[kHeld<V>][8], dot = 0.0f;
-    auto take = [&](uint32_t c, int at) {  // n = sum * rstd and dy
-      load8<TS>(a.sum, row, c, a.cols, n[at]);
-      load8<TY>(a.dy, row, c, a.cols, g[at]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) n[at][i] *= rstd;
+    Loaded<TS> n[R::kHeld];
+    Loaded<TY> g[R::kHeld], r[R::kHeld];
+    float dot = 0.0f;
+    const auto take = [&](uint32_t c, int at) {
+      if (!V) {
+        load(row, c, at);
+        w[at].from(weight, 0, c, a.cols);
+      }
+      n[at] = next_n[at];
+      g[at] = next_g[at];
+      r[at] = next_r[at];
     };
-    each_vector<T, V>(a.cols, [&](uint32_t c, int at) {
-      take(c, at);
-      const Raw<float> w = load_raw(a.weight, c, a.cols);
+    if (V) {
+      R::each(a.cols, take);
+      fetch(row + R::step());
+    }
+    R::each(a.cols, [&](uint32_t c, int at) {
+      if (!V) take(c, at);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) dot = fmaf(g[at][i] * w.e[i], n[at][i], dot);
+      for (int i = 0; i < 8; ++i) dot = fmaf(g[at].at(i) * w[at].at(i), n[at].at(i) * rstd, dot);
     });
     red.reduce(dot, nullptr);
     const float mean = dot / static_cast<float>(a.cols);
-    each_vector<T, V>(a.cols, [&](uint32_t c, int at) {
+    R::each(a.cols, [&](uint32_t c, int at) {
       if (c >= a.cols) return;
       if (!V) {
         take(c, at);
-        if (row != Rows<T>::first()) {
-          const Raw<float> r = load_raw(part, c, a.cols);
+        Loaded<kF32> t;
+        if (row != R::first()) t.from(to_part, 0, c, a.cols);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) dw[at][i] = r.e[i];
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) dw[at][i] = 0.0f;
-        }
+        for (int i = 0; i < 8; ++i) dw[at][i] = row != R::first() ? t.at(i) : 0.0f;
       }
-      const Raw<float> w = load_raw(a.weight, c, a.cols);
       float d[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        dw[at][i] = fmaf(g[at][i], n[at][i], dw[at][i]);
-        d[i] = rstd * (g[at][i] * w.e[i] - n[at][i] * mean);
-      }
-      if (a.dres.p) {
-        float r[8];
-        load8<TY>(a.dres, row, c, a.cols, r);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] += r[i];
+        const float x = n[at].at(i) * rstd;
+        dw[at][i] = fmaf(g[at].at(i), x, dw[at][i]);
+        d[i] = rstd * (g[at].at(i) * w[at].at(i) - x * mean);
+        if (a.dres.p) d[i] += r[at].at(i);
       }
       store8<TY>(a.dx, row, c, a.cols, d);
-      if (!V) store8<kF32>(Mat{part, nullptr, 0, 0, 0}, 0, c, a.cols, dw[at]);
+      if (!V) store8<kF32>(to_part, 0, c, a.cols, dw[at]);
     });
   }
   if (!V) return;
-  if constexpr (T < 256) {  // the rows of several waves
-    __shared__ float of_wave[3][kHeld<V>][64][9];
+  if constexpr (R::WAVES) {  // the rows of several waves
+    __shared__ float of_wave[3][R::kHeld][64][9];
     const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     if (wave) {
 #pragma unroll
@@ -385,68 +415,101 @@ __global__ __launch_bounds__(Rows<T>::kThreads) void rms_norm_grad_kernel(const 
 #pragma unroll
       for (int i = 0; i < 8; ++i) dw[j][i] += (of_wave[0][j][lane][i] + of_wave[1][j][lane][i]) + of_wave[2][j][lane][i];
   }
-  each_vector<T, V>(a.cols, [&](uint32_t c, int at) {
-    if (c < a.cols) store8<kF32>(Mat{part, nullptr, 0, 0, 0}, 0, c, a.cols, dw[at]);
+  R::each(a.cols, [&](uint32_t c, int at) {
+    if (c < a.cols) store8<kF32>(to_part, 0, c, a.cols, dw[at]);
   });
 }
-// dweight[c] = the sum of the parts of column c: 64 columns and 8 waves a workgroup, which take the parts in turn.
-__global__ __launch_bounds__(512) void sum_parts_kernel(const float* partial, float* out, uint32_t groups, uint32_t cols) {
-  __shared__ float box[8][64];
-  const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = blockIdx.x * 64 + lane;
+// dweight[c] = the sum of the parts of column c: 32 columns a workgroup, whose 32 half waves take the parts in turn.
+__global__ __launch_bounds__(1024) void sum_parts_kernel(const float* partial, float* out, uint32_t groups, uint32_t cols) {
+  __shared__ float box[32][33];
+  const uint32_t turn = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * 32 + lane;
   float s = 0.0f;
   if (c < cols) {
-#pragma unroll 8
-    for (uint32_t g = wave; g < groups; g += 8) s += as_global(partial)[static_cast<uint64_t>(g) * cols + c];
+#pragma unroll 16
+    for (uint32_t g = turn; g < groups; g += 32) s += as_global(partial)[static_cast<uint64_t>(g) * cols + c];
   }
-  box[wave][lane] = s;
+  box[turn][lane] = s;
   __syncthreads();
-  if (wave || c >= cols) return;
+  if (turn || c >= cols) return;
 #pragma unroll
-  for (int w = 1; w < 8; ++w) s += box[w][lane];
+  for (int k = 1; k < 32; ++k) s += box[k][lane];
   as_global(out)[c] = s;
 }
 
 // ---------------------------------------------------------------------------------------------- gated activation
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
 
-template <uint32_t TY, int T, int V>
-__global__ __launch_bounds__(Rows<T>::kThreads) void gated_kernel(const GatedArgs a) {
-  __shared__ typename RowReducer<T, 3>::Box box[2];
-  RowReducer<T, 3> red{box, 0};
-  for (uint32_t row = Rows<T>::first(); row < a.rows; row += Rows<T>::step()) {
-    float y[kHeld<V>][8], g[kHeld<V>][8], u[kHeld<V>][8];
+template <uint32_t TY, class R>
+STQ_ROWS_KERNEL gated_kernel(const GatedArgs a) {
+  constexpr int V = R::V;
+  __shared__ typename RowReducer<R, 3>::Box box[2];
+  RowReducer<R, 3> red{box, 0};
+  Loaded<TY> next_g[R::kHeld], next_u[R::kHeld];
+  const auto load = [&](uint32_t row, uint32_t c, int at) {
+    next_g[at].from(a.gate, row, c, a.cols);
+    next_u[at].from(a.up, row, c, a.cols);
+  };
+  const auto fetch = [&](uint32_t row) {
+    if (V && row < a.rows) R::each(a.cols, [&](uint32_t c, int at) { load(row, c, at); });
+  };
+  fetch(R::first());
+  for (uint32_t row = R::first(); row < a.rows; row += R::step()) {
+    float y[R::kHeld][8];
+    Loaded<TY> g[R::kHeld], u[R::kHeld];
     uint32_t largest[3] = {0, 0, 0};  // of y, gate, up
-    auto take = [&](uint32_t c, int at) {
-      load8<TY>(a.gate, row, c, a.cols, g[at]);
-      load8<TY>(a.up, row, c, a.cols, u[at]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) y[at][i] = g[at][i] * sigmoid(g[at][i]) * u[at][i];
+    const auto take = [&](uint32_t c, int at) {
+      if (!V) load(row, c, at);
+      g[at] = next_g[at];
+      u[at] = next_u[at];
     };
-    each_vector<T, V>(a.cols, [&](uint32_t c, int at) {
-      take(c, at);
+    const auto product = [&](int at, float (&gate)[8], float (&up)[8]) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        gate[i] = g[at].at(i);
+        up[i] = u[at].at(i);
+        y[at][i] = gate[i] * sigmoid(gate[i]) * up[i];
+      }
+    };
+    if (V) {
+      R::each(a.cols, take);
+      fetch(row + R::step());
+    }
+    R::each(a.cols, [&](uint32_t c, int at) {
+      if (!V) take(c, at);
+      float gate[8], up[8];
+      product(at, gate, up);
       largest[0] = max(largest[0], largest8(y[at]));
       if (!a.saved_gate.p) return;
       if (a.saved_gate.lg) {
-        store_block_codes(a.saved_gate, row, c, a.cols, g[at]);
-        store_block_codes(a.saved_up, row, c, a.cols, u[at]);
+        store_block_codes(a.saved_gate, row, c, a.cols, gate);
+        store_block_codes(a.saved_up, row, c, a.cols, up);
       } else {
-        largest[1] = max(largest[1], largest8(g[at]));
-        largest[2] = max(largest[2], largest8(u[at]));
+        largest[1] = max(largest[1], largest8(gate));
+        largest[2] = max(largest[2], largest8(up));
       }
     });
     float none = 0.0f;
     red.reduce(none, largest);
     const bool rows_saved = a.saved_gate.p && !a.saved_gate.lg;
     const Coder k = coder_of(largest[0]), kg = coder_of(largest[1]), ku = coder_of(largest[2]);
-    each_vector<T, V>(a.cols, [&](uint32_t c, int at) {
+    R::each(a.cols, [&](uint32_t c, int at) {
       if (c >= a.cols) return;
-      if (!V) take(c, at);
+      float gate[8], up[8];
+      if (!V) {
+        take(c, at);
+        product(at, gate, up);
+      }
       store_codes(a.y, row, c, a.cols, y[at], k);
       if (!rows_saved) return;
-      store_codes(a.saved_gate, row, c, a.cols, g[at], kg);
-      store_codes(a.saved_up, row, c, a.cols, u[at], ku);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        gate[i] = g[at].at(i);
+        up[i] = u[at].at(i);
+      }
+      store_codes(a.saved_gate, row, c, a.cols, gate, kg);
+      store_codes(a.saved_up, row, c, a.cols, up, ku);
     });
-    if (Rows<T>::column() == 0) {
+    if (R::thread() == 0) {
       as_global(a.y.s)[row] = k.scale;
       if (rows_saved) {
         as_global(a.saved_gate.s)[row] = kg.scale;
@@ -458,34 +521,49 @@ __global__ __launch_bounds__(Rows<T>::kThreads) void gated_kernel(const GatedArg
 
 template <uint32_t TS, uint32_t TY>
 __global__ __launch_bounds__(256) void gated_grad_kernel(const GatedGradArgs a, uint32_t lg_t) {
+  constexpr uint32_t kRowsNow = kTogether / 2;  // (of three inputs)
   const Flat f(lg_t);
   if (f.c >= a.cols) return;
-  for (uint32_t row = f.row; row < a.rows; row += f.step) {
-    float g[8], u[8], d[8], dg[8], du[8];
-    load8<TS>(a.gate, row, f.c, a.cols, g);
-    load8<TS>(a.up, row, f.c, a.cols, u);
-    load8<TY>(a.dy, row, f.c, a.cols, d);
+  for (uint32_t row = f.row; row < a.rows; row += kRowsNow * f.step) {
+    Loaded<TS> gate[kRowsNow], up[kRowsNow];
+    Loaded<TY> dy[kRowsNow];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float s = sigmoid(g[i]);
-      dg[i] = d[i] * (u[i] * (s * (1.0f + g[i] * (1.0f - s))));
-      du[i] = d[i] * (g[i] * s);
+    for (uint32_t k = 0; k < kRowsNow; ++k)
+      if (row + k * f.step < a.rows) {
+        gate[k].from(a.gate, row + k * f.step, f.c, a.cols);
+        up[k].from(a.up, row + k * f.step, f.c, a.cols);
+        dy[k].from(a.dy, row + k * f.step, f.c, a.cols);
+      }
+#pragma unroll
+    for (uint32_t k = 0; k < kRowsNow; ++k) {
+      if (row + k * f.step >= a.rows) break;
+      float dg[8], du[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float g = gate[k].at(i), d = dy[k].at(i), s = sigmoid(g);
+        dg[i] = d * (up[k].at(i) * (s * (1.0f + g * (1.0f - s))));
+        du[i] = d * (g * s);
+      }
+      store8<TY>(a.dgate, row + k * f.step, f.c, a.cols, dg);
+      store8<TY>(a.dup, row + k * f.step, f.c, a.cols, du);
     }
-    store8<TY>(a.dgate, row, f.c, a.cols, dg);
-    store8<TY>(a.dup, row, f.c, a.cols, du);
   }
 }
 
 // ---------------------------------------------------------------------------------------------- launches
-// Threads and vectors for a row of `cols` columns: f(T, V) as compile-time constants.
-template <int T_, int V_> struct Shape { static constexpr int T = T_, V = V_; };
-template <class F>
-void with_shape(uint32_t cols, F f) {
-  if (cols <= 1024) f(Shape<64, 2>{});
-  else if (cols <= 4096) f(Shape<256, 2>{});
-  else if (cols <= 8192) f(Shape<512, 2>{});
-  else if (cols <= 16384) f(Shape<1024, 2>{});
-  else f(Shape<1024, 0>{});
+// The shape for rows of `cols` columns: f(Rows<WAVES, V>, threads of a workgroup).  TWO: whether a thread may hold two vectors (the
+// norm's gradients have no registers for that).
+template <bool TWO, class F>
+void with_rows(uint32_t cols, F f) {
+  const uint32_t vectors = (cols - 1) / 8 + 1, most = 64 * kMostWaves;
+  const auto threads = [&](uint32_t v) { return ((vectors + v - 1) / v + 63) / 64 * 64; };
+  if (vectors <= 64) return f(Rows<true, 1>{}, 256u);
+  if constexpr (TWO) {
+    if (vectors <= 128) return f(Rows<true, 2>{}, 256u);
+    if (vectors > most && vectors <= 2 * most) return f(Rows<false, 2>{}, threads(2));
+  }
+  if (vectors <= most) f(Rows<false, 1>{}, threads(1));
+  else f(Rows<false, 0>{}, most);
 }
 template <class F>
 void with_type(uint32_t type, F f) {
@@ -497,61 +575,70 @@ void with_kept(uint32_t type, F f) {
   if (type == kQ8) f(std::integral_constant<uint32_t, kQ8>{});
   else with_type(type, f);
 }
-// Workgroups for rows held by T threads: as many as fit the card at once, which then go through the rows.
-template <int T>
-uint32_t groups_of(uint32_t rows, uint32_t n_cu) {
-  const uint32_t need = (rows + Rows<T>::kPerGroup - 1) / Rows<T>::kPerGroup, fit = n_cu * (2048 / Rows<T>::kThreads);
+// Workgroups for rows that are held: as many as fit the card at once, which then go through the rows.
+template <class R>
+uint32_t groups_of(uint32_t rows, uint32_t threads, uint32_t n_cu) {
+  const uint32_t need = (rows + R::kPerGroup - 1) / R::kPerGroup, fit = n_cu * ((R::V == 1 ? 20 : 16) * 64 / threads);
   return need < fit ? need : fit;
 }
-// Launch shape of the elementwise kernels.
+// Launch shape of the elementwise kernels: of 32 to 256 threads for a row (8 for the narrowest) those that leave the fewest without
+// work; 16 workgroups on a CU, which go through the rows.
 struct FlatShape { uint32_t lg_t; dim3 grid; };
-FlatShape flat_shape(uint32_t rows, uint32_t cols) {
+FlatShape flat_shape(uint32_t rows, uint32_t cols, uint32_t n_cu) {
   const uint32_t vectors = (cols - 1) / 8 + 1;
-  uint32_t lg = 3;
-  while (lg < 8 && (1u << lg) < vectors) ++lg;
-  const uint32_t per_group = 256u >> lg, y = (rows - 1) / per_group + 1;
-  return {lg, dim3(((vectors - 1) >> lg) + 1, y < 16384u ? y : 16384u)};
+  const auto whole = [&](uint32_t lg) { return (((vectors - 1) >> lg) + 1) << lg; };
+  uint32_t lg = vectors <= 8 ? 3 : (vectors <= 16 ? 4 : 8);
+  for (uint32_t l = 7; lg > 4 && l >= 5; --l)
+    if (whole(l) < whole(lg)) lg = l;
+  const uint32_t x = whole(lg) >> lg, per_group = 256u >> lg, need = (rows - 1) / per_group + 1;
+  const uint32_t fit = (n_cu * 16 - 1) / x + 1;
+  const uint32_t y = need < fit ? need : fit;
+  return {lg, dim3(x, y < 65535u ? y : 65535u)};
 }
 
 }  // namespace
 
 int launch_quantize_rows(const RowsArgs& a, uint32_t type, uint32_t n_cu, void* stream) {
-  with_shape(a.cols, [&](auto s) { with_type(type, [&](auto ty) {
-    quantize_kernel<ty(), s.T, s.V><<<groups_of<s.T>(a.rows, n_cu), Rows<s.T>::kThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
+  with_rows<true>(a.cols, [&](auto r, uint32_t threads) { with_type(type, [&](auto ty) {
+    using R = decltype(r);
+    quantize_kernel<ty(), R><<<groups_of<R>(a.rows, threads, n_cu), threads, 0, static_cast<hipStream_t>(stream)>>>(a);
   }); });
   return hipGetLastError();
 }
-int launch_dequantize_rows(const RowsArgs& a, uint32_t type, void* stream) {
-  const FlatShape f = flat_shape(a.rows, a.cols);
+int launch_dequantize_rows(const RowsArgs& a, uint32_t type, uint32_t n_cu, void* stream) {
+  const FlatShape f = flat_shape(a.rows, a.cols, n_cu);
   with_type(type, [&](auto ty) { dequantize_kernel<ty()><<<f.grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, f.lg_t); });
   return hipGetLastError();
 }
 int launch_rms_norm(const NormArgs& a, uint32_t type, uint32_t n_cu, void* stream) {
-  with_shape(a.cols, [&](auto s) { with_type(type, [&](auto ty) {
-    rms_norm_kernel<ty(), s.T, s.V><<<groups_of<s.T>(a.rows, n_cu), Rows<s.T>::kThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
+  with_rows<true>(a.cols, [&](auto r, uint32_t threads) { with_type(type, [&](auto ty) {
+    using R = decltype(r);
+    rms_norm_kernel<ty(), R><<<groups_of<R>(a.rows, threads, n_cu), threads, 0, static_cast<hipStream_t>(stream)>>>(a);
   }); });
   return hipGetLastError();
 }
 int launch_rms_norm_grad(NormGradArgs a, uint32_t sum_type, uint32_t type, void* stream) {
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  a.groups = norm_grad_groups(a.rows, a.cols);
-  if (a.groups) {
-    with_shape(a.cols, [&](auto s) { with_kept(sum_type, [&](auto ts) { with_type(type, [&](auto ty) {
-      rms_norm_grad_kernel<ts(), ty(), s.T, s.V><<<a.groups, Rows<s.T>::kThreads, 0, st>>>(a);
+  const uint32_t groups = norm_grad_groups(a.rows, a.cols);
+  if (groups) {
+    with_rows<false>(a.cols, [&](auto r, uint32_t threads) { with_kept(sum_type, [&](auto ts) { with_type(type, [&](auto ty) {
+      using R = decltype(r);
+      rms_norm_grad_kernel<ts(), ty(), R><<<groups, threads, 0, st>>>(a);
     }); }); });
     if (const hipError_t e = hipGetLastError()) return e;
   }
-  sum_parts_kernel<<<(a.cols - 1) / 64 + 1, 512, 0, st>>>(a.partial, a.dweight, a.groups, a.cols);
+  sum_parts_kernel<<<(a.cols - 1) / 32 + 1, 1024, 0, st>>>(a.partial, a.dweight, groups, a.cols);
   return hipGetLastError();
 }
 int launch_gated(const GatedArgs& a, uint32_t type, uint32_t n_cu, void* stream) {
-  with_shape(a.cols, [&](auto s) { with_type(type, [&](auto ty) {
-    gated_kernel<ty(), s.T, s.V><<<groups_of<s.T>(a.rows, n_cu), Rows<s.T>::kThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
+  with_rows<true>(a.cols, [&](auto r, uint32_t threads) { with_type(type, [&](auto ty) {
+    using R = decltype(r);
+    gated_kernel<ty(), R><<<groups_of<R>(a.rows, threads, n_cu), threads, 0, static_cast<hipStream_t>(stream)>>>(a);
   }); });
   return hipGetLastError();
 }
-int launch_gated_grad(const GatedGradArgs& a, uint32_t kept_type, uint32_t type, void* stream) {
-  const FlatShape f = flat_shape(a.rows, a.cols);
+int launch_gated_grad(const GatedGradArgs& a, uint32_t kept_type, uint32_t type, uint32_t n_cu, void* stream) {
+  const FlatShape f = flat_shape(a.rows, a.cols, n_cu);
   with_kept(kept_type, [&](auto ts) { with_type(type, [&](auto ty) {
     gated_grad_kernel<ts(), ty()><<<f.grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, f.lg_t);
   }); });
