@@ -48,10 +48,11 @@ struct MatmulArgs {
   uint32_t m, n, k;
 };
 
-constexpr uint32_t kNormGroups = 512;  // partial sums of dweight at most
+// Workgroups of the norm's gradients, each of which leaves a part of dweight: as many as have 16 waves on each of 256 CUs.
 inline uint32_t norm_grad_groups(uint64_t rows, uint32_t cols) {
-  const uint64_t at_once = cols <= 512 ? 4 : 1, g = (rows + at_once - 1) / at_once;  // (rows of a workgroup, see with_rows)
-  return g < kNormGroups ? static_cast<uint32_t>(g) : kNormGroups;
+  const uint64_t at_once = cols <= 512 ? 4 : 1, need = (rows + at_once - 1) / at_once;  // (rows of a workgroup, see with_rows)
+  const uint32_t waves = cols <= 512 ? 4 : (cols <= 8192 ? (cols + 511) / 512 : 16), most = 4096 / waves;
+  return need < most ? static_cast<uint32_t>(need) : most;
 }
 
 // Launchers; `stream` is a hipStream_t.  Return a hipError_t as int.  rows, m > 0.

@@ -72,8 +72,8 @@ __device__ __forceinline__ Coder coder_of(uint32_t largest) {
   const bool finite = largest < kInf;
   return {127.0f / a, finite ? a / 127.0f : __builtin_nanf(""), finite ? 0xFFFFFFFFu : 0u};
 }
-// rint by the addition of 1.5 * 2^23: the low byte of the sum is the code in two's complement
-__device__ __forceinline__ uint32_t code_byte(float x, float inv) { return f2u(x * inv + 12582912.0f); }
+// rint by the addition of 1.5 * 2^23, of the product as it is: the low byte of the sum is the code in two's complement
+__device__ __forceinline__ uint32_t code_byte(float x, float inv) { return f2u(fmaf(x, inv, 12582912.0f)); }
 __device__ __forceinline__ uint32_t codes4(const float* x, float inv, uint32_t keep) {
   const uint32_t lo = __builtin_amdgcn_perm(code_byte(x[1], inv), code_byte(x[0], inv), 0x0C0C0400u);
   const uint32_t hi = __builtin_amdgcn_perm(code_byte(x[3], inv), code_byte(x[2], inv), 0x04000C0Cu);
@@ -439,28 +439,20 @@ __global__ __launch_bounds__(1024) void sum_parts_kernel(const float* partial, f
 // ---------------------------------------------------------------------------------------------- gated activation
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
 
+// (No row is loaded ahead here: more waves hide more than a row of each would.)
+template <class R> constexpr uint32_t kGatedWaves = R::V == 2 ? 6 : 8;  // of a SIMD
 template <uint32_t TY, class R>
-STQ_ROWS_KERNEL gated_kernel(const GatedArgs a) {
+__global__ __launch_bounds__(R::WAVES ? 256 : 64 * kMostWaves, kGatedWaves<R>) void gated_kernel(const GatedArgs a) {
   constexpr int V = R::V;
   __shared__ typename RowReducer<R, 3>::Box box[2];
   RowReducer<R, 3> red{box, 0};
-  Loaded<TY> next_g[R::kHeld], next_u[R::kHeld];
-  const auto load = [&](uint32_t row, uint32_t c, int at) {
-    next_g[at].from(a.gate, row, c, a.cols);
-    next_u[at].from(a.up, row, c, a.cols);
-  };
-  const auto fetch = [&](uint32_t row) {
-    if (V && row < a.rows) R::each(a.cols, [&](uint32_t c, int at) { load(row, c, at); });
-  };
-  fetch(R::first());
   for (uint32_t row = R::first(); row < a.rows; row += R::step()) {
     float y[R::kHeld][8];
     Loaded<TY> g[R::kHeld], u[R::kHeld];
     uint32_t largest[3] = {0, 0, 0};  // of y, gate, up
     const auto take = [&](uint32_t c, int at) {
-      if (!V) load(row, c, at);
-      g[at] = next_g[at];
-      u[at] = next_u[at];
+      g[at].from(a.gate, row, c, a.cols);
+      u[at].from(a.up, row, c, a.cols);
     };
     const auto product = [&](int at, float (&gate)[8], float (&up)[8]) {
 #pragma unroll
@@ -470,10 +462,7 @@ STQ_ROWS_KERNEL gated_kernel(const GatedArgs a) {
         y[at][i] = gate[i] * sigmoid(gate[i]) * up[i];
       }
     };
-    if (V) {
-      R::each(a.cols, take);
-      fetch(row + R::step());
-    }
+    if (V) R::each(a.cols, take);
     R::each(a.cols, [&](uint32_t c, int at) {
       if (!V) take(c, at);
       float gate[8], up[8];
@@ -501,6 +490,7 @@ STQ_ROWS_KERNEL gated_kernel(const GatedArgs a) {
       }
       store_codes(a.y, row, c, a.cols, y[at], k);
       if (!rows_saved) return;
+      if (V) take(c, at);  // again, out of the caches: held, they would cost waves also where they are not needed
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         gate[i] = g[at].at(i);
@@ -577,11 +567,11 @@ void with_kept(uint32_t type, F f) {
 }
 // Workgroups for rows that are held: as many as fit the card at once, which then go through the rows.
 template <class R>
-uint32_t groups_of(uint32_t rows, uint32_t threads, uint32_t n_cu) {
-  const uint32_t need = (rows + R::kPerGroup - 1) / R::kPerGroup, fit = n_cu * ((R::V == 1 ? 20 : 16) * 64 / threads);
+uint32_t groups_of(uint32_t rows, uint32_t threads, uint32_t n_cu, uint32_t waves = R::V == 1 ? 5 : 4) {  // of a SIMD
+  const uint32_t need = (rows + R::kPerGroup - 1) / R::kPerGroup, fit = n_cu * (waves * 256 / threads);
   return need < fit ? need : fit;
 }
-// Launch shape of the elementwise kernels: of 32 to 256 threads for a row (8 for the narrowest) those that leave the fewest without
+// Launch shape of the elementwise kernels: of 32 to 256 threads for a row (8 for the narrowest) those that leave few without
 // work; 16 workgroups on a CU, which go through the rows.
 struct FlatShape { uint32_t lg_t; dim3 grid; };
 FlatShape flat_shape(uint32_t rows, uint32_t cols, uint32_t n_cu) {
@@ -589,7 +579,7 @@ FlatShape flat_shape(uint32_t rows, uint32_t cols, uint32_t n_cu) {
   const auto whole = [&](uint32_t lg) { return (((vectors - 1) >> lg) + 1) << lg; };
   uint32_t lg = vectors <= 8 ? 3 : (vectors <= 16 ? 4 : 8);
   for (uint32_t l = 7; lg > 4 && l >= 5; --l)
-    if (whole(l) < whole(lg)) lg = l;
+    if (whole(l) * 16 < whole(lg) * 15) lg = l;
   const uint32_t x = whole(lg) >> lg, per_group = 256u >> lg, need = (rows - 1) / per_group + 1;
   const uint32_t fit = (n_cu * 16 - 1) / x + 1;
   const uint32_t y = need < fit ? need : fit;
@@ -633,7 +623,7 @@ int launch_rms_norm_grad(NormGradArgs a, uint32_t sum_type, uint32_t type, void*
 int launch_gated(const GatedArgs& a, uint32_t type, uint32_t n_cu, void* stream) {
   with_rows<true>(a.cols, [&](auto r, uint32_t threads) { with_type(type, [&](auto ty) {
     using R = decltype(r);
-    gated_kernel<ty(), R><<<groups_of<R>(a.rows, threads, n_cu), threads, 0, static_cast<hipStream_t>(stream)>>>(a);
+    gated_kernel<ty(), R><<<groups_of<R>(a.rows, threads, n_cu, kGatedWaves<R>), threads, 0, static_cast<hipStream_t>(stream)>>>(a);
   }); });
   return hipGetLastError();
 }
