@@ -18,20 +18,29 @@ typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 #define STQ_LDS __attribute__((address_space(3)))
 
-// N elements of a row from element c on; those at or beyond `end` are zeros and are not read (nor any, of a row that is not there).
-template <int N, class T>
-struct Vec { T e[N]; };
-template <int N, class T>
-__device__ __forceinline__ Vec<N, T> load_vec(const T* row, uint32_t c, uint32_t end, bool there) {
-  Vec<N, T> r;
-  const STQ_GLOBAL T* p = as_global(row) + c;
-  if (there && c + N <= end) {
-    __builtin_memcpy(&r, p, sizeof(r));
-  } else {
+__device__ __forceinline__ v4i load_fragment(const int8_t* p) {
+  v4i v;
+  __builtin_memcpy(&v, as_global(p), 16);
+  return v;
+}
+// 16 codes of which only the first `valid` (any number) are wanted, zeros in place of the others, at offset `at` of a matrix of `total`
+// (16 at least): what would lie beyond its end is not read, but 16 that end there, moved into place.
+__device__ __forceinline__ v4i load_last(const int8_t* p, int64_t at, int64_t total, int32_t valid) {
+  const int64_t from = min(at, total - 16);
+  v4i v = load_fragment(p + from);
+  if (valid >= 16 && from == at) return v;
+  const int32_t far = valid > 0 ? static_cast<int32_t>(at - from) : 0;  // (what is wanted is there: below 16)
+  for (int32_t k = 0; k < far; ++k) {
 #pragma unroll
-    for (uint32_t i = 0; i < N; ++i) r.e[i] = there && c + i < end ? p[i] : static_cast<T>(0);
+    for (int i = 0; i < 3; ++i) v[i] = __builtin_amdgcn_alignbit(v[i + 1], v[i], 8);
+    v[3] = static_cast<int>(static_cast<uint32_t>(v[3]) >> 8);
   }
-  return r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int32_t n = valid - 4 * i;
+    v[i] &= n >= 4 ? -1 : (n <= 0 ? 0 : (1 << (8 * n)) - 1);
+  }
+  return v;
 }
 
 // What a lane has of a wave's result at a time is four neighbouring columns of one row; 16 bytes of a row, as an output has them.
@@ -120,48 +129,74 @@ __device__ __forceinline__ TileAt tile_at(uint32_t id, uint32_t rows, uint32_t c
 // straight into LDS, into one of two buffers while the other is worked on.  A row is 128 bytes there, eight pieces of 16, which lie at
 // the places that their number and the row's give by exclusive or, so that the reads of a fragment meet every bank once.
 // Rows beyond the matrix' end repeat its last one; a step that goes beyond the rows' end comes through registers, with zeros there.
+// PIECES: whether the rows lie in 16-byte pieces; others come through registers altogether, loaded a step ahead.
 constexpr uint32_t kStepK = 128;
 
-template <uint32_t TO, int TM, int TN, int WM, int WN>
+template <uint32_t TO, int TM, int TN, int WM, int WN, bool PIECES>
 __global__ __launch_bounds__(WM * WN * 64) void matmul_tile_kernel(const MatmulArgs a, uint32_t tiles_m, uint32_t tiles_n) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host's compiler has no buffer descriptors)
   constexpr uint32_t FM = TM / WM / 32, FN = TN / WN / 32;  // fragments of 32 of a wave
   constexpr uint32_t kAtOnce = WM * WN * 8;                 // rows that a load of all waves fills
+  constexpr uint32_t VA = TM / kAtOnce, VB = TN / kAtOnce;
   __shared__ __align__(1024) int8_t a0[TM * kStepK], b0[TN * kStepK], a1[TM * kStepK], b1[TN * kStepK];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const TileAt at = tile_at(blockIdx.x, tiles_m, tiles_n);
   const uint32_t m0 = at.row * TM, n0 = at.col * TN;
   int8_t* const pa = static_cast<int8_t*>(a.a.p) + m0 * a.a.stride;
   int8_t* const pb = static_cast<int8_t*>(a.b.p) + n0 * a.b.stride;
+  const int64_t total_a = static_cast<int64_t>((a.m - 1 - m0) * a.a.stride + a.k), total_b = static_cast<int64_t>((a.n - 1 - n0) * a.b.stride + a.k);
   const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(pa, 0, 0x7FFFFFFF, 0x00020000);
   const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(pb, 0, 0x7FFFFFFF, 0x00020000);
   // load i of a wave fills rows kAtOnce i + 8 wave .. + 7 of LDS, in lane order
-  const uint32_t load_row = wave * 8 + (lane >> 3), piece = ((lane & 7) ^ (load_row >> 1)) & 7;
-  uint32_t oa[TM / kAtOnce], ob[TN / kAtOnce];
+  const uint32_t load_row = wave * 8 + (lane >> 3), piece = ((lane & 7) ^ (load_row >> 1)) & 7, to = load_row * kStepK + (lane & 7) * 16;
+  uint32_t oa[VA], ob[VB];
 #pragma unroll
-  for (uint32_t i = 0; i < TM / kAtOnce; ++i) oa[i] = min(load_row + kAtOnce * i, a.m - 1 - m0) * static_cast<uint32_t>(a.a.stride) + piece * 16;
+  for (uint32_t i = 0; i < VA; ++i) oa[i] = min(load_row + kAtOnce * i, a.m - 1 - m0) * static_cast<uint32_t>(a.a.stride) + piece * 16;
 #pragma unroll
-  for (uint32_t i = 0; i < TN / kAtOnce; ++i) ob[i] = min(load_row + kAtOnce * i, a.n - 1 - n0) * static_cast<uint32_t>(a.b.stride) + piece * 16;
+  for (uint32_t i = 0; i < VB; ++i) ob[i] = min(load_row + kAtOnce * i, a.n - 1 - n0) * static_cast<uint32_t>(a.b.stride) + piece * 16;
   const uint32_t both_end = (a.k + 2 * kStepK - 1) / (2 * kStepK) * (2 * kStepK);  // of the steps, taken two at a time
-  const auto load = [&](uint32_t k, int8_t* la, int8_t* lb) {
+  const auto load_pieces = [&](uint32_t k, int8_t* la, int8_t* lb) {
     if (k + kStepK <= a.k) {
 #pragma unroll
-      for (uint32_t i = 0; i < TM / kAtOnce; ++i)
+      for (uint32_t i = 0; i < VA; ++i)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (STQ_LDS void*)(la + (i * kAtOnce + wave * 8) * kStepK), 16, oa[i], k, 0, 0);
 #pragma unroll
-      for (uint32_t i = 0; i < TN / kAtOnce; ++i)
+      for (uint32_t i = 0; i < VB; ++i)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (STQ_LDS void*)(lb + (i * kAtOnce + wave * 8) * kStepK), 16, ob[i], k, 0, 0);
     } else if (k < both_end) {
-      const auto rest = [&](const int8_t* p, uint64_t stride, uint32_t last, int8_t* to, uint32_t rows) {
+      const int32_t valid = static_cast<int32_t>(a.k) - static_cast<int32_t>(k + piece * 16);
 #pragma unroll 1
-        for (uint32_t r = load_row; r < rows; r += kAtOnce) {
-          const Vec<16, int8_t> v = load_vec<16>(p + min(r, last) * stride, k + piece * 16, a.k, true);
-          __builtin_memcpy(to + r * kStepK + (lane & 7) * 16, &v, 16);
-        }
-      };
-      rest(pa, a.a.stride, a.m - 1 - m0, la, TM);
-      rest(pb, a.b.stride, a.n - 1 - n0, lb, TN);
+      for (uint32_t i = 0; i < TM / kAtOnce; ++i) {
+        const v4i v = load_last(pa, static_cast<int64_t>(min(load_row + kAtOnce * i, a.m - 1 - m0)) * a.a.stride + k + piece * 16, total_a, valid);
+        __builtin_memcpy(la + to + i * kAtOnce * kStepK, &v, 16);
+      }
+#pragma unroll 1
+      for (uint32_t i = 0; i < TN / kAtOnce; ++i) {
+        const v4i v = load_last(pb, static_cast<int64_t>(min(load_row + kAtOnce * i, a.n - 1 - n0)) * a.b.stride + k + piece * 16, total_b, valid);
+        __builtin_memcpy(lb + to + i * kAtOnce * kStepK, &v, 16);
+      }
     }
+  };
+  v4i va[PIECES ? 1 : VA], vb[PIECES ? 1 : VB];
+  const auto load_any = [&](uint32_t k) {
+    if (k + kStepK <= a.k) {
+#pragma unroll
+      for (uint32_t i = 0; i < VA; ++i) va[i] = load_fragment(pa + k + oa[i]);
+#pragma unroll
+      for (uint32_t i = 0; i < VB; ++i) vb[i] = load_fragment(pb + k + ob[i]);
+    } else if (k < both_end) {
+      const int32_t valid = static_cast<int32_t>(a.k) - static_cast<int32_t>(k + piece * 16);
+#pragma unroll
+      for (uint32_t i = 0; i < VA; ++i) va[i] = load_last(pa, static_cast<int64_t>(oa[i]) + k, total_a, valid);
+#pragma unroll
+      for (uint32_t i = 0; i < VB; ++i) vb[i] = load_last(pb, static_cast<int64_t>(ob[i]) + k, total_b, valid);
+    }
+  };
+  const auto put_any = [&](int8_t* la, int8_t* lb) {
+#pragma unroll
+    for (uint32_t i = 0; i < VA; ++i) __builtin_memcpy(la + to + i * kAtOnce * kStepK, &va[i], 16);
+#pragma unroll
+    for (uint32_t i = 0; i < VB; ++i) __builtin_memcpy(lb + to + i * kAtOnce * kStepK, &vb[i], 16);
   };
   v16i acc[FM][FN] = {};
   const uint32_t wm = wave / WN * (TM / WM), wn = wave % WN * (TN / WN);
@@ -178,24 +213,34 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul_tile_kernel(const MatmulA
 #pragma unroll
     for (uint32_t j = 0; j < FN; ++j) fb[s & 1][j] = *reinterpret_cast<const v4i*>(lb + at_piece(wn + j * 32 + r, s));
   };
-  const auto work = [&](uint32_t k, int8_t* la, int8_t* lb, const int8_t* na, const int8_t* nb) {
+  const auto work = [&](uint32_t k, int8_t* la, int8_t* lb, int8_t* na, int8_t* nb) {
 #pragma unroll
     for (uint32_t u = 0; u < kUnits; ++u) {
       if (u == kUnits - kAhead) {
         __syncthreads();
-        load(k + 2 * kStepK, la, lb);
+        if (PIECES) load_pieces(k + 2 * kStepK, la, lb);
       }
 #pragma unroll
       for (uint32_t j = 0; j < FN; ++j)
         acc[u % FM][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[u / FM & 1][j], fa[u % kAhead], acc[u % FM][j], 0, 0, 0);
       if (u + kAhead < kUnits) read(u + kAhead, la, lb);
       else read(u + kAhead - kUnits, na, nb);
+      if (!PIECES && u == 0) {
+        put_any(na, nb);
+        load_any(k + 2 * kStepK);
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  load(0, a0, b0);
+  if (PIECES) {
+    load_pieces(0, a0, b0);
+  } else {
+    load_any(0);
+    put_any(a0, b0);
+    load_any(kStepK);
+  }
   __syncthreads();
-  load(kStepK, a1, b1);
+  if (PIECES) load_pieces(kStepK, a1, b1);
 #pragma unroll
   for (uint32_t u = 0; u < kAhead; ++u) read(u, a0, b0);
   // Two steps at a time, of which the second may lie beyond the rows' end and be one of zeros: with one way out of the loop the sums
@@ -220,129 +265,94 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul_tile_kernel(const MatmulA
 #endif
 }
 
-// The same for operands of any alignment and inner size, through registers: 128 x 128 of the result, 64 codes at a time.
-constexpr uint32_t kAnyM = 128, kAnyN = 128, kAnyK = 64, kAnyRow = kAnyK + 16;
-
-template <uint32_t TO>
-__global__ __launch_bounds__(256) void matmul_any_kernel(const MatmulArgs a, uint32_t tiles_m, uint32_t tiles_n) {
-  __shared__ __align__(16) int8_t sa[kAnyM * kAnyRow], sb[kAnyN * kAnyRow];
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const TileAt at = tile_at(blockIdx.x, tiles_m, tiles_n);
-  const uint32_t m0 = at.row * kAnyM, n0 = at.col * kAnyN;
-  const uint32_t row = threadIdx.x >> 2, col = (threadIdx.x & 3) * 16;  // of a thread's two vectors of either tile, 64 rows apart
-  const int8_t* pa = static_cast<const int8_t*>(a.a.p);
-  const int8_t* pb = static_cast<const int8_t*>(a.b.p);
-  Vec<16, int8_t> va[2], vb[2];
-  auto load = [&](uint32_t k) {
-#pragma unroll
-    for (uint32_t h = 0; h < 2; ++h) {
-      const uint32_t m = m0 + row + 64 * h, n = n0 + row + 64 * h;
-      va[h] = load_vec<16>(pa + m * a.a.stride, k + col, a.k, m < a.m);
-      vb[h] = load_vec<16>(pb + n * a.b.stride, k + col, a.k, n < a.n);
-    }
-  };
-  v4i acc[4][4] = {};
-  const uint32_t wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
-  load(0);
-  for (uint32_t k = 0; k < a.k; k += kAnyK) {
-    __syncthreads();
-#pragma unroll
-    for (uint32_t h = 0; h < 2; ++h) {
-      __builtin_memcpy(sa + (row + 64 * h) * kAnyRow + col, &va[h], 16);
-      __builtin_memcpy(sb + (row + 64 * h) * kAnyRow + col, &vb[h], 16);
-    }
-    __syncthreads();
-    if (k + kAnyK < a.k) load(k + kAnyK);
-    v4i fa[4], fb[4];
-#pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) {
-      fa[i] = *reinterpret_cast<const v4i*>(sa + (wm + i * 16 + (lane & 15)) * kAnyRow + (lane >> 4) * 16);
-      fb[i] = *reinterpret_cast<const v4i*>(sb + (wn + i * 16 + (lane & 15)) * kAnyRow + (lane >> 4) * 16);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
-  }
-#pragma unroll
-  for (uint32_t i = 0; i < 4; ++i) {
-    const uint32_t m = m0 + wm + i * 16 + (lane & 15);
-    const float s = as_global(a.a.s)[min(m, a.m - 1)];
-#pragma unroll
-    for (uint32_t j = 0; j < 4; ++j) {
-      const uint32_t n = n0 + wn + j * 16 + (lane >> 4) * 4;
-      float v[4];
-#pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) v[e] = static_cast<float>(acc[i][j][e]) * s * as_global(a.b.s)[min(n + e, a.n - 1)];
-      if (m < a.m) store4<TO>(a.out, m, n, a.n, v);
-    }
-  }
-}
-
-__device__ __forceinline__ v4i load_fragment(const int8_t* p) {
-  v4i v;
-  __builtin_memcpy(&v, as_global(p), 16);
-  return v;
-}
-
-// Few tokens: what counts is how fast w's codes arrive.  A workgroup has 16 of w's rows and up to 16 G tokens; its eight waves share
-// the inner dimension, a run of 128 codes each in turn, read straight into the fragments, and add up at the end.
-template <uint32_t TO, int G>
+// Few tokens: what counts is how fast w's codes arrive.  A workgroup has 16 R of w's rows and up to 16 G tokens; its eight waves share
+// the inner dimension, a run of 128 codes each in turn, read straight into the fragments, and add up at the end.  The loads of A runs
+// are under way together.
+template <uint32_t TO, int G, int R, int A>
 __global__ __launch_bounds__(512) void matmul_few_kernel(const MatmulArgs a) {
-  __shared__ __align__(16) v4i part[8][G][64];
+  __shared__ __align__(16) v4i part[8][G * R][64];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * G;
-  const uint32_t row = lane & 15, piece = (lane >> 4) * 16;
-  const int8_t* pw = static_cast<const int8_t*>(a.b.p) + min(n0 + row, a.n - 1) * a.b.stride;
-  const int8_t* px[G];
+  const uint32_t n0 = blockIdx.x * 16 * R, row = lane & 15, piece = (lane >> 4) * 16;
+  const int8_t* const px = static_cast<const int8_t*>(a.a.p);
+  const int8_t* const pw = static_cast<const int8_t*>(a.b.p);
+  uint64_t ox[G], ow[R];
 #pragma unroll
-  for (uint32_t g = 0; g < G; ++g) px[g] = static_cast<const int8_t*>(a.a.p) + min(m0 + g * 16 + row, a.m - 1) * a.a.stride;
-  v4i acc[G] = {};
-  uint32_t k = wave * 128 + piece;
-  constexpr uint32_t kAhead = 4;  // runs whose loads are under way together
-  for (; (k & ~127u) + (kAhead - 1) * 1024 + 128 <= a.k; k += kAhead * 1024) {
-    v4i fw[2 * kAhead], fx[G][2 * kAhead];
+  for (uint32_t g = 0; g < G; ++g) ox[g] = min(g * 16 + row, a.m - 1) * a.a.stride + piece;
 #pragma unroll
-    for (uint32_t h = 0; h < 2 * kAhead; ++h) {
-      const uint32_t c = k + (h >> 1) * 1024 + (h & 1) * 64;
-      fw[h] = load_fragment(pw + c);
+  for (uint32_t r = 0; r < R; ++r) ow[r] = min(n0 + r * 16 + row, a.n - 1) * a.b.stride + piece;
+  v4i acc[R][G] = {};
+  for (uint32_t k0 = wave * 128; k0 < a.k; k0 += A * 1024) {
+    v4i fw[A][2][R], fx[A][2][G];
 #pragma unroll
-      for (uint32_t g = 0; g < G; ++g) fx[g][h] = load_fragment(px[g] + c);
-    }
+    for (uint32_t t = 0; t < A; ++t) {
+      const uint32_t k = k0 + t * 1024;
+      if (k + 128 > a.k) break;
 #pragma unroll
-    for (uint32_t h = 0; h < 2 * kAhead; ++h)
+      for (uint32_t h = 0; h < 2; ++h) {
 #pragma unroll
-      for (uint32_t g = 0; g < G; ++g) acc[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[h], fx[g][h], acc[g], 0, 0, 0);
-  }
-  for (; (k & ~127u) < a.k; k += 1024) {
+        for (uint32_t r = 0; r < R; ++r) fw[t][h][r] = load_fragment(pw + ow[r] + k + h * 64);
 #pragma unroll
-    for (uint32_t h = 0; h < 2; ++h) {
-      const Vec<16, int8_t> w = load_vec<16>(pw, k + h * 64, a.k, true);
-      v4i fw;
-      __builtin_memcpy(&fw, &w, 16);
-#pragma unroll
-      for (uint32_t g = 0; g < G; ++g) {
-        const Vec<16, int8_t> x = load_vec<16>(px[g], k + h * 64, a.k, true);
-        v4i fx;
-        __builtin_memcpy(&fx, &x, 16);
-        acc[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw, fx, acc[g], 0, 0, 0);
+        for (uint32_t g = 0; g < G; ++g) fx[t][h][g] = load_fragment(px + ox[g] + k + h * 64);
       }
     }
+#pragma unroll
+    for (uint32_t t = 0; t < A; ++t) {
+      if (k0 + t * 1024 + 128 > a.k) break;
+#pragma unroll
+      for (uint32_t h = 0; h < 2; ++h)
+#pragma unroll
+        for (uint32_t r = 0; r < R; ++r)
+#pragma unroll
+          for (uint32_t g = 0; g < G; ++g) acc[r][g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[t][h][r], fx[t][h][g], acc[r][g], 0, 0, 0);
+    }
+  }
+  if (const uint32_t k = a.k & ~127u; k < a.k && k / 128 % 8 == wave) {  // a run that is no whole one
+    const int64_t total_x = static_cast<int64_t>((a.m - 1) * a.a.stride + a.k), total_w = static_cast<int64_t>((a.n - 1) * a.b.stride + a.k);
+#pragma unroll
+    for (uint32_t h = 0; h < 2; ++h) {
+      const int32_t valid = static_cast<int32_t>(a.k) - static_cast<int32_t>(k + h * 64 + piece);
+      v4i fw[R], fx[G];
+#pragma unroll
+      for (uint32_t r = 0; r < R; ++r) fw[r] = load_last(pw, ow[r] + k + h * 64, total_w, valid);
+#pragma unroll
+      for (uint32_t g = 0; g < G; ++g) fx[g] = load_last(px, ox[g] + k + h * 64, total_x, valid);
+#pragma unroll
+      for (uint32_t r = 0; r < R; ++r)
+#pragma unroll
+        for (uint32_t g = 0; g < G; ++g) acc[r][g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[r], fx[g], acc[r][g], 0, 0, 0);
+    }
   }
 #pragma unroll
-  for (uint32_t g = 0; g < G; ++g) part[wave][g][lane] = acc[g];
+  for (uint32_t r = 0; r < R; ++r)
+#pragma unroll
+    for (uint32_t g = 0; g < G; ++g) part[wave][r * G + g][lane] = acc[r][g];
   __syncthreads();
-  if (wave >= G) return;
+  if (wave >= G * R) return;
   v4i sum = part[0][wave][lane];
 #pragma unroll
   for (uint32_t w = 1; w < 8; ++w) sum += part[w][wave][lane];
-  const uint32_t m = m0 + wave * 16 + row, n = n0 + (lane >> 4) * 4;
+  const uint32_t m = wave % G * 16 + row, n = n0 + wave / G * 16 + (lane >> 4) * 4;
   if (m >= a.m) return;
   const float s = as_global(a.a.s)[m];
   float v[4];
 #pragma unroll
   for (uint32_t e = 0; e < 4; ++e) v[e] = static_cast<float>(sum[e]) * s * as_global(a.b.s)[min(n + e, a.n - 1)];
   store4<TO>(a.out, m, n, a.n, v);
+}
+
+// Operands of fewer than 16 codes, or of rows too far apart for the offsets of a tile: an element to a thread.
+template <uint32_t TO>
+__global__ __launch_bounds__(256) void matmul_each_kernel(const MatmulArgs a) {
+  const uint64_t total = static_cast<uint64_t>(a.m) * a.n;
+  for (uint64_t t = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; t < total; t += static_cast<uint64_t>(gridDim.x) * 256) {
+    const uint64_t m = t / a.n, n = t % a.n;
+    const STQ_GLOBAL int8_t* x = as_global(static_cast<const int8_t*>(a.a.p)) + m * a.a.stride;
+    const STQ_GLOBAL int8_t* w = as_global(static_cast<const int8_t*>(a.b.p)) + n * a.b.stride;
+    int32_t sum = 0;
+    for (uint32_t k = 0; k < a.k; ++k) sum += x[k] * w[k];
+    using T = typename Elem<TO>::type;
+    as_global(static_cast<T*>(a.out.p))[m * a.out.stride + n] = static_cast<T>(static_cast<float>(sum) * as_global(a.a.s)[m] * as_global(a.b.s)[n]);
+  }
 }
 
 // ---------------------------------------------------------------------------------------------- gradients
@@ -383,20 +393,9 @@ struct GradShape {
   float* partial;           // [splits][ni][nj] where there are several
 };
 
-// Elements x .. x+7 of a row of `size`; what lies beyond its end is anything that the row holds (it meets zeros, or results that are
-// not stored).
-template <class T>
-__device__ __forceinline__ Packed<T> load_each(const T* row, uint32_t x, uint32_t size) {
-  T e[8];
-#pragma unroll
-  for (uint32_t i = 0; i < 8; ++i) e[i] = as_global(row)[min(x + i, size - 1)];
-  Packed<T> r;
-  __builtin_memcpy(&r, e, sizeof(r));
-  return r;
-}
-
-// EIGHTS: the sizes along the operands' rows are multiples of eight, so that a vector is there or is not, and a tile's offsets fit 32
-// bits.
+// Rows along i and j have eight elements at least, and a tile's offsets fit 32 bits.  What a vector has beyond its row's end is whatever
+// comes next in the matrix: it meets zeros, or results that are not stored.  Beyond the matrix' end nothing is read: the vector is then
+// one that ends there, moved into place.  EIGHTS: sizes along the rows are multiples of eight, so that there are no such vectors.
 template <bool WEIGHT, bool EIGHTS, uint32_t TY, uint32_t TO, int TI, int TJ, int WI, int WJ, int STEP>
 __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, const GradShape g) {
   constexpr uint32_t kThreads = WI * WJ * 64, FI = TI / WI / 32, FJ = TJ / WJ / 32, T = kTerms<TO>;
@@ -415,26 +414,39 @@ __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, 
   constexpr uint32_t kApartB = kThreads / (TJ / 8), kApartA = WEIGHT ? kThreads / (TI / 8) : kThreads / (STEP / 8);
   const uint32_t br = threadIdx.x / (TJ / 8), bc = threadIdx.x % (TJ / 8) * 8;
   const uint32_t ar = threadIdx.x / (WEIGHT ? TI / 8 : STEP / 8), ac = threadIdx.x % (WEIGHT ? TI / 8 : STEP / 8) * 8;
-  // EIGHTS: offsets of the vectors and scales from the start of a step, [1]: of the last one, where rows (or, along c, vectors) that
-  // are not there repeat the last that is
-  uint32_t oa[2][VA], ob[2][VB], os[2][WEIGHT ? VA : 1];
-  if (EIGHTS) {
+  // Offsets of the vectors and scales from the start of a step, [1]: of the last one, where rows (or, along c, vectors) that are not
+  // there repeat others.  far: by how many elements a vector of the last step ends too early, four bits for each piece.
+  int32_t oa[2][VA], ob[2][VB], os[2][WEIGHT ? VA : 1];
+  uint32_t far = 0;
 #pragma unroll
-    for (uint32_t l = 0; l < 2; ++l) {
-      const uint32_t rows = l ? end - 1 - last : STEP - 1;
+  for (uint32_t l = 0; l < 2; ++l) {
+    const uint32_t rows = l ? end - 1 - last : STEP - 1;
+    const auto in_matrix = [&](int32_t& o, uint64_t rest, uint32_t p) {  // rest: elements of the matrix from the step's start on
+      const int32_t most = static_cast<int32_t>(min(rest, static_cast<uint64_t>(0x7FFFFFFF))) - 8;
+      if (EIGHTS || !l || o <= most) return;
+      far |= static_cast<uint32_t>(o - most) << (4 * p);
+      o = most;
+    };
 #pragma unroll
-      for (uint32_t h = 0; h < VB; ++h) ob[l][h] = min(br + kApartB * h, rows) * static_cast<uint32_t>(a.b.stride) + min(j0 + bc, g.nj - 8);
+    for (uint32_t h = 0; h < VB; ++h) {
+      ob[l][h] = static_cast<int32_t>(min(br + kApartB * h, rows) * static_cast<uint32_t>(a.b.stride) + (j0 + bc < g.nj ? j0 + bc : 0));
+      in_matrix(ob[l][h], (g.nc - 1 - last) * a.b.stride + g.nj, VA + h);
+    }
 #pragma unroll
-      for (uint32_t h = 0; h < VA; ++h) {
-        const uint32_t r = ar + kApartA * h;
-        if (WEIGHT) {
-          os[l][h] = min(r, rows);
-          oa[l][h] = os[l][h] * static_cast<uint32_t>(a.a.stride) + min(i0 + ac, g.ni - 8);
-        } else {
-          oa[l][h] = min(r, g.ni - 1 - i0) * static_cast<uint32_t>(a.a.stride) + min(ac, rows - 7);
-        }
+    for (uint32_t h = 0; h < VA; ++h) {
+      const uint32_t r = ar + kApartA * h;
+      if (WEIGHT) {
+        os[l][h] = static_cast<int32_t>(min(r, rows));
+        oa[l][h] = static_cast<int32_t>(min(r, rows) * static_cast<uint32_t>(a.a.stride) + (i0 + ac < g.ni ? i0 + ac : 0));
+        in_matrix(oa[l][h], (g.nc - 1 - last) * a.a.stride + g.ni, h);
+      } else {
+        oa[l][h] = static_cast<int32_t>(min(r, g.ni - 1 - i0) * static_cast<uint32_t>(a.a.stride) + (ac <= rows ? ac : 0));
+        in_matrix(oa[l][h], (g.ni - 1 - i0) * a.a.stride + (g.nc - last), h);
       }
-      if (!WEIGHT) os[l][0] = min(ac, rows - 7);
+    }
+    if (!WEIGHT) {
+      os[l][0] = static_cast<int32_t>(ac <= rows ? ac : 0);
+      in_matrix(os[l][0], g.nc - last, 7);
     }
   }
 
@@ -447,24 +459,31 @@ __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, 
     const bool l = c == last;
     if (p < VA) {
       const uint32_t h = p;
-      if (EIGHTS) va[h] = load_packed(dy + (WEIGHT ? c : i0) * a.a.stride + (WEIGHT ? 0 : c) + (l ? oa[1][h] : oa[0][h]));
-      else if (WEIGHT) va[h] = load_each(dy + min(c + ar + kApartA * h, end - 1) * a.a.stride, i0 + ac, g.ni);
-      else va[h] = load_each(dy + min(i0 + ar + kApartA * h, g.ni - 1) * a.a.stride, c + ac, end);
+      va[h] = load_packed(dy + (WEIGHT ? c : i0) * a.a.stride + (WEIGHT ? 0 : c) + (l ? oa[1][h] : oa[0][h]));
       if (WEIGHT) {
-        vs[h] = EIGHTS ? as_global(scales + c)[l ? os[1][h] : os[0][h]] : as_global(scales)[min(c + ar + kApartA * h, end - 1)];
+        vs[h] = as_global(scales + c)[l ? os[1][h] : os[0][h]];
       } else if (h == VA - 1) {
-        const Packed<float> t = EIGHTS ? load_packed(scales + c + (l ? os[1][0] : os[0][0])) : load_each(scales, c + ac, end);
+        const Packed<float> t = load_packed(scales + c + (l ? os[1][0] : os[0][0]));
 #pragma unroll
         for (uint32_t e = 0; e < 8; ++e) vs[e] = t.at(e);
       }
     } else {
       const uint32_t h = p - VA;
-      if (EIGHTS) vb[h] = load_packed(q + c * a.b.stride + (l ? ob[1][h] : ob[0][h]));
-      else vb[h] = load_each(q + min(c + br + kApartB * h, end - 1) * a.b.stride, j0 + bc, g.nj);
+      vb[h] = load_packed(q + c * a.b.stride + (l ? ob[1][h] : ob[0][h]));
     }
   };
   // Piece p, which was loaded for step c, into LDS.  What lies beyond the sum's end is zero, whatever was read in its place.
   const auto put = [&](uint32_t c, uint32_t p, __bf16 (*ta)[kSizeA], __bf16* tb) {
+    if (!EIGHTS && c == last && far) {
+      if (p < VA) va[p].move(far >> (4 * p) & 15u);
+      else vb[p - VA].move(far >> (4 * p) & 15u);
+      if (!WEIGHT && p == 0) {
+        for (uint32_t k = far >> 28; k; --k) {
+#pragma unroll
+          for (uint32_t e = 0; e < 7; ++e) vs[e] = vs[e + 1];
+        }
+      }
+    }
     if (p < VA) {
       const uint32_t h = p;
       if (WEIGHT) va[h].keep(c + ar + kApartA * h < end);
@@ -558,6 +577,31 @@ __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, 
   }
 }
 
+// Results or sums of fewer than eight along a side, or rows too far apart for the offsets of a tile: 32 columns of a row to a workgroup,
+// with eight threads for each that share c.
+template <bool WEIGHT, uint32_t TY, uint32_t TO>
+__global__ __launch_bounds__(256) void grad_each_kernel(const MatmulArgs a, const GradShape g) {
+  __shared__ float part[8][32];
+  const uint32_t j = blockIdx.x * 32 + (threadIdx.x & 31), turn = threadIdx.x >> 5;
+  const STQ_GLOBAL typename Elem<TY>::type* dy = as_global(static_cast<const typename Elem<TY>::type*>(a.a.p));
+  const STQ_GLOBAL int8_t* q = as_global(static_cast<const int8_t*>(a.b.p));
+  for (uint32_t i = blockIdx.y; i < g.ni; i += gridDim.y) {
+    float sum = 0.0f;
+    if (j < g.nj)
+      for (uint32_t c = turn; c < g.nc; c += 8)
+        sum = fmaf(static_cast<float>(dy[(WEIGHT ? c : i) * a.a.stride + (WEIGHT ? i : c)]) * as_global(a.b.s)[c], static_cast<float>(q[c * a.b.stride + j]), sum);
+    part[turn][threadIdx.x & 31] = sum;
+    __syncthreads();
+    if (turn == 0 && j < g.nj) {
+#pragma unroll
+      for (int k = 1; k < 8; ++k) sum += part[k][threadIdx.x];
+      using T = typename Elem<TO>::type;
+      as_global(static_cast<T*>(a.out.p))[i * a.out.stride + j] = static_cast<T>(sum);
+    }
+    __syncthreads();
+  }
+}
+
 // The parts of a sum that was taken in parts, in one order.
 template <uint32_t TO>
 __global__ __launch_bounds__(256) void join_kernel(const Mat out, const float* partial, uint32_t splits, uint32_t ni, uint32_t nj) {
@@ -567,9 +611,16 @@ __global__ __launch_bounds__(256) void join_kernel(const Mat out, const float* p
     const uint32_t row = static_cast<uint32_t>(t / per_row), col = static_cast<uint32_t>(t % per_row) * 4;
     float v[4] = {0, 0, 0, 0};
     for (uint32_t k = 0; k < splits; ++k) {
-      const Vec<4, float> p = load_vec<4>(partial + k * size + static_cast<uint64_t>(row) * nj, col, nj, true);
+      const float* p = partial + k * size + static_cast<uint64_t>(row) * nj + col;
+      if (col + 4 <= nj) {
+        const v4i w = load_fragment(reinterpret_cast<const int8_t*>(p));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += p.e[e];
+        for (int e = 0; e < 4; ++e) v[e] += u2f(static_cast<uint32_t>(w[e]));
+      } else {
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e)
+          if (col + e < nj) v[e] += as_global(p)[e];
+      }
     }
     store4<TO>(out, row, col, nj, v);
   }
@@ -577,48 +628,57 @@ __global__ __launch_bounds__(256) void join_kernel(const Mat out, const float* p
 
 uint32_t tiles_of(uint32_t size, uint32_t tile) { return (size - 1) / tile + 1; }
 
-// Whether a matrix' rows can be loaded straight into LDS: 16-byte pieces, a tile's rows within reach of a 31-bit offset.
-bool in_pieces(const Mat& x) { return (reinterpret_cast<uintptr_t>(x.p) & 15) == 0 && x.stride % 16 == 0 && x.stride < (1u << 22); }
+constexpr uint32_t kCus = 256;  // for sizes that must not depend on the device
+bool near(const Mat& x) { return x.stride < (1u << 22); }  // a tile's rows within reach of a 31-bit offset
+// Whether a matrix' rows can be loaded straight into LDS.
+bool in_pieces(const Mat& x) { return (reinterpret_cast<uintptr_t>(x.p) & 15) == 0 && x.stride % 16 == 0; }
 
 template <uint32_t TO>
 void run_matmul(const MatmulArgs& a, uint32_t n_cu, hipStream_t st) {
-  if (a.m <= 64) {
-    const uint32_t groups = tiles_of(a.n, 16);
-    if (a.m <= 16) matmul_few_kernel<TO, 1><<<groups, 512, 0, st>>>(a);
-    else if (a.m <= 32) matmul_few_kernel<TO, 2><<<groups, 512, 0, st>>>(a);
-    else matmul_few_kernel<TO, 4><<<groups, 512, 0, st>>>(a);
-    return;
+  const auto size = [&](uint32_t rows, const Mat& x) { return (rows - 1) * x.stride + a.k; };
+  const bool few = a.m <= 64;
+  if (size(a.m, a.a) < 16 || size(a.n, a.b) < 16 || (!few && (!near(a.a) || !near(a.b)))) {
+    const uint64_t groups = (static_cast<uint64_t>(a.m) * a.n + 255) / 256;
+    matmul_each_kernel<TO><<<static_cast<uint32_t>(groups < 65536 ? groups : 65536), 256, 0, st>>>(a);
+  } else if (few) {
+    if (a.m <= 16 && tiles_of(a.n, 16) > 2 * n_cu) matmul_few_kernel<TO, 1, 1, 2><<<tiles_of(a.n, 16), 512, 0, st>>>(a);
+    else if (a.m <= 16) matmul_few_kernel<TO, 1, 1, 4><<<tiles_of(a.n, 16), 512, 0, st>>>(a);
+    else if (a.m <= 32) matmul_few_kernel<TO, 2, 2, 2><<<tiles_of(a.n, 32), 512, 0, st>>>(a);
+    else matmul_few_kernel<TO, 4, 2, 2><<<tiles_of(a.n, 32), 512, 0, st>>>(a);
+  } else {
+    const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(a.m, t)) * tiles_of(a.n, t); };
+    const bool pieces = in_pieces(a.a) && in_pieces(a.b);
+    const uint32_t t = pieces && count(256) >= n_cu ? 256 : (count(128) >= n_cu ? 128 : 64), rows = tiles_of(a.m, t), cols = tiles_of(a.n, t);
+    if (t == 256) matmul_tile_kernel<TO, 256, 256, 2, 4, true><<<rows * cols, 512, 0, st>>>(a, rows, cols);
+    else if (t == 128 && pieces) matmul_tile_kernel<TO, 128, 128, 2, 2, true><<<rows * cols, 256, 0, st>>>(a, rows, cols);
+    else if (t == 128) matmul_tile_kernel<TO, 128, 128, 2, 2, false><<<rows * cols, 256, 0, st>>>(a, rows, cols);
+    else if (pieces) matmul_tile_kernel<TO, 64, 64, 2, 2, true><<<rows * cols, 256, 0, st>>>(a, rows, cols);
+    else matmul_tile_kernel<TO, 64, 64, 2, 2, false><<<rows * cols, 256, 0, st>>>(a, rows, cols);
   }
-  if (!in_pieces(a.a) || !in_pieces(a.b)) {
-    const uint32_t rows = tiles_of(a.m, kAnyM), cols = tiles_of(a.n, kAnyN);
-    matmul_any_kernel<TO><<<rows * cols, 256, 0, st>>>(a, rows, cols);
-    return;
-  }
-  const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(a.m, t)) * tiles_of(a.n, t); };
-  const uint32_t t = count(256) >= n_cu ? 256 : (count(128) >= n_cu ? 128 : 64), rows = tiles_of(a.m, t), cols = tiles_of(a.n, t);
-  if (t == 256) matmul_tile_kernel<TO, 256, 256, 2, 4><<<rows * cols, 512, 0, st>>>(a, rows, cols);
-  else if (t == 128) matmul_tile_kernel<TO, 128, 128, 2, 2><<<rows * cols, 256, 0, st>>>(a, rows, cols);
-  else matmul_tile_kernel<TO, 64, 64, 2, 2><<<rows * cols, 256, 0, st>>>(a, rows, cols);
 }
 
-// Parts of the tokens for a weight gradient of few tiles: as many as give every CU a workgroup, of 512 tokens at least (a part
-// costs a write and a read of the result in fp32).
-constexpr uint32_t kCus = 256, kLeastPart = 512;
+// Parts of the tokens for a weight gradient of few tiles, of 512 tokens at least.  What a number of parts takes, in units of the time of
+// a token of a tile: the tiles that a CU takes one after the other, and for several parts a write and a read of the result in fp32 and
+// another launch (measured: 169 tiles of 16384 tokens 196 us, in three parts 153; 36 of 5001 tokens in seven parts 36 us, in nine 43;
+// 256 of 4096 53 us, in two 65).
+constexpr uint32_t kLeastPart = 512;
 uint32_t splits_of(uint64_t m, uint64_t n, uint64_t k) {
-  const uint64_t tiles = ((n + 127) / 128) * ((k + 127) / 128);
-  if (tiles * 2 > kCus || m < 2 * kLeastPart) return 1;
-  const uint64_t s = kCus / tiles, most = m / kLeastPart;
-  return static_cast<uint32_t>(s < most ? s : most);
+  const auto count = [&](uint64_t t) { return ((n + t - 1) / t) * ((k + t - 1) / t); };
+  if (n < 8 || k < 8 || count(256) >= kCus) return 1;
+  const uint64_t tiles = count(128);
+  uint32_t best = 1;
+  double least = 0;
+  for (uint32_t s = 1; s == 1 || (s <= 64 && s * kLeastPart <= m); ++s) {
+    const double turns = static_cast<double>((tiles * s + kCus - 1) / kCus);
+    const double t = turns * static_cast<double>(m) / s + (s > 1 ? 200.0 + 1.1e-4 * static_cast<double>(s * n * k) : 0.0);
+    if (s == 1 || t < least) { least = t; best = s; }
+  }
+  return best;
 }
 
 template <bool WEIGHT, uint32_t TY, uint32_t TO>
-void run_grad(const MatmulArgs& a, GradShape g, uint32_t n_cu, hipStream_t st) {
+void run_grad(const MatmulArgs& a, GradShape g, hipStream_t st) {
   constexpr int kStepC = 32;
-  const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(g.ni, t)) * tiles_of(g.nj, t); };
-  const bool eights = g.nj % 8 == 0 && (WEIGHT ? g.ni : g.nc) % 8 == 0 && a.a.stride < (1u << 22) && a.b.stride < (1u << 22);
-  const uint32_t t = eights && g.splits == 1 && count(256) >= n_cu ? 256 : 128;
-  g.tiles_i = tiles_of(g.ni, t);
-  g.tiles_j = tiles_of(g.nj, t);
   const auto join = [&] {
     const uint64_t groups = (static_cast<uint64_t>(g.ni) * ((g.nj + 3) / 4) + 255) / 256;
     join_kernel<TO><<<static_cast<uint32_t>(groups < 4096 ? groups : 4096), 256, 0, st>>>(a.out, g.partial, g.splits, g.ni, g.nj);
@@ -627,23 +687,33 @@ void run_grad(const MatmulArgs& a, GradShape g, uint32_t n_cu, hipStream_t st) {
     g.splits = 0;
     return join();
   }
+  if (g.ni < 8 || g.nj < 8 || g.nc < 8 || !near(a.a) || !near(a.b)) {
+    grad_each_kernel<WEIGHT, TY, TO><<<dim3(tiles_of(g.nj, 32), g.ni < 65535 ? g.ni : 65535), 256, 0, st>>>(a, g);
+    return;
+  }
+  const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(g.ni, t)) * tiles_of(g.nj, t); };
+  const bool eights = g.nj % 8 == 0 && (WEIGHT ? g.ni : g.nc) % 8 == 0;
+  const uint32_t t = count(256) >= kCus ? 256 : 128;
+  g.tiles_i = tiles_of(g.ni, t);
+  g.tiles_j = tiles_of(g.nj, t);
   g.each = tiles_of(g.nc, g.splits * 64) * 64;
   g.splits = tiles_of(g.nc, g.each);
   const dim3 grid(g.tiles_i * g.tiles_j, g.splits);
-  if (!eights) grad_kernel<WEIGHT, false, TY, TO, 128, 128, 2, 2, kStepC><<<grid, 256, 0, st>>>(a, g);
-  else if (t == 256) grad_kernel<WEIGHT, true, TY, TO, 256, 256, 2, 4, kStepC><<<grid, 512, 0, st>>>(a, g);
-  else grad_kernel<WEIGHT, true, TY, TO, 128, 128, 2, 2, kStepC><<<grid, 256, 0, st>>>(a, g);
+  if (t == 256 && eights) grad_kernel<WEIGHT, true, TY, TO, 256, 256, 2, 4, kStepC><<<grid, 512, 0, st>>>(a, g);
+  else if (t == 256) grad_kernel<WEIGHT, false, TY, TO, 256, 256, 2, 4, kStepC><<<grid, 512, 0, st>>>(a, g);
+  else if (eights) grad_kernel<WEIGHT, true, TY, TO, 128, 128, 2, 4, kStepC><<<grid, 512, 0, st>>>(a, g);
+  else grad_kernel<WEIGHT, false, TY, TO, 128, 128, 2, 4, kStepC><<<grid, 512, 0, st>>>(a, g);
   if (g.splits > 1) join();
 }
 template <bool WEIGHT>
-int run_grads(const MatmulArgs& a, const GradShape& g, uint32_t dy_type, uint32_t out_type, uint32_t n_cu, void* stream) {
+int run_grads(const MatmulArgs& a, const GradShape& g, uint32_t dy_type, uint32_t out_type, void* stream) {
   const hipStream_t st = static_cast<hipStream_t>(stream);
   if (dy_type == kF32) {
-    if (out_type == kF32) run_grad<WEIGHT, kF32, kF32>(a, g, n_cu, st);
-    else run_grad<WEIGHT, kF32, kBF16>(a, g, n_cu, st);
+    if (out_type == kF32) run_grad<WEIGHT, kF32, kF32>(a, g, st);
+    else run_grad<WEIGHT, kF32, kBF16>(a, g, st);
   } else {
-    if (out_type == kF32) run_grad<WEIGHT, kBF16, kF32>(a, g, n_cu, st);
-    else run_grad<WEIGHT, kBF16, kBF16>(a, g, n_cu, st);
+    if (out_type == kF32) run_grad<WEIGHT, kBF16, kF32>(a, g, st);
+    else run_grad<WEIGHT, kBF16, kBF16>(a, g, st);
   }
   return hipGetLastError();
 }
@@ -655,11 +725,11 @@ int launch_matmul(const MatmulArgs& a, uint32_t out_type, uint32_t n_cu, void* s
   else run_matmul<kBF16>(a, n_cu, static_cast<hipStream_t>(stream));
   return hipGetLastError();
 }
-int launch_matmul_grad_input(const MatmulArgs& a, uint32_t dy_type, uint32_t out_type, uint32_t n_cu, void* stream) {
-  return run_grads<false>(a, GradShape{a.m, a.k, a.n, 0, 0, 1, 0, nullptr}, dy_type, out_type, n_cu, stream);
+int launch_matmul_grad_input(const MatmulArgs& a, uint32_t dy_type, uint32_t out_type, void* stream) {
+  return run_grads<false>(a, GradShape{a.m, a.k, a.n, 0, 0, 1, 0, nullptr}, dy_type, out_type, stream);
 }
-int launch_matmul_grad_weight(const MatmulArgs& a, uint32_t dy_type, uint32_t out_type, float* workspace, uint32_t n_cu, void* stream) {
-  return run_grads<true>(a, GradShape{a.n, a.k, a.m, 0, 0, splits_of(a.m, a.n, a.k), 0, workspace}, dy_type, out_type, n_cu, stream);
+int launch_matmul_grad_weight(const MatmulArgs& a, uint32_t dy_type, uint32_t out_type, float* workspace, void* stream) {
+  return run_grads<true>(a, GradShape{a.n, a.k, a.m, 0, 0, splits_of(a.m, a.n, a.k), 0, workspace}, dy_type, out_type, stream);
 }
 uint64_t grad_weight_bytes(uint64_t m, uint64_t n, uint64_t k) {
   const uint64_t s = splits_of(m, n, k);

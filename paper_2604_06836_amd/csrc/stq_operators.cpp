@@ -224,7 +224,7 @@ int stq_matmul_grad_input(stq_ctx* ctx, const stq_matrix* dy, const stq_matrix* 
   if (!a.m) return STQ_OK;
   DeviceGuard g(ctx->device);
   if (!g.ok) return STQ_EHIP;
-  return launched(launch_matmul_grad_input(a, dy->dtype, dx->dtype, ctx->n_cu, stream));
+  return launched(launch_matmul_grad_input(a, dy->dtype, dx->dtype, stream));
 }
 
 int stq_matmul_grad_weight_bytes(uint64_t tokens, uint64_t outputs, uint64_t inputs, uint64_t* bytes) {
@@ -254,7 +254,7 @@ int stq_matmul_grad_weight(stq_ctx* ctx, const stq_matrix* dy, const stq_matrix*
   a.k = static_cast<uint32_t>(x->cols);
   DeviceGuard g(ctx->device);
   if (!g.ok) return STQ_EHIP;
-  return launched(launch_matmul_grad_weight(a, dy->dtype, dw->dtype, need ? static_cast<float*>(workspace) : nullptr, ctx->n_cu, stream));
+  return launched(launch_matmul_grad_weight(a, dy->dtype, dw->dtype, need ? static_cast<float*>(workspace) : nullptr, stream));
 }
 
 }  // extern "C"

@@ -63,8 +63,8 @@ int launch_rms_norm_grad(NormGradArgs a, uint32_t sum_type, uint32_t type, void*
 int launch_gated(const GatedArgs& a, uint32_t type, uint32_t n_cu, void* stream);
 int launch_gated_grad(const GatedGradArgs& a, uint32_t kept_type, uint32_t type, uint32_t n_cu, void* stream);
 int launch_matmul(const MatmulArgs& a, uint32_t out_type, uint32_t n_cu, void* stream);
-int launch_matmul_grad_input(const MatmulArgs& a, uint32_t dy_type, uint32_t out_type, uint32_t n_cu, void* stream);
-int launch_matmul_grad_weight(const MatmulArgs& a, uint32_t dy_type, uint32_t out_type, float* workspace, uint32_t n_cu, void* stream);
+int launch_matmul_grad_input(const MatmulArgs& a, uint32_t dy_type, uint32_t out_type, void* stream);
+int launch_matmul_grad_weight(const MatmulArgs& a, uint32_t dy_type, uint32_t out_type, float* workspace, void* stream);
 uint64_t grad_weight_bytes(uint64_t m, uint64_t n, uint64_t k);
 
 }  // namespace stq

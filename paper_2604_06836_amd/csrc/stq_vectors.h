@@ -24,6 +24,13 @@ struct Packed {
 #pragma unroll
     for (uint32_t i = 0; i < kWords; ++i) w[i] = there ? w[i] : 0u;
   }
+  __device__ __forceinline__ void move(uint32_t by) {  // elements by, by+1 .. to the front
+    for (; by; --by) {
+#pragma unroll
+      for (uint32_t i = 0; i + 1 < kWords; ++i) w[i] = sizeof(T) == 4 ? w[i + 1] : __builtin_amdgcn_alignbit(w[i + 1], w[i], 8 * sizeof(T) % 32);
+      w[kWords - 1] = sizeof(T) == 4 ? 0u : w[kWords - 1] >> (8 * sizeof(T) % 32);
+    }
+  }
   __device__ __forceinline__ float at(uint32_t e) const {
     if constexpr (sizeof(T) == 4) return u2f(w[e]);
     else if constexpr (sizeof(T) == 2) return u2f(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);  // bf16
