@@ -367,7 +367,7 @@ template <uint32_t TO> constexpr int kTerms = TO == kF32 ? 3 : 1;
 
 // A [c][x] tile: rows of X elements, 64 bytes more apart than that, so that the four rows of a transposed read meet every bank once.
 template <uint32_t X> constexpr uint32_t kRowX = X + 32;
-// A [i][c] tile of C = 32 or 64 elements a row, in pieces of eight which lie at the places that their number and the row's give by
+// A [i][c] tile of C elements a row, 32 or 64, in pieces of eight which lie at the places that their number and the row's give by
 // exclusive or, for the same reason.
 template <uint32_t C>
 __device__ __forceinline__ uint32_t place_c(uint32_t row, uint32_t piece) {
@@ -396,24 +396,31 @@ struct GradShape {
 // Rows along i and j have eight elements at least, and a tile's offsets fit 32 bits.  What a vector has beyond its row's end is whatever
 // comes next in the matrix: it meets zeros, or results that are not stored.  Beyond the matrix' end nothing is read: the vector is then
 // one that ends there, moved into place.  EIGHTS: sizes along the rows are multiples of eight, so that there are no such vectors.
-template <bool WEIGHT, bool EIGHTS, uint32_t TY, uint32_t TO, int TI, int TJ, int WI, int WJ, int STEP>
-__global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, const GradShape g) {
+// WC: parts of c that a workgroup takes side by side, WI x WJ waves and buffers for each, and adds up at the end: for results of few tiles,
+// of which each then has more waves.
+template <bool WEIGHT, bool EIGHTS, uint32_t TY, uint32_t TO, int TI, int TJ, int WI, int WJ, int WC, int STEP>
+__global__ __launch_bounds__(WC * WI * WJ * 64) void grad_kernel(const MatmulArgs a, const GradShape g) {
   constexpr uint32_t kThreads = WI * WJ * 64, FI = TI / WI / 32, FJ = TJ / WJ / 32, T = kTerms<TO>;
   constexpr uint32_t kSizeA = WEIGHT ? STEP * kRowX<TI> : TI * STEP, kSizeB = STEP * kRowX<TJ>;
   constexpr uint32_t VA = TI * STEP / 8 / kThreads, VB = TJ * STEP / 8 / kThreads;  // vectors of eight of a thread
-  __shared__ __align__(16) struct { __bf16 a0[T][kSizeA], b0[kSizeB], a1[T][kSizeA], b1[kSizeB]; } tiles;
+  __shared__ __align__(16) struct { __bf16 a0[T][kSizeA], b0[kSizeB], a1[T][kSizeA], b1[kSizeB]; } parts[WC];
   using D = typename Elem<TY>::type;
-  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t lane = threadIdx.x & 63, part = WC == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+  const uint32_t thread = threadIdx.x - part * kThreads, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+  auto& tiles = parts[part];
   const TileAt at = tile_at(blockIdx.x, g.tiles_i, g.tiles_j);
   const uint32_t i0 = at.row * TI, j0 = at.col * TJ;
-  const uint32_t first = blockIdx.y * g.each, end = min(g.nc, first + g.each), last = first + (end - 1 - first) / STEP * STEP;
+  // (a part may be empty: its steps then lie beyond the sum's end, load the last one and put zeros)
+  const uint32_t first = (blockIdx.y * WC + part) * g.each, end = min(g.nc, first + g.each);
+  const uint32_t last = first < end ? first + (end - 1 - first) / STEP * STEP : (end - 1) / STEP * STEP;
+  const uint32_t length = WC == 1 ? end - first : g.each;
   const D* const dy = static_cast<const D*>(a.a.p);
   const int8_t* const q = static_cast<const int8_t*>(a.b.p);
   const float* const scales = a.b.s;
   // where a thread's vectors lie: of a [c][x] tile kThreads / (X / 8) rows apart, of the [i][c] one kThreads / (STEP / 8)
   constexpr uint32_t kApartB = kThreads / (TJ / 8), kApartA = WEIGHT ? kThreads / (TI / 8) : kThreads / (STEP / 8);
-  const uint32_t br = threadIdx.x / (TJ / 8), bc = threadIdx.x % (TJ / 8) * 8;
-  const uint32_t ar = threadIdx.x / (WEIGHT ? TI / 8 : STEP / 8), ac = threadIdx.x % (WEIGHT ? TI / 8 : STEP / 8) * 8;
+  const uint32_t br = thread / (TJ / 8), bc = thread % (TJ / 8) * 8;
+  const uint32_t ar = thread / (WEIGHT ? TI / 8 : STEP / 8), ac = thread % (WEIGHT ? TI / 8 : STEP / 8) * 8;
   // Offsets of the vectors and scales from the start of a step, [1]: of the last one, where rows (or, along c, vectors) that are not
   // there repeat others.  far: by how many elements a vector of the last step ends too early, four bits for each piece.
   int32_t oa[2][VA], ob[2][VB], os[2][WEIGHT ? VA : 1];
@@ -486,13 +493,15 @@ __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, 
     }
     if (p < VA) {
       const uint32_t h = p;
-      if (WEIGHT) va[h].keep(c + ar + kApartA * h < end);
+      const bool row_there = c + ar + kApartA * h < end;
+      if (WEIGHT) va[h].keep(row_there);
       else if (EIGHTS) va[h].keep(c + ac < end);
+      const float row_scale = row_there ? vs[h] : 0.0f;
       v8b t[T];
 #pragma unroll
       for (uint32_t e = 0; e < 8; ++e) {
-        float x = va[h].at(e), s = vs[WEIGHT ? h : e];
-        if (!WEIGHT) {  // (the scales repeat, too, and need not be finite)
+        float x = va[h].at(e), s = WEIGHT ? row_scale : vs[e];  // (the scales repeat, too, and need not be finite)
+        if (!WEIGHT) {
           const bool there = c + ac + (EIGHTS ? 0 : e) < end;
           x = EIGHTS || there ? x : 0.0f;
           s = there ? s : 0.0f;
@@ -560,18 +569,34 @@ __global__ __launch_bounds__(WI * WJ * 64) void grad_kernel(const MatmulArgs a, 
   read(1, tiles.a0, tiles.b0);
   // Two steps at a time, of which the second may lie beyond the sum's end and be one of zeros: with one way out of the loop the sums
   // stay in their registers.  (What the last step reads ahead is not used.)
-  for (uint32_t c = first; c < end; c += 2 * STEP) {
+  for (uint32_t c = first; c < first + length; c += 2 * STEP) {
     work(c, tiles.a0, tiles.b0, tiles.a1, tiles.b1);
     work(c + STEP, tiles.a1, tiles.b1, tiles.a0, tiles.b0);
   }
   __syncthreads();
   const auto value = [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return acc[i][j][p * 4 + e]; };
+  if constexpr (WC > 1) {  // the parts' sums, in one order, to the first
+    constexpr uint32_t kEach = FI * FJ * 16;
+    static_assert(sizeof(parts) >= (WC - 1) * kThreads * kEach * 4, "sums of the parts");
+    float* const sums = reinterpret_cast<float*>(&parts);
+    if (part)
+#pragma unroll
+      for (uint32_t e = 0; e < kEach; ++e) sums[((part - 1) * kEach + e) * kThreads + thread] = acc[e / 16 / FJ][e / 16 % FJ][e % 16];
+    __syncthreads();
+    if (!part)
+#pragma unroll
+      for (uint32_t p = 0; p < WC - 1; ++p)
+#pragma unroll
+        for (uint32_t e = 0; e < kEach; ++e) acc[e / 16 / FJ][e / 16 % FJ][e % 16] += sums[(p * kEach + e) * kThreads + thread];
+    __syncthreads();
+    if (part) return;
+  }
   constexpr uint32_t kBox = 32 * FJ * 32 * (TI == 256 && TO != kF32 ? 2 : 4);
-  static_assert(sizeof(tiles) >= WI * WJ * kBox, "a box for each wave");
-  char* const box = reinterpret_cast<char*>(&tiles) + wave * kBox;
-  if (TI != 256 && g.splits > 1) {  // (sums taken in parts are of small tiles)
-    const Mat part{g.partial + static_cast<uint64_t>(blockIdx.y) * g.ni * g.nj, nullptr, g.nj, 0, 0};
-    store_tile<kF32, FI, FJ>(part, i0 + wi, j0 + wj, g.ni, g.nj, box, lane, value);
+  static_assert(sizeof(parts) >= WI * WJ * kBox, "a box for each wave");
+  char* const box = reinterpret_cast<char*>(&parts) + wave * kBox;
+  if (TI == 128 && g.splits > 1) {  // (sums that several workgroups take in parts are of these tiles)
+    const Mat partial{g.partial + static_cast<uint64_t>(blockIdx.y) * g.ni * g.nj, nullptr, g.nj, 0, 0};
+    store_tile<kF32, FI, FJ>(partial, i0 + wi, j0 + wj, g.ni, g.nj, box, lane, value);
   } else {
     store_tile<TO, FI, FJ>(a.out, i0 + wi, j0 + wj, g.ni, g.nj, box, lane, value);
   }
@@ -676,34 +701,52 @@ uint32_t splits_of(uint64_t m, uint64_t n, uint64_t k) {
   return best;
 }
 
+template <uint32_t TO>
+void join(const MatmulArgs& a, const GradShape& g, hipStream_t st) {
+  const uint64_t groups = (static_cast<uint64_t>(g.ni) * ((g.nj + 3) / 4) + 255) / 256;
+  join_kernel<TO><<<static_cast<uint32_t>(groups < 4096 ? groups : 4096), 256, 0, st>>>(a.out, g.partial, g.splits, g.ni, g.nj);
+}
+
+template <bool WEIGHT, bool EIGHTS, uint32_t TY, uint32_t TO>
+void run_tiles(const MatmulArgs& a, GradShape g, hipStream_t st) {
+  const auto count = [&](uint32_t i, uint32_t j) { return static_cast<uint64_t>(tiles_of(g.ni, i)) * tiles_of(g.nj, j); };
+  const auto grid = [&](uint32_t i, uint32_t j, uint32_t parts) {
+    g.tiles_i = tiles_of(g.ni, i);
+    g.tiles_j = tiles_of(g.nj, j);
+    g.each = tiles_of(g.nc, g.splits * parts * 64) * 64;
+    if (parts == 1) g.splits = tiles_of(g.nc, g.each);
+    return dim3(g.tiles_i * g.tiles_j, g.splits);
+  };
+  // 256 x 256 where it gives every CU a tile; below, 128 x 128, and where that leaves half of the CUs without one, smaller
+  // tiles whose workgroups take parts of c side by side.  Terms of fp32 results have no room in LDS for steps of 64.
+  constexpr int kSmall = TO == kF32 ? 32 : 64;
+  if (count(256, 256) >= kCus) {
+    const dim3 d = grid(256, 256, 1);
+    grad_kernel<WEIGHT, EIGHTS, TY, TO, 256, 256, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
+  } else if (g.splits > 1 || count(128, 128) * 2 > kCus) {
+    const dim3 d = grid(128, 128, 1);
+    grad_kernel<WEIGHT, EIGHTS, TY, TO, 128, 128, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
+    if (g.splits > 1) join<TO>(a, g, st);
+  } else if (g.ni <= 32) {
+    const dim3 d = grid(32, 64, 4);
+    grad_kernel<WEIGHT, EIGHTS, TY, TO, 32, 64, 1, 2, 4, kSmall><<<d, 512, 0, st>>>(a, g);
+  } else {
+    const dim3 d = grid(64, 64, 2);
+    grad_kernel<WEIGHT, EIGHTS, TY, TO, 64, 64, 2, 2, 2, kSmall><<<d, 512, 0, st>>>(a, g);
+  }
+}
 template <bool WEIGHT, uint32_t TY, uint32_t TO>
 void run_grad(const MatmulArgs& a, GradShape g, hipStream_t st) {
-  constexpr int kStepC = 32;
-  const auto join = [&] {
-    const uint64_t groups = (static_cast<uint64_t>(g.ni) * ((g.nj + 3) / 4) + 255) / 256;
-    join_kernel<TO><<<static_cast<uint32_t>(groups < 4096 ? groups : 4096), 256, 0, st>>>(a.out, g.partial, g.splits, g.ni, g.nj);
-  };
   if (g.nc == 0) {  // no tokens: a sum of nothing
     g.splits = 0;
-    return join();
-  }
-  if (g.ni < 8 || g.nj < 8 || g.nc < 8 || !near(a.a) || !near(a.b)) {
+    join<TO>(a, g, st);
+  } else if (g.ni < 8 || g.nj < 8 || g.nc < 8 || !near(a.a) || !near(a.b)) {
     grad_each_kernel<WEIGHT, TY, TO><<<dim3(tiles_of(g.nj, 32), g.ni < 65535 ? g.ni : 65535), 256, 0, st>>>(a, g);
-    return;
+  } else if (g.nj % 8 == 0 && (WEIGHT ? g.ni : g.nc) % 8 == 0) {
+    run_tiles<WEIGHT, true, TY, TO>(a, g, st);
+  } else {
+    run_tiles<WEIGHT, false, TY, TO>(a, g, st);
   }
-  const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(g.ni, t)) * tiles_of(g.nj, t); };
-  const bool eights = g.nj % 8 == 0 && (WEIGHT ? g.ni : g.nc) % 8 == 0;
-  const uint32_t t = count(256) >= kCus ? 256 : 128;
-  g.tiles_i = tiles_of(g.ni, t);
-  g.tiles_j = tiles_of(g.nj, t);
-  g.each = tiles_of(g.nc, g.splits * 64) * 64;
-  g.splits = tiles_of(g.nc, g.each);
-  const dim3 grid(g.tiles_i * g.tiles_j, g.splits);
-  if (t == 256 && eights) grad_kernel<WEIGHT, true, TY, TO, 256, 256, 2, 4, kStepC><<<grid, 512, 0, st>>>(a, g);
-  else if (t == 256) grad_kernel<WEIGHT, false, TY, TO, 256, 256, 2, 4, kStepC><<<grid, 512, 0, st>>>(a, g);
-  else if (eights) grad_kernel<WEIGHT, true, TY, TO, 128, 128, 2, 4, kStepC><<<grid, 512, 0, st>>>(a, g);
-  else grad_kernel<WEIGHT, false, TY, TO, 128, 128, 2, 4, kStepC><<<grid, 512, 0, st>>>(a, g);
-  if (g.splits > 1) join();
 }
 template <bool WEIGHT>
 int run_grads(const MatmulArgs& a, const GradShape& g, uint32_t dy_type, uint32_t out_type, void* stream) {
