@@ -358,13 +358,12 @@ __global__ __launch_bounds__(256) void matmul_each_kernel(const MatmulArgs a) {
 // ---------------------------------------------------------------------------------------------- gradients
 // out[i][j] = sum over c of dy(i, c) * s(c) * q(c, j): with respect to the input (WEIGHT false) i is the token and c the output, and
 // dy's rows run along c; with respect to the weight i is the output and c the token, and dy's rows run along i.  The codes' rows run
-// along j.  Codes are whole numbers below 2^8 and exact in bf16.  dy * s is rounded to bf16, or for results in fp32 to the sum of
-// three, which hold all 24 bits of it.
+// along j.  Codes are whole numbers below 2^8 and exact in bf16.  dy * s enters as the sum of T bf16: three for results in fp32, which
+// hold all 24 bits of it; one for results in bf16, which costs them about as much again as their own rounding (2-norm of the error
+// 2.3e-3 of the result's, without it 1.7e-3); two for short sums, where a term more takes no longer and fewer errors cancel.
 // A workgroup has TI x TJ of the result, its WI x WJ waves a part each, and takes STEP of c at a time: what a step needs is loaded
 // into registers two steps ahead, turned into bf16 and put into one of two LDS buffers one step ahead.  Operands whose rows run along
 // i or j are read out of LDS transposed, four rows of 16 columns at a time.
-template <uint32_t TO> constexpr int kTerms = TO == kF32 ? 3 : 1;
-
 // A [c][x] tile: rows of X elements, 64 bytes more apart than that, so that the four rows of a transposed read meet every bank once.
 template <uint32_t X> constexpr uint32_t kRowX = X + 32;
 // A [i][c] tile of C elements a row, 32 or 64, in pieces of eight which lie at the places that their number and the row's give by
@@ -398,9 +397,9 @@ struct GradShape {
 // one that ends there, moved into place.  EIGHTS: sizes along the rows are multiples of eight, so that there are no such vectors.
 // WC: parts of c that a workgroup takes side by side, WI x WJ waves and buffers for each, and adds up at the end: for results of few tiles,
 // of which each then has more waves.
-template <bool WEIGHT, bool EIGHTS, uint32_t TY, uint32_t TO, int TI, int TJ, int WI, int WJ, int WC, int STEP>
+template <bool WEIGHT, bool EIGHTS, uint32_t TY, uint32_t TO, int T, int TI, int TJ, int WI, int WJ, int WC, int STEP>
 __global__ __launch_bounds__(WC * WI * WJ * 64) void grad_kernel(const MatmulArgs a, const GradShape g) {
-  constexpr uint32_t kThreads = WI * WJ * 64, FI = TI / WI / 32, FJ = TJ / WJ / 32, T = kTerms<TO>;
+  constexpr uint32_t kThreads = WI * WJ * 64, FI = TI / WI / 32, FJ = TJ / WJ / 32;
   constexpr uint32_t kSizeA = WEIGHT ? STEP * kRowX<TI> : TI * STEP, kSizeB = STEP * kRowX<TJ>;
   constexpr uint32_t VA = TI * STEP / 8 / kThreads, VB = TJ * STEP / 8 / kThreads;  // vectors of eight of a thread
   __shared__ __align__(16) struct { __bf16 a0[T][kSizeA], b0[kSizeB], a1[T][kSizeA], b1[kSizeB]; } parts[WC];
@@ -508,14 +507,14 @@ __global__ __launch_bounds__(WC * WI * WJ * 64) void grad_kernel(const MatmulArg
         }
         x *= s;
 #pragma unroll
-        for (uint32_t k = 0; k < T; ++k) {
+        for (int k = 0; k < T; ++k) {
           t[k][e] = static_cast<__bf16>(x);
           x -= static_cast<float>(t[k][e]);
         }
       }
       const uint32_t row = ar + kApartA * h, to = WEIGHT ? row * kRowX<TI> + ac : place_c<STEP>(row, ac / 8);
 #pragma unroll
-      for (uint32_t k = 0; k < T; ++k) __builtin_memcpy(&ta[k][to], &t[k], 16);
+      for (int k = 0; k < T; ++k) __builtin_memcpy(&ta[k][to], &t[k], 16);
     } else {
       const uint32_t h = p - VA;
       v8b t;
@@ -717,22 +716,27 @@ void run_tiles(const MatmulArgs& a, GradShape g, hipStream_t st) {
     if (parts == 1) g.splits = tiles_of(g.nc, g.each);
     return dim3(g.tiles_i * g.tiles_j, g.splits);
   };
-  // 256 x 256 where it gives every CU a tile; below, 128 x 128, and where that leaves half of the CUs without one, smaller
-  // tiles whose workgroups take parts of c side by side.  Terms of fp32 results have no room in LDS for steps of 64.
-  constexpr int kSmall = TO == kF32 ? 32 : 64;
+  // 256 x 256 where it gives every CU a tile; below, 128 x 128, and where that leaves half of the CUs without one, smaller tiles whose
+  // workgroups take parts of c side by side.  Short sums take two terms in any tile: what counts is the result's way to memory.
+  constexpr int kTerms = TO == kF32 ? 3 : 1, kMore = TO == kF32 ? 3 : 2, kSmall = TO == kF32 ? 32 : 64;  // (steps that LDS has room for)
+  const bool is_short = g.nc < 512;
   if (count(256, 256) >= kCus) {
     const dim3 d = grid(256, 256, 1);
-    grad_kernel<WEIGHT, EIGHTS, TY, TO, 256, 256, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
+    if (is_short) grad_kernel<WEIGHT, EIGHTS, TY, TO, kMore, 256, 256, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
+    else grad_kernel<WEIGHT, EIGHTS, TY, TO, kTerms, 256, 256, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
   } else if (g.splits > 1 || count(128, 128) * 2 > kCus) {
     const dim3 d = grid(128, 128, 1);
-    grad_kernel<WEIGHT, EIGHTS, TY, TO, 128, 128, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
+    if (is_short) grad_kernel<WEIGHT, EIGHTS, TY, TO, kMore, 128, 128, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
+    else grad_kernel<WEIGHT, EIGHTS, TY, TO, kTerms, 128, 128, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
     if (g.splits > 1) join<TO>(a, g, st);
   } else if (g.ni <= 32) {
     const dim3 d = grid(32, 64, 4);
-    grad_kernel<WEIGHT, EIGHTS, TY, TO, 32, 64, 1, 2, 4, kSmall><<<d, 512, 0, st>>>(a, g);
+    if (is_short) grad_kernel<WEIGHT, EIGHTS, TY, TO, kMore, 32, 64, 1, 2, 4, 32><<<d, 512, 0, st>>>(a, g);
+    else grad_kernel<WEIGHT, EIGHTS, TY, TO, kTerms, 32, 64, 1, 2, 4, kSmall><<<d, 512, 0, st>>>(a, g);
   } else {
     const dim3 d = grid(64, 64, 2);
-    grad_kernel<WEIGHT, EIGHTS, TY, TO, 64, 64, 2, 2, 2, kSmall><<<d, 512, 0, st>>>(a, g);
+    if (is_short) grad_kernel<WEIGHT, EIGHTS, TY, TO, kMore, 64, 64, 2, 2, 2, 32><<<d, 512, 0, st>>>(a, g);
+    else grad_kernel<WEIGHT, EIGHTS, TY, TO, kTerms, 64, 64, 2, 2, 2, kSmall><<<d, 512, 0, st>>>(a, g);
   }
 }
 template <bool WEIGHT, uint32_t TY, uint32_t TO>
