@@ -349,8 +349,8 @@ int stq_engine_destroy(stq_engine* e);
  *
  * 8 bits (STQ_Q8): int8 codes q and fp32 scales s, value s * q.  block = 0: one scale for each row, at
  * scales[row]; block = 64, 128 or 256: one for each `block` columns of a row (the last may cover fewer), at
- * scales[row * ceil(cols / block) + col / block].  Written codes are q = rint(x * (127 / a)), s = a / 127 with
- * a = max(max|x|, 2^-100) over the scale's elements (ties to even; -127 <= q <= 127).  Where one of these
+ * scales[row * ceil(cols / block) + col / block].  Written are s = a / 127 and q = rint(x / s) with
+ * a = max(max|x|, 2^-100) over the scale's elements (both but for a few units in the last place of fp32; |q| <= 127).  Where one of these
  * elements is not finite, s is NaN and the codes are 0: everything computed from them is NaN then.
  *
  * Gradients pass through the conversion as if it were the identity; they are those of the values that the

@@ -65,12 +65,13 @@ __device__ __forceinline__ uint32_t largest8(const float (&v)[8]) {
   return a;
 }
 
-// How a group's elements become codes: q = rint(x * inv); scale = largest / 127.
+// How a group's elements become codes: scale = largest / 127, q = rint(x / scale), by the reciprocal of the scale (two divisions for each
+// block were a sixth of the gated kernel's instructions; of the largest itself the reciprocal might be too small for fp32).
 struct Coder { float inv, scale; uint32_t keep; };
 __device__ __forceinline__ Coder coder_of(uint32_t largest) {
-  const float a = fmaxf(u2f(largest), kLeast);
+  const float scale = fmaxf(u2f(largest), kLeast) * (1.0f / 127.0f);
   const bool finite = largest < kInf;
-  return {127.0f / a, finite ? a / 127.0f : __builtin_nanf(""), finite ? 0xFFFFFFFFu : 0u};
+  return {__builtin_amdgcn_rcpf(scale), finite ? scale : __builtin_nanf(""), finite ? 0xFFFFFFFFu : 0u};
 }
 // rint by the addition of 1.5 * 2^23, of the product as it is: the low byte of the sum is the code in two's complement
 __device__ __forceinline__ uint32_t code_byte(float x, float inv) { return f2u(fmaf(x, inv, 12582912.0f)); }
@@ -247,7 +248,7 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const RowsArgs a, uint3
 }
 
 // ---------------------------------------------------------------------------------------------- norm
-// One pass: with h the sum, the scale of y is rstd * max|h w| / 127 and its codes are rint(h w * (127 / max|h w|)), free of rstd, so
+// One pass: with h the sum, the scale of y is rstd * max|h w| / 127 and its codes are rint(h w / (max|h w| / 127)), free of rstd, so
 // that the sum of squares and the maxima are reduced together.
 template <uint32_t TY, class R>
 STQ_ROWS_KERNEL rms_norm_kernel(const NormArgs a) {
@@ -419,21 +420,25 @@ STQ_ROWS_KERNEL rms_norm_grad_kernel(const NormGradArgs a) {
     if (c < a.cols) store8<kF32>(to_part, 0, c, a.cols, dw[at]);
   });
 }
-// dweight[c] = the sum of the parts of column c: 32 columns a workgroup, whose 32 half waves take the parts in turn.
+// dweight[c] = the sum of the parts of column c: 16 columns a workgroup, of whose 64 threads for each a part goes to each in turn.
 __global__ __launch_bounds__(1024) void sum_parts_kernel(const float* partial, float* out, uint32_t groups, uint32_t cols) {
-  __shared__ float box[32][33];
-  const uint32_t turn = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * 32 + lane;
+  __shared__ float box[64][17];
+  const uint32_t turn = threadIdx.x >> 4, lane = threadIdx.x & 15, c = blockIdx.x * 16 + lane;
   float s = 0.0f;
   if (c < cols) {
 #pragma unroll 16
-    for (uint32_t g = turn; g < groups; g += 32) s += as_global(partial)[static_cast<uint64_t>(g) * cols + c];
+    for (uint32_t g = turn; g < groups; g += 64) s += as_global(partial)[static_cast<uint64_t>(g) * cols + c];
   }
   box[turn][lane] = s;
-  __syncthreads();
-  if (turn || c >= cols) return;
 #pragma unroll
-  for (int k = 1; k < 32; ++k) s += box[k][lane];
-  as_global(out)[c] = s;
+  for (uint32_t n = 64; n > 1; n /= 4) {  // four to one
+    __syncthreads();
+    if (turn < n / 4) {
+      s = (box[turn][lane] + box[turn + n / 4][lane]) + (box[turn + n / 2][lane] + box[turn + n / 4 * 3][lane]);
+      box[turn][lane] = s;
+    }
+  }
+  if (turn == 0 && c < cols) as_global(out)[c] = s;
 }
 
 // ---------------------------------------------------------------------------------------------- gated activation
@@ -617,7 +622,7 @@ int launch_rms_norm_grad(NormGradArgs a, uint32_t sum_type, uint32_t type, void*
     }); }); });
     if (const hipError_t e = hipGetLastError()) return e;
   }
-  sum_parts_kernel<<<(a.cols - 1) / 32 + 1, 1024, 0, st>>>(a.partial, a.dweight, groups, a.cols);
+  sum_parts_kernel<<<(a.cols - 1) / 16 + 1, 1024, 0, st>>>(a.partial, a.dweight, groups, a.cols);
   return hipGetLastError();
 }
 int launch_gated(const GatedArgs& a, uint32_t type, uint32_t n_cu, void* stream) {
