@@ -660,15 +660,21 @@ bool in_pieces(const Mat& x) { return (reinterpret_cast<uintptr_t>(x.p) & 15) ==
 template <uint32_t TO>
 void run_matmul(const MatmulArgs& a, uint32_t n_cu, hipStream_t st) {
   const auto size = [&](uint32_t rows, const Mat& x) { return (rows - 1) * x.stride + a.k; };
-  const bool few = a.m <= 64;
-  if (size(a.m, a.a) < 16 || size(a.n, a.b) < 16 || (!few && (!near(a.a) || !near(a.b)))) {
+  // Up to 32 tokens, or 64 where a tile kernel would leave half of the CUs without work (64 tokens through 4096 x 4096: 11.6 us, by
+  // tiles 16.6; through 11008 x 4096 29.5 and 17.7).
+  const bool tiles = near(a.a) && near(a.b), wide = tiles_of(a.n, 16) > 2 * n_cu;
+  const bool few = a.m <= 32 || (a.m <= 64 && (!tiles || tiles_of(a.n, 64) * 2 < n_cu));
+  if (size(a.m, a.a) < 16 || size(a.n, a.b) < 16 || (!few && !tiles)) {
     const uint64_t groups = (static_cast<uint64_t>(a.m) * a.n + 255) / 256;
     matmul_each_kernel<TO><<<static_cast<uint32_t>(groups < 65536 ? groups : 65536), 256, 0, st>>>(a);
   } else if (few) {
-    if (a.m <= 16 && tiles_of(a.n, 16) > 2 * n_cu) matmul_few_kernel<TO, 1, 1, 2><<<tiles_of(a.n, 16), 512, 0, st>>>(a);
+    // Many rows of w: fewer runs ahead, so that all workgroups fit the card (one token through 11008 x 4096 11.7 us, with four 12.6), or,
+    // with more tokens, two fragments of rows for each of tokens (32 tokens 17.7 us, with one 19.1; 4096 x 4096 10.0 and 8.4).
+    if (a.m <= 16 && wide) matmul_few_kernel<TO, 1, 1, 2><<<tiles_of(a.n, 16), 512, 0, st>>>(a);
     else if (a.m <= 16) matmul_few_kernel<TO, 1, 1, 4><<<tiles_of(a.n, 16), 512, 0, st>>>(a);
-    else if (a.m <= 32) matmul_few_kernel<TO, 2, 2, 2><<<tiles_of(a.n, 32), 512, 0, st>>>(a);
-    else matmul_few_kernel<TO, 4, 2, 2><<<tiles_of(a.n, 32), 512, 0, st>>>(a);
+    else if (a.m <= 32 && wide) matmul_few_kernel<TO, 2, 2, 2><<<tiles_of(a.n, 32), 512, 0, st>>>(a);
+    else if (a.m <= 32) matmul_few_kernel<TO, 2, 1, 2><<<tiles_of(a.n, 16), 512, 0, st>>>(a);
+    else matmul_few_kernel<TO, 4, 1, 2><<<tiles_of(a.n, 16), 512, 0, st>>>(a);
   } else {
     const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(a.m, t)) * tiles_of(a.n, t); };
     const bool pieces = in_pieces(a.a) && in_pieces(a.b);
