@@ -360,7 +360,8 @@ __global__ __launch_bounds__(256) void matmul_each_kernel(const MatmulArgs a) {
 // dy's rows run along c; with respect to the weight i is the output and c the token, and dy's rows run along i.  The codes' rows run
 // along j.  Codes are whole numbers below 2^8 and exact in bf16.  dy * s enters as the sum of T bf16: three for results in fp32, which
 // hold all 24 bits of it; one for results in bf16, which costs them about as much again as their own rounding (2-norm of the error
-// 2.3e-3 of the result's, without it 1.7e-3); two for short sums, where a term more takes no longer and fewer errors cancel.
+// 2.3e-3 of the result's, without it 1.7e-3); two for very short sums, where fewer errors cancel
+// (31 terms: 2.8e-3) and a term more costs less than elsewhere.
 // A workgroup has TI x TJ of the result, its WI x WJ waves a part each, and takes STEP of c at a time: what a step needs is loaded
 // into registers two steps ahead, turned into bf16 and put into one of two LDS buffers one step ahead.  Operands whose rows run along
 // i or j are read out of LDS transposed, four rows of 16 columns at a time.
@@ -678,7 +679,10 @@ void run_matmul(const MatmulArgs& a, uint32_t n_cu, hipStream_t st) {
   } else {
     const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(a.m, t)) * tiles_of(a.n, t); };
     const bool pieces = in_pieces(a.a) && in_pieces(a.b);
-    const uint32_t t = pieces && count(256) >= n_cu ? 256 : (count(128) >= n_cu ? 128 : 64), rows = tiles_of(a.m, t), cols = tiles_of(a.n, t);
+    // 256 x 256 from three quarters of a tile for each CU on (3008 x 4096 x 4096: 61.5 us, by 128 x 128 72; 2048 tokens 54.5 and 42.3), 128 x 128
+    // from one on (1024 x 4096 x 4096: 27.3 us, by 64 x 64 30.5; 2048 outputs 23.8 and 19.0); rows that are not in pieces by way of registers
+    // (8192 x 4096 x 4096: 137 us in pieces, 177 not).
+    const uint32_t t = pieces && count(256) * 4 >= 3 * n_cu ? 256 : (count(128) >= n_cu ? 128 : 64), rows = tiles_of(a.m, t), cols = tiles_of(a.n, t);
     if (t == 256) matmul_tile_kernel<TO, 256, 256, 2, 4, true><<<rows * cols, 512, 0, st>>>(a, rows, cols);
     else if (t == 128 && pieces) matmul_tile_kernel<TO, 128, 128, 2, 2, true><<<rows * cols, 256, 0, st>>>(a, rows, cols);
     else if (t == 128) matmul_tile_kernel<TO, 128, 128, 2, 2, false><<<rows * cols, 256, 0, st>>>(a, rows, cols);
@@ -694,7 +698,7 @@ void run_matmul(const MatmulArgs& a, uint32_t n_cu, hipStream_t st) {
 constexpr uint32_t kLeastPart = 512;
 uint32_t splits_of(uint64_t m, uint64_t n, uint64_t k) {
   const auto count = [&](uint64_t t) { return ((n + t - 1) / t) * ((k + t - 1) / t); };
-  if (n < 8 || k < 8 || count(256) >= kCus) return 1;
+  if (n < 8 || k < 8 || count(256) * 2 >= kCus) return 1;
   const uint64_t tiles = count(128);
   uint32_t best = 1;
   double least = 0;
@@ -722,11 +726,13 @@ void run_tiles(const MatmulArgs& a, GradShape g, hipStream_t st) {
     if (parts == 1) g.splits = tiles_of(g.nc, g.each);
     return dim3(g.tiles_i * g.tiles_j, g.splits);
   };
-  // 256 x 256 where it gives every CU a tile; below, 128 x 128, and where that leaves half of the CUs without one, smaller tiles whose
-  // workgroups take parts of c side by side.  Short sums take two terms in any tile: what counts is the result's way to memory.
+  // 256 x 256 where half of the CUs have a tile (dx 2048 x 4096 x 4096: 119 us, by 128 x 128 130; 8192 tokens 280 and 409), of short sums
+  // where all have (dw 2048 x 4096 over 400 tokens: 30 us and 25).  Below, 128 x 128, and where that leaves half of the CUs without one,
+  // smaller tiles whose workgroups take parts of c side by side (dx 300 x 1600 x 1600: 11.9 us, by 128 x 128 22.9; 2048 tokens 37.7 and
+  // 25.4).  Very short sums have two terms (dw 11008 x 4096 over 100 tokens: 51 us, with one 43).
   constexpr int kTerms = TO == kF32 ? 3 : 1, kMore = TO == kF32 ? 3 : 2, kSmall = TO == kF32 ? 32 : 64;  // (steps that LDS has room for)
-  const bool is_short = g.nc < 512;
-  if (count(256, 256) >= kCus) {
+  const bool is_short = g.nc < 128;
+  if (g.splits == 1 && count(256, 256) >= (g.nc < 512 ? kCus : kCus / 2)) {
     const dim3 d = grid(256, 256, 1);
     if (is_short) grad_kernel<WEIGHT, EIGHTS, TY, TO, kMore, 256, 256, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
     else grad_kernel<WEIGHT, EIGHTS, TY, TO, kTerms, 256, 256, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
