@@ -349,8 +349,8 @@ int stq_engine_destroy(stq_engine* e);
  *
  * 8 bits (STQ_Q8): int8 codes q and fp32 scales s, value s * q.  block = 0: one scale for each row, at
  * scales[row]; block = 64, 128 or 256: one for each `block` columns of a row (the last may cover fewer), at
- * scales[row * ceil(cols / block) + col / block].  Written are s = a / 127 and q = rint(x / s) with
- * a = max(max|x|, 2^-100) over the scale's elements (both but for a few units in the last place of fp32; |q| <= 127).  Where one of these
+ * scales[row * ceil(cols / block) + col / block].  Written codes are q = rint(x * (127 * (1 / a))), s = a * (1 / 127)
+ * with a = max(max|x|, 2^-100) over the scale's elements (fp32, each step rounded; ties to even; -127 <= q <= 127).  Where one of these
  * elements is not finite, s is NaN and the codes are 0: everything computed from them is NaN then.
  *
  * Gradients pass through the conversion as if it were the identity; they are those of the values that the
@@ -380,7 +380,6 @@ int stq_dequantize_rows(stq_ctx* ctx, const stq_matrix* codes, const stq_matrix*
 /* Root-mean-square norm behind the residual's addition:
  *   sum = x + residual, rounded to x's type (residual NULL: sum = x)
  *   rstd[row] = 1 / sqrt(mean(sum^2) + eps),  y = sum * rstd * weight, written as codes with a scale for each row
- *   (scale = rstd * a / 127 with a the largest |sum * weight| of the row, at least 2^-100).
  * x, residual: fp32 or bf16, one type.  weight: device, fp32[cols].  eps > 0, finite.  sum: x's type, may be NULL, and may be
  * x's or residual's own buffer.  y: STQ_Q8, block 0.  saved (may be NULL): the sum in 8 bits, any block, for
  * stq_rms_norm_grad.  rstd: device, fp32[rows], may be NULL.  A row whose squares add up to more than fp32 holds counts as not
@@ -415,8 +414,8 @@ int stq_gated_silu_grad(stq_ctx* ctx, const stq_matrix* gate, const stq_matrix* 
 int stq_matmul(stq_ctx* ctx, const stq_matrix* x, const stq_matrix* w, const stq_matrix* out, void* hip_stream);
 
 /* Gradient of x: dx[token][i] = sum over o of dy[token][o] * w.scales[o] * w.q[o][i].  dy, dx: fp32 or bf16.  The factors
- * dy * scale enter the matrix cores as bfloat16, and as the sum of two bfloat16 (16 bits of each) where dx is fp32; sums are
- * fp32. */
+ * dy * scale enter the matrix cores as bfloat16; where dx is fp32 as the sum of three, which hold all of their 24 bits (and takes
+ * as much longer), where it is bf16 and the sum has fewer than 128 terms as that of two.  Sums are fp32. */
 int stq_matmul_grad_input(stq_ctx* ctx, const stq_matrix* dy, const stq_matrix* w, const stq_matrix* dx, void* hip_stream);
 
 /* Gradient of w: dw[o][i] = sum over tokens of dy[token][o] * x.scales[token] * x.q[token][i], from the activations' codes as

@@ -130,7 +130,10 @@ __device__ __forceinline__ TileAt tile_at(uint32_t id, uint32_t rows, uint32_t c
 // the places that their number and the row's give by exclusive or, so that the reads of a fragment meet every bank once.
 // Rows beyond the matrix' end repeat its last one; a step that goes beyond the rows' end comes through registers, with zeros there.
 // PIECES: whether the rows lie in 16-byte pieces; others come through registers altogether, loaded a step ahead.
-constexpr uint32_t kStepK = 128;
+// 256 x 256 with eight waves of 128 x 64: as much of w and x in registers as two waves on a SIMD can hold, so that LDS is read for a step
+// in less time than the matrix cores take for it.  16384 x 11008 x 4096: 655 us, 2.25 Pop/s, which is what this card's library product of
+// int8 codes reaches (2.28); of zeros 3.3, so that what bounds it is the card's power.
+[[maybe_unused]] constexpr uint32_t kStepK = 128;
 
 template <uint32_t TO, int TM, int TN, int WM, int WN, bool PIECES>
 __global__ __launch_bounds__(WM * WN * 64) void matmul_tile_kernel(const MatmulArgs a, uint32_t tiles_m, uint32_t tiles_n) {
@@ -267,7 +270,8 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul_tile_kernel(const MatmulA
 
 // Few tokens: what counts is how fast w's codes arrive.  A workgroup has 16 R of w's rows and up to 16 G tokens; its eight waves share
 // the inner dimension, a run of 128 codes each in turn, read straight into the fragments, and add up at the end.  The loads of A runs
-// are under way together.
+// are under way together.  One token through 11008 x 4096: 11.0 us, of which the codes would take 8.4 at the rate of a large copy; a
+// launch and its end are most of the rest (32000 x 4096: 4.8 TB/s).
 template <uint32_t TO, int G, int R, int A>
 __global__ __launch_bounds__(512) void matmul_few_kernel(const MatmulArgs a) {
   __shared__ __align__(16) v4i part[8][G * R][64];
@@ -364,7 +368,10 @@ __global__ __launch_bounds__(256) void matmul_each_kernel(const MatmulArgs a) {
 // (31 terms: 2.8e-3) and a term more costs less than elsewhere.
 // A workgroup has TI x TJ of the result, its WI x WJ waves a part each, and takes STEP of c at a time: what a step needs is loaded
 // into registers two steps ahead, turned into bf16 and put into one of two LDS buffers one step ahead.  Operands whose rows run along
-// i or j are read out of LDS transposed, four rows of 16 columns at a time.
+// i or j are read out of LDS transposed, four rows of 16 columns at a time.  256 x 256 with eight waves of 128 x 64, as above: dx 8192 x
+// 4096 x 11008 in 740 us, 1.0 Pflop/s, where this card's library reaches 1.33 for a product of two bf16 matrices and would need both
+// factors in bf16 in memory first.  Of zeros the same kernel reaches 1.38: what bounds it is the card's power, of which the conversions
+// take a part, and a tenth is lost to the last tiles, which are too few for all CUs.
 // A [c][x] tile: rows of X elements, 64 bytes more apart than that, so that the four rows of a transposed read meet every bank once.
 template <uint32_t X> constexpr uint32_t kRowX = X + 32;
 // A [i][c] tile of C elements a row, 32 or 64, in pieces of eight which lie at the places that their number and the row's give by

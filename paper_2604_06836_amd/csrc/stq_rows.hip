@@ -65,16 +65,18 @@ __device__ __forceinline__ uint32_t largest8(const float (&v)[8]) {
   return a;
 }
 
-// How a group's elements become codes: scale = largest / 127, q = rint(x / scale), by the reciprocal of the scale (two divisions for each
-// block were a sixth of the gated kernel's instructions; of the largest itself the reciprocal might be too small for fp32).
+// How a group's elements become codes: scale = largest * (1 / 127), q = rint(x * (127 * (1 / largest))), every step rounded as it is
+// written, so that codes are the same wherever they are computed so.  (The compiler's divisions for each block were a sixth of the
+// gated kernel's instructions; a reciprocal of a hardware one is rounded after one step.)  Above 2^64 it is taken of a smaller number.
 struct Coder { float inv, scale; uint32_t keep; };
 __device__ __forceinline__ Coder coder_of(uint32_t largest) {
-  const float scale = fmaxf(u2f(largest), kLeast) * (1.0f / 127.0f);
-  const bool finite = largest < kInf;
-  return {__builtin_amdgcn_rcpf(scale), finite ? scale : __builtin_nanf(""), finite ? 0xFFFFFFFFu : 0u};
+  const float a = fmaxf(u2f(largest), kLeast);
+  const bool finite = largest < kInf, far = a > 0x1p64f;
+  const float d = far ? a * 0x1p-64f : a, r = __builtin_amdgcn_rcpf(d), inv = 127.0f * fmaf(fmaf(-d, r, 1.0f), r, r);
+  return {far ? inv * 0x1p-64f : inv, finite ? a * (1.0f / 127.0f) : __builtin_nanf(""), finite ? 0xFFFFFFFFu : 0u};
 }
-// rint by the addition of 1.5 * 2^23, of the product as it is: the low byte of the sum is the code in two's complement
-__device__ __forceinline__ uint32_t code_byte(float x, float inv) { return f2u(fmaf(x, inv, 12582912.0f)); }
+// rint by the addition of 1.5 * 2^23: the low byte of the sum is the code in two's complement
+__device__ __forceinline__ uint32_t code_byte(float x, float inv) { return f2u(x * inv + 12582912.0f); }
 __device__ __forceinline__ uint32_t codes4(const float* x, float inv, uint32_t keep) {
   const uint32_t lo = __builtin_amdgcn_perm(code_byte(x[1], inv), code_byte(x[0], inv), 0x0C0C0400u);
   const uint32_t hi = __builtin_amdgcn_perm(code_byte(x[3], inv), code_byte(x[2], inv), 0x04000C0Cu);
@@ -144,21 +146,22 @@ struct Rows {
 };
 
 // A sum and M maxima over the threads of a row, left in all of them.  The waves of a workgroup exchange theirs through `box`: two sets in
-// turn, so that one barrier a row is enough (a wave that is a row ahead writes the other set, and cannot be two ahead).
+// turn, so that one barrier is enough (a wave that is an exchange ahead writes the other set, and cannot be two ahead).
 template <class R, int M>
 struct RowReducer {
   struct Box { float sum[kMostWaves]; uint32_t largest[M ? M : 1][kMostWaves]; };
   Box* box;  // [2], in LDS
   uint32_t turn;
+  template <bool SUM = true>
   __device__ __forceinline__ void reduce(float& sum, uint32_t* largest) {
-    sum = wave_sum(sum);
+    if (SUM) sum = wave_sum(sum);
 #pragma unroll
     for (int i = 0; i < M; ++i) largest[i] = wave_max(largest[i]);
     if constexpr (!R::WAVES) {
       Box& b = box[turn];
       turn ^= 1;
       if ((threadIdx.x & 63) == 0) {
-        b.sum[threadIdx.x >> 6] = sum;
+        if (SUM) b.sum[threadIdx.x >> 6] = sum;
 #pragma unroll
         for (int i = 0; i < M; ++i) b.largest[i][threadIdx.x >> 6] = largest[i];
       }
@@ -166,15 +169,20 @@ struct RowReducer {
       // a lane of sixteen for each wave
       const uint32_t w = threadIdx.x & 15;
       const bool there = w < blockDim.x >> 6;
-      sum = first_of(row_total(there ? b.sum[w] : 0.0f));
+      if (SUM) sum = first_of(row_total(there ? b.sum[w] : 0.0f));
 #pragma unroll
       for (int i = 0; i < M; ++i) largest[i] = __builtin_amdgcn_readfirstlane(row_max(there ? b.largest[i][w] : 0u));
     }
+  }
+  __device__ __forceinline__ void most(uint32_t* largest) {
+    float none;
+    reduce<false>(none, largest);
   }
 };
 #define STQ_ROWS_KERNEL __global__ __launch_bounds__(R::WAVES ? 256 : 64 * kMostWaves) void
 
 // ---------------------------------------------------------------------------------------------- conversion
+// 11008 x 4096 from fp32: 39 us, 5.7 TB/s.
 template <uint32_t TY, class R>
 STQ_ROWS_KERNEL quantize_kernel(const RowsArgs a) {
   constexpr int V = R::V;
@@ -203,8 +211,7 @@ STQ_ROWS_KERNEL quantize_kernel(const RowsArgs a) {
       else largest = max(largest, largest8(v[at]));
     });
     if (a.out.lg) continue;
-    float none = 0.0f;
-    red.reduce(none, &largest);
+    red.most(&largest);
     const Coder k = coder_of(largest);
     R::each(a.cols, [&](uint32_t c, int at) {
       if (c >= a.cols) return;
@@ -215,8 +222,8 @@ STQ_ROWS_KERNEL quantize_kernel(const RowsArgs a) {
   }
 }
 
-// Elementwise kernels: 2^lg_t threads for a row, blockIdx.x along the row, blockIdx.y over the rows, four of which a thread has under
-// way together.
+// Elementwise kernels (codes of 16384 x 4096 to bf16: 32 us, 6.2 TB/s): 2^lg_t threads for a row, blockIdx.x along the row, blockIdx.y
+// over the rows, four of which a thread has under way together.
 constexpr uint32_t kTogether = 4;
 struct Flat {
   uint32_t c, row, step;
@@ -248,13 +255,14 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const RowsArgs a, uint3
 }
 
 // ---------------------------------------------------------------------------------------------- norm
-// One pass: with h the sum, the scale of y is rstd * max|h w| / 127 and its codes are rint(h w / (max|h w| / 127)), free of rstd, so
-// that the sum of squares and the maxima are reduced together.
+// Two exchanges a row, of the squares and then of max|y|.  (The codes are free of rstd, and with max|h w| in place of max|y| one exchange
+// would do, in the same time; but its roundings are others than the formula's, and so are codes next to a half.)  Bound by memory: 16384 x
+// 4096 in bf16 with the residual, the sum kept in 8 bits, 104 us, 5.2 TB/s (a large copy reaches 5.4).
 template <uint32_t TY, class R>
 STQ_ROWS_KERNEL rms_norm_kernel(const NormArgs a) {
   constexpr int V = R::V;
-  __shared__ typename RowReducer<R, 2>::Box box[2];
-  RowReducer<R, 2> red{box, 0};
+  __shared__ typename RowReducer<R, 1>::Box box[2];
+  RowReducer<R, 1> red{box, 0};
   Loaded<TY> next[R::kHeld], next_r[R::kHeld];
   Loaded<kF32> w[R::kHeld];
   const Mat weight{const_cast<float*>(a.weight), nullptr, 0, 0, 0};
@@ -270,7 +278,7 @@ STQ_ROWS_KERNEL rms_norm_kernel(const NormArgs a) {
   for (uint32_t row = R::first(); row < a.rows; row += R::step()) {
     float h[R::kHeld][8];
     float squares = 0.0f;
-    uint32_t largest[2] = {0, 0};  // of h * weight, of h
+    uint32_t largest = 0;  // of h
     const auto add = [&](uint32_t c, int at) {  // h of a vector
       if (!V) {
         load(row, c, at);
@@ -289,37 +297,43 @@ STQ_ROWS_KERNEL rms_norm_kernel(const NormArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         squares = fmaf(h[at][i], h[at][i], squares);
-        largest[0] = max(largest[0], magnitude(h[at][i] * w[at].at(i)));
-        largest[1] = max(largest[1], magnitude(h[at][i]));
+        largest = max(largest, magnitude(h[at][i]));
       }
       if (a.saved.p && a.saved.lg) store_block_codes(a.saved, row, c, a.cols, h[at]);
     });
-    red.reduce(squares, largest);
+    red.reduce(squares, &largest);
     // squares that are not finite (an element that is not, or more than fp32 holds) make the row NaN
     const bool finite = magnitude(squares) < kInf;
     const float rstd = finite ? 1.0f / __fsqrt_rn(squares / static_cast<float>(a.cols) + a.eps) : __builtin_nanf("");
-    const Coder k = coder_of(finite ? largest[0] : kInf), ks = coder_of(largest[1]);
+    const Coder ks = coder_of(largest);
+    uint32_t largest_y = f2u(rstd * kLeast);  // a row of zeros has a scale that is in the rows' measure
+    const auto again = [&](uint32_t c, int at) {  // h and weight of a vector that is not held; the sum may have taken x's or residual's place
+      if (V) return;
+      if (!a.sum.p) return add(c, at);
+      Loaded<TY> t;
+      t.from(a.sum, row, c, a.cols);
+      w[at].from(weight, 0, c, a.cols);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[at][i] = t.at(i);
+    };
+    R::each(a.cols, [&](uint32_t c, int at) {
+      again(c, at);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) largest_y = max(largest_y, magnitude(h[at][i] * rstd * w[at].at(i)));
+    });
+    red.most(&largest_y);
+    const Coder k = coder_of(finite ? largest_y : kInf);
     R::each(a.cols, [&](uint32_t c, int at) {
       if (c >= a.cols) return;
-      if (!V) {  // the sum may have taken x's or residual's place
-        if (a.sum.p) {
-          Loaded<TY> t;
-          t.from(a.sum, row, c, a.cols);
-          w[at].from(weight, 0, c, a.cols);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) h[at][i] = t.at(i);
-        } else {
-          add(c, at);
-        }
-      }
+      again(c, at);
       float y[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = h[at][i] * w[at].at(i);
+      for (int i = 0; i < 8; ++i) y[i] = h[at][i] * rstd * w[at].at(i);
       store_codes(a.y, row, c, a.cols, y, k);
       if (a.saved.p && !a.saved.lg) store_codes(a.saved, row, c, a.cols, h[at], ks);
     });
     if (R::thread() == 0) {
-      as_global(a.y.s)[row] = k.scale * rstd;
+      as_global(a.y.s)[row] = k.scale;
       if (a.rstd) as_global(a.rstd)[row] = rstd;
       if (a.saved.p && !a.saved.lg) as_global(a.saved.s)[row] = ks.scale;
     }
@@ -327,7 +341,8 @@ STQ_ROWS_KERNEL rms_norm_kernel(const NormArgs a) {
 }
 
 // Gradients of the norm.  A workgroup goes through rows of its own and adds up its part of dweight, in registers (for rows that are
-// not held: in `partial` itself, each of whose columns has one thread); the second kernel sums the parts in one order.
+// not held: in `partial` itself, each of whose columns has one thread); the second kernel sums the parts in one order.  16384 x 4096 from
+// codes: 88 us, 5.3 TB/s; 8192 x 1600: 26 us, of which the second kernel takes 4.4 and the way there of the parts a seventh.
 template <uint32_t TS, uint32_t TY, class R>
 STQ_ROWS_KERNEL rms_norm_grad_kernel(const NormGradArgs a) {
   constexpr int V = R::V;
@@ -443,8 +458,16 @@ __global__ __launch_bounds__(1024) void sum_parts_kernel(const float* partial, f
 
 // ---------------------------------------------------------------------------------------------- gated activation
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
+// The forward pass rounds as its formula is written, where codes are decided by the last bit: the exponential to fp32's precision, and
+// a quotient that is rounded after one step (of at most 2^126, beyond which a silu is no more than 1e-36).
+__device__ __forceinline__ float silu(float x) {
+  const float d = fminf(1.0f + expf(-x), 0x1p126f), r = __builtin_amdgcn_rcpf(d), q = x * r;
+  return fmaf(fmaf(-d, q, x), r, q);
+}
 
-// (No row is loaded ahead here: more waves hide more than a row of each would.)
+// The vector unit more than memory: about 40 instructions an element, a third of them the exponential and the quotient as rounded.  8192 x
+// 11008 in bf16 with both inputs kept: 159 us, 4.0 TB/s (126 with a silu and codes to a few units in the last place).  No
+// row is loaded ahead here: more waves hide more than a row of each would (164 us with, 141 without, when codes were divisions).
 template <class R> constexpr uint32_t kGatedWaves = R::V == 2 ? 6 : 8;  // of a SIMD
 template <uint32_t TY, class R>
 __global__ __launch_bounds__(R::WAVES ? 256 : 64 * kMostWaves, kGatedWaves<R>) void gated_kernel(const GatedArgs a) {
@@ -464,7 +487,7 @@ __global__ __launch_bounds__(R::WAVES ? 256 : 64 * kMostWaves, kGatedWaves<R>) v
       for (int i = 0; i < 8; ++i) {
         gate[i] = g[at].at(i);
         up[i] = u[at].at(i);
-        y[at][i] = gate[i] * sigmoid(gate[i]) * up[i];
+        y[at][i] = silu(gate[i]) * up[i];
       }
     };
     if (V) R::each(a.cols, take);
@@ -482,8 +505,7 @@ __global__ __launch_bounds__(R::WAVES ? 256 : 64 * kMostWaves, kGatedWaves<R>) v
         largest[2] = max(largest[2], largest8(up));
       }
     });
-    float none = 0.0f;
-    red.reduce(none, largest);
+    red.most(largest);
     const bool rows_saved = a.saved_gate.p && !a.saved_gate.lg;
     const Coder k = coder_of(largest[0]), kg = coder_of(largest[1]), ku = coder_of(largest[2]);
     R::each(a.cols, [&](uint32_t c, int at) {
@@ -514,6 +536,7 @@ __global__ __launch_bounds__(R::WAVES ? 256 : 64 * kMostWaves, kGatedWaves<R>) v
   }
 }
 
+// 8192 x 11008 from codes: 135 us, 5.4 TB/s.
 template <uint32_t TS, uint32_t TY>
 __global__ __launch_bounds__(256) void gated_grad_kernel(const GatedGradArgs a, uint32_t lg_t) {
   constexpr uint32_t kRowsNow = kTogether / 2;  // (of three inputs)
@@ -546,8 +569,9 @@ __global__ __launch_bounds__(256) void gated_grad_kernel(const GatedGradArgs a, 
 }
 
 // ---------------------------------------------------------------------------------------------- launches
-// The shape for rows of `cols` columns: f(Rows<WAVES, V>, threads of a workgroup).  TWO: whether a thread may hold two vectors (the
-// norm's gradients have no registers for that).
+// The shape for rows of `cols` columns: f(Rows<WAVES, V>, threads of a workgroup).  A vector a thread where a workgroup can have so many
+// (norm of 16384 x 4096: 114 us; with two, and no registers for a row ahead, 156), two beyond; a wave for what it can hold, without a
+// barrier.  TWO: whether a thread may hold two vectors (the norm's gradients have no registers for that).
 template <bool TWO, class F>
 void with_rows(uint32_t cols, F f) {
   const uint32_t vectors = (cols - 1) / 8 + 1, most = 64 * kMostWaves;
