@@ -737,25 +737,20 @@ void run_tiles(const MatmulArgs& a, GradShape g, hipStream_t st) {
   // where all have (dw 2048 x 4096 over 400 tokens: 30 us and 25).  Below, 128 x 128, and where that leaves half of the CUs without one,
   // smaller tiles whose workgroups take parts of c side by side (dx 300 x 1600 x 1600: 11.9 us, by 128 x 128 22.9; 2048 tokens 37.7 and
   // 25.4).  Very short sums have two terms (dw 11008 x 4096 over 100 tokens: 51 us, with one 43).
-  constexpr int kTerms = TO == kF32 ? 3 : 1, kMore = TO == kF32 ? 3 : 2, kSmall = TO == kF32 ? 32 : 64;  // (steps that LDS has room for)
-  const bool is_short = g.nc < 128;
+  constexpr int kTerms = TO == kF32 ? 3 : 2;
   if (g.splits == 1 && count(256, 256) >= (g.nc < 512 ? kCus : kCus / 2)) {
     const dim3 d = grid(256, 256, 1);
-    if (is_short) grad_kernel<WEIGHT, EIGHTS, TY, TO, kMore, 256, 256, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
-    else grad_kernel<WEIGHT, EIGHTS, TY, TO, kTerms, 256, 256, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
+    grad_kernel<WEIGHT, EIGHTS, TY, TO, kTerms, 256, 256, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
   } else if (g.splits > 1 || count(128, 128) * 2 > kCus) {
     const dim3 d = grid(128, 128, 1);
-    if (is_short) grad_kernel<WEIGHT, EIGHTS, TY, TO, kMore, 128, 128, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
-    else grad_kernel<WEIGHT, EIGHTS, TY, TO, kTerms, 128, 128, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
+    grad_kernel<WEIGHT, EIGHTS, TY, TO, kTerms, 128, 128, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
     if (g.splits > 1) join<TO>(a, g, st);
   } else if (g.ni <= 32) {
     const dim3 d = grid(32, 64, 4);
-    if (is_short) grad_kernel<WEIGHT, EIGHTS, TY, TO, kMore, 32, 64, 1, 2, 4, 32><<<d, 512, 0, st>>>(a, g);
-    else grad_kernel<WEIGHT, EIGHTS, TY, TO, kTerms, 32, 64, 1, 2, 4, kSmall><<<d, 512, 0, st>>>(a, g);
+    grad_kernel<WEIGHT, EIGHTS, TY, TO, kTerms, 32, 64, 1, 2, 4, 32><<<d, 512, 0, st>>>(a, g);
   } else {
     const dim3 d = grid(64, 64, 2);
-    if (is_short) grad_kernel<WEIGHT, EIGHTS, TY, TO, kMore, 64, 64, 2, 2, 2, 32><<<d, 512, 0, st>>>(a, g);
-    else grad_kernel<WEIGHT, EIGHTS, TY, TO, kTerms, 64, 64, 2, 2, 2, kSmall><<<d, 512, 0, st>>>(a, g);
+    grad_kernel<WEIGHT, EIGHTS, TY, TO, kTerms, 64, 64, 2, 2, 2, 32><<<d, 512, 0, st>>>(a, g);
   }
 }
 template <bool WEIGHT, uint32_t TY, uint32_t TO>
