@@ -414,8 +414,8 @@ int stq_gated_silu_grad(stq_ctx* ctx, const stq_matrix* gate, const stq_matrix* 
 int stq_matmul(stq_ctx* ctx, const stq_matrix* x, const stq_matrix* w, const stq_matrix* out, void* hip_stream);
 
 /* Gradient of x: dx[token][i] = sum over o of dy[token][o] * w.scales[o] * w.q[o][i].  dy, dx: fp32 or bf16.  The factors
- * dy * scale enter the matrix cores as bfloat16; where dx is fp32 as the sum of three, which hold all of their 24 bits (and takes
- * as much longer), where it is bf16 and the sum has fewer than 128 terms as that of two.  Sums are fp32. */
+ * dy * scale enter the matrix cores as the sum of two bfloat16, and of three, which hold all of their 24 bits (and take as much
+ * longer), where dx is fp32.  Sums are fp32. */
 int stq_matmul_grad_input(stq_ctx* ctx, const stq_matrix* dy, const stq_matrix* w, const stq_matrix* dx, void* hip_stream);
 
 /* Gradient of w: dw[o][i] = sum over tokens of dy[token][o] * x.scales[token] * x.q[token][i], from the activations' codes as

@@ -363,15 +363,14 @@ __global__ __launch_bounds__(256) void matmul_each_kernel(const MatmulArgs a) {
 // out[i][j] = sum over c of dy(i, c) * s(c) * q(c, j): with respect to the input (WEIGHT false) i is the token and c the output, and
 // dy's rows run along c; with respect to the weight i is the output and c the token, and dy's rows run along i.  The codes' rows run
 // along j.  Codes are whole numbers below 2^8 and exact in bf16.  dy * s enters as the sum of T bf16: three for results in fp32, which
-// hold all 24 bits of it; one for results in bf16, which costs them about as much again as their own rounding (2-norm of the error
-// 2.3e-3 of the result's, without it 1.7e-3); two for very short sums, where fewer errors cancel
-// (31 terms: 2.8e-3) and a term more costs less than elsewhere.
+// hold all 24 bits of it; two for results in bf16.  (One would add to them about as much again as their own rounding, 2.3e-3 for 1.7e-3
+// of the result's 2-norm, at three fifths of the time; but a small element beside large ones, of an output or token with large
+// gradients, it leaves with an error of half of the result's root mean square.)
 // A workgroup has TI x TJ of the result, its WI x WJ waves a part each, and takes STEP of c at a time: what a step needs is loaded
 // into registers two steps ahead, turned into bf16 and put into one of two LDS buffers one step ahead.  Operands whose rows run along
 // i or j are read out of LDS transposed, four rows of 16 columns at a time.  256 x 256 with eight waves of 128 x 64, as above: dx 8192 x
-// 4096 x 11008 in 740 us, 1.0 Pflop/s, where this card's library reaches 1.33 for a product of two bf16 matrices and would need both
-// factors in bf16 in memory first.  Of zeros the same kernel reaches 1.38: what bounds it is the card's power, of which the conversions
-// take a part, and a tenth is lost to the last tiles, which are too few for all CUs.
+// 4096 x 11008 in bf16 in 1295 us, 1.14 Pflop/s of the matrix cores (this card's library reaches 1.33 for a product of two bf16 matrices,
+// and would need both factors and both terms in memory first).  What bounds it is the card's power.
 // A [c][x] tile: rows of X elements, 64 bytes more apart than that, so that the four rows of a transposed read meet every bank once.
 template <uint32_t X> constexpr uint32_t kRowX = X + 32;
 // A [i][c] tile of C elements a row, 32 or 64, in pieces of eight which lie at the places that their number and the row's give by
@@ -700,8 +699,8 @@ void run_matmul(const MatmulArgs& a, uint32_t n_cu, hipStream_t st) {
 
 // Parts of the tokens for a weight gradient of few tiles, of 512 tokens at least.  What a number of parts takes, in units of the time of
 // a token of a tile: the tiles that a CU takes one after the other, and for several parts a write and a read of the result in fp32 and
-// another launch (measured: 169 tiles of 16384 tokens 196 us, in three parts 153; 36 of 5001 tokens in seven parts 36 us, in nine 43;
-// 256 of 4096 53 us, in two 65).
+// another launch (measured: 169 tiles of 16384 tokens 319 us, in three parts 249; 36 of 5001 tokens in one 43 us, in seven 29, in nine 35;
+// 256 of 4096 90 us, in two 95).
 constexpr uint32_t kLeastPart = 512;
 uint32_t splits_of(uint64_t m, uint64_t n, uint64_t k) {
   const auto count = [&](uint64_t t) { return ((n + t - 1) / t) * ((k + t - 1) / t); };
@@ -733,12 +732,12 @@ void run_tiles(const MatmulArgs& a, GradShape g, hipStream_t st) {
     if (parts == 1) g.splits = tiles_of(g.nc, g.each);
     return dim3(g.tiles_i * g.tiles_j, g.splits);
   };
-  // 256 x 256 where half of the CUs have a tile (dx 2048 x 4096 x 4096: 119 us, by 128 x 128 130; 8192 tokens 280 and 409), of short sums
-  // where all have (dw 2048 x 4096 over 400 tokens: 30 us and 25).  Below, 128 x 128, and where that leaves half of the CUs without one,
-  // smaller tiles whose workgroups take parts of c side by side (dx 300 x 1600 x 1600: 11.9 us, by 128 x 128 22.9; 2048 tokens 37.7 and
-  // 25.4).  Very short sums have two terms (dw 11008 x 4096 over 100 tokens: 51 us, with one 43).
+  // 256 x 256 where more than half of the CUs have a tile (dx 2304 x 4096 x 4096: 180 us, by 128 x 128 221; 8192 tokens 451 and 607; at
+  // half, 2048 tokens, 191 and 184), of short sums where all have (dw 2048 x 4096 over 400 tokens: 32 us and 24).  Below, 128 x 128, and
+  // where that leaves half of the CUs without one, smaller tiles whose workgroups take parts of c side by side (dx 300 x 1600 x 1600: 16.8
+  // us, by 128 x 128 31.8; 2048 tokens 49.8 and 36.5).
   constexpr int kTerms = TO == kF32 ? 3 : 2;
-  if (g.splits == 1 && count(256, 256) >= (g.nc < 512 ? kCus : kCus / 2)) {
+  if (g.splits == 1 && count(256, 256) > (g.nc < 512 ? kCus - 1 : kCus / 2)) {
     const dim3 d = grid(256, 256, 1);
     grad_kernel<WEIGHT, EIGHTS, TY, TO, kTerms, 256, 256, 2, 4, 1, 32><<<d, 512, 0, st>>>(a, g);
   } else if (g.splits > 1 || count(128, 128) * 2 > kCus) {
