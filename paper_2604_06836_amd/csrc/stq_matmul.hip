@@ -369,7 +369,7 @@ __global__ __launch_bounds__(256) void matmul_each_kernel(const MatmulArgs a) {
 // A workgroup has TI x TJ of the result, its WI x WJ waves a part each, and takes STEP of c at a time: what a step needs is loaded
 // into registers two steps ahead, turned into bf16 and put into one of two LDS buffers one step ahead.  Operands whose rows run along
 // i or j are read out of LDS transposed, four rows of 16 columns at a time.  256 x 256 with eight waves of 128 x 64, as above: dx 8192 x
-// 4096 x 11008 in bf16 in 1295 us, 1.14 Pflop/s of the matrix cores (this card's library reaches 1.33 for a product of two bf16 matrices,
+// 4096 x 11008 in bf16 in 1240 to 1295 us, 1.19 to 1.14 Pflop/s of the matrix cores (this card's library reaches 1.33 for a product of two bf16 matrices,
 // and would need both factors and both terms in memory first).  What bounds it is the card's power.
 // A [c][x] tile: rows of X elements, 64 bytes more apart than that, so that the four rows of a transposed read meet every bank once.
 template <uint32_t X> constexpr uint32_t kRowX = X + 32;
