@@ -458,11 +458,12 @@ __global__ __launch_bounds__(1024) void sum_parts_kernel(const float* partial, f
 
 // ---------------------------------------------------------------------------------------------- gated activation
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
-// The forward pass rounds as its formula is written, where codes are decided by the last bit: the exponential to fp32's precision, and
-// a quotient that is rounded after one step (of at most 2^126, beyond which a silu is no more than 1e-36).
+// The forward pass rounds as its formula x / (1 + exp(-x)) is written, where codes are decided by the last bit: the exponential to fp32's
+// precision, and a quotient that is rounded after one step, of a quarter of both sides, so that the reciprocal of a finite denominator is
+// a normal number.  The fixup has the quotients of what is not finite: where the exponential passes fp32's range, 0 of any finite gate.
 __device__ __forceinline__ float silu(float x) {
-  const float d = fminf(1.0f + expf(-x), 0x1p126f), r = __builtin_amdgcn_rcpf(d), q = x * r;
-  return fmaf(fmaf(-d, q, x), r, q);
+  const float d = fmaf(expf(-x), 0.25f, 0.25f), n = x * 0.25f, r = __builtin_amdgcn_rcpf(d), q = n * r;
+  return __builtin_amdgcn_div_fixupf(fmaf(fmaf(-d, q, n), r, q), d, n);
 }
 
 // The vector unit more than memory: about 40 instructions an element, a third of them the exponential and the quotient as rounded.  8192 x
