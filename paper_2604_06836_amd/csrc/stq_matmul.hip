@@ -143,7 +143,8 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul_tile_kernel(const MatmulA
   constexpr uint32_t VA = TM / kAtOnce, VB = TN / kAtOnce;
   __shared__ __align__(1024) int8_t a0[TM * kStepK], b0[TN * kStepK], a1[TM * kStepK], b1[TN * kStepK];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const TileAt at = tile_at(blockIdx.x, tiles_m, tiles_n);
+  if (group_number() >= tiles_m * tiles_n) return;
+  const TileAt at = tile_at(group_number(), tiles_m, tiles_n);
   const uint32_t m0 = at.row * TM, n0 = at.col * TN;
   int8_t* const pa = static_cast<int8_t*>(a.a.p) + m0 * a.a.stride;
   int8_t* const pb = static_cast<int8_t*>(a.b.p) + n0 * a.b.stride;
@@ -276,7 +277,8 @@ template <uint32_t TO, int G, int R, int A>
 __global__ __launch_bounds__(512) void matmul_few_kernel(const MatmulArgs a) {
   __shared__ __align__(16) v4i part[8][G * R][64];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t n0 = blockIdx.x * 16 * R, row = lane & 15, piece = (lane >> 4) * 16;
+  const uint32_t n0 = group_number() * 16 * R, row = lane & 15, piece = (lane >> 4) * 16;
+  if (n0 >= a.n) return;
   const int8_t* const px = static_cast<const int8_t*>(a.a.p);
   const int8_t* const pw = static_cast<const int8_t*>(a.b.p);
   uint64_t ox[G], ow[R];
@@ -414,7 +416,8 @@ __global__ __launch_bounds__(WC * WI * WJ * 64) void grad_kernel(const MatmulArg
   const uint32_t lane = threadIdx.x & 63, part = WC == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
   const uint32_t thread = threadIdx.x - part * kThreads, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
   auto& tiles = parts[part];
-  const TileAt at = tile_at(blockIdx.x, g.tiles_i, g.tiles_j);
+  if (group_number() >= g.tiles_i * g.tiles_j) return;
+  const TileAt at = tile_at(group_number(), g.tiles_i, g.tiles_j);
   const uint32_t i0 = at.row * TI, j0 = at.col * TJ;
   // (a part may be empty: its steps then lie beyond the sum's end, load the last one and put zeros)
   const uint32_t first = (blockIdx.y * WC + part) * g.each, end = min(g.nc, first + g.each);
@@ -613,7 +616,7 @@ __global__ __launch_bounds__(WC * WI * WJ * 64) void grad_kernel(const MatmulArg
 template <bool WEIGHT, uint32_t TY, uint32_t TO>
 __global__ __launch_bounds__(256) void grad_each_kernel(const MatmulArgs a, const GradShape g) {
   __shared__ float part[8][32];
-  const uint32_t j = blockIdx.x * 32 + (threadIdx.x & 31), turn = threadIdx.x >> 5;
+  const uint32_t j = group_number() * 32 + (threadIdx.x & 31), turn = threadIdx.x >> 5;
   const STQ_GLOBAL typename Elem<TY>::type* dy = as_global(static_cast<const typename Elem<TY>::type*>(a.a.p));
   const STQ_GLOBAL int8_t* q = as_global(static_cast<const int8_t*>(a.b.p));
   for (uint32_t i = blockIdx.y; i < g.ni; i += gridDim.y) {
@@ -677,11 +680,11 @@ void run_matmul(const MatmulArgs& a, uint32_t n_cu, hipStream_t st) {
   } else if (few) {
     // Many rows of w: fewer runs ahead, so that all workgroups fit the card (one token through 11008 x 4096 11.7 us, with four 12.6), or,
     // with more tokens, two fragments of rows for each of tokens (32 tokens 17.7 us, with one 19.1; 4096 x 4096 10.0 and 8.4).
-    if (a.m <= 16 && wide) matmul_few_kernel<TO, 1, 1, 2><<<tiles_of(a.n, 16), 512, 0, st>>>(a);
-    else if (a.m <= 16) matmul_few_kernel<TO, 1, 1, 4><<<tiles_of(a.n, 16), 512, 0, st>>>(a);
-    else if (a.m <= 32 && wide) matmul_few_kernel<TO, 2, 2, 2><<<tiles_of(a.n, 32), 512, 0, st>>>(a);
-    else if (a.m <= 32) matmul_few_kernel<TO, 2, 1, 2><<<tiles_of(a.n, 16), 512, 0, st>>>(a);
-    else matmul_few_kernel<TO, 4, 1, 2><<<tiles_of(a.n, 16), 512, 0, st>>>(a);
+    if (a.m <= 16 && wide) matmul_few_kernel<TO, 1, 1, 2><<<in_layers(tiles_of(a.n, 16)), 512, 0, st>>>(a);
+    else if (a.m <= 16) matmul_few_kernel<TO, 1, 1, 4><<<in_layers(tiles_of(a.n, 16)), 512, 0, st>>>(a);
+    else if (a.m <= 32 && wide) matmul_few_kernel<TO, 2, 2, 2><<<in_layers(tiles_of(a.n, 32)), 512, 0, st>>>(a);
+    else if (a.m <= 32) matmul_few_kernel<TO, 2, 1, 2><<<in_layers(tiles_of(a.n, 16)), 512, 0, st>>>(a);
+    else matmul_few_kernel<TO, 4, 1, 2><<<in_layers(tiles_of(a.n, 16)), 512, 0, st>>>(a);
   } else {
     const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(a.m, t)) * tiles_of(a.n, t); };
     const bool pieces = in_pieces(a.a) && in_pieces(a.b);
@@ -689,11 +692,12 @@ void run_matmul(const MatmulArgs& a, uint32_t n_cu, hipStream_t st) {
     // from one on (1024 x 4096 x 4096: 27.3 us, by 64 x 64 30.5; 2048 outputs 23.8 and 19.0); rows that are not in pieces by way of registers
     // (8192 x 4096 x 4096: 137 us in pieces, 177 not).
     const uint32_t t = pieces && count(256) * 4 >= 3 * n_cu ? 256 : (count(128) >= n_cu ? 128 : 64), rows = tiles_of(a.m, t), cols = tiles_of(a.n, t);
-    if (t == 256) matmul_tile_kernel<TO, 256, 256, 2, 4, true><<<rows * cols, 512, 0, st>>>(a, rows, cols);
-    else if (t == 128 && pieces) matmul_tile_kernel<TO, 128, 128, 2, 2, true><<<rows * cols, 256, 0, st>>>(a, rows, cols);
-    else if (t == 128) matmul_tile_kernel<TO, 128, 128, 2, 2, false><<<rows * cols, 256, 0, st>>>(a, rows, cols);
-    else if (pieces) matmul_tile_kernel<TO, 64, 64, 2, 2, true><<<rows * cols, 256, 0, st>>>(a, rows, cols);
-    else matmul_tile_kernel<TO, 64, 64, 2, 2, false><<<rows * cols, 256, 0, st>>>(a, rows, cols);
+    const dim3 grid = in_layers(count(t));
+    if (t == 256) matmul_tile_kernel<TO, 256, 256, 2, 4, true><<<grid, 512, 0, st>>>(a, rows, cols);
+    else if (t == 128 && pieces) matmul_tile_kernel<TO, 128, 128, 2, 2, true><<<grid, 256, 0, st>>>(a, rows, cols);
+    else if (t == 128) matmul_tile_kernel<TO, 128, 128, 2, 2, false><<<grid, 256, 0, st>>>(a, rows, cols);
+    else if (pieces) matmul_tile_kernel<TO, 64, 64, 2, 2, true><<<grid, 256, 0, st>>>(a, rows, cols);
+    else matmul_tile_kernel<TO, 64, 64, 2, 2, false><<<grid, 256, 0, st>>>(a, rows, cols);
   }
 }
 
@@ -730,7 +734,7 @@ void run_tiles(const MatmulArgs& a, GradShape g, hipStream_t st) {
     g.tiles_j = tiles_of(g.nj, j);
     g.each = tiles_of(g.nc, g.splits * parts * 64) * 64;
     if (parts == 1) g.splits = tiles_of(g.nc, g.each);
-    return dim3(g.tiles_i * g.tiles_j, g.splits);
+    return in_layers(count(i, j), g.splits);
   };
   // 256 x 256 where more than half of the CUs have a tile (dx 2304 x 4096 x 4096: 180 us, by 128 x 128 221; 8192 tokens 451 and 607; at
   // half, 2048 tokens, 191 and 184), of short sums where all have (dw 2048 x 4096 over 400 tokens: 32 us and 24).  Below, 128 x 128, and
@@ -758,7 +762,7 @@ void run_grad(const MatmulArgs& a, GradShape g, hipStream_t st) {
     g.splits = 0;
     join<TO>(a, g, st);
   } else if (g.ni < 8 || g.nj < 8 || g.nc < 8 || !near(a.a) || !near(a.b)) {
-    grad_each_kernel<WEIGHT, TY, TO><<<dim3(tiles_of(g.nj, 32), g.ni < 65535 ? g.ni : 65535), 256, 0, st>>>(a, g);
+    grad_each_kernel<WEIGHT, TY, TO><<<in_layers(tiles_of(g.nj, 32), g.ni < 65535 ? g.ni : 65535), 256, 0, st>>>(a, g);
   } else if (g.nj % 8 == 0 && (WEIGHT ? g.ni : g.nc) % 8 == 0) {
     run_tiles<WEIGHT, true, TY, TO>(a, g, st);
   } else {

@@ -438,7 +438,7 @@ STQ_ROWS_KERNEL rms_norm_grad_kernel(const NormGradArgs a) {
 // dweight[c] = the sum of the parts of column c: 16 columns a workgroup, of whose 64 threads for each a part goes to each in turn.
 __global__ __launch_bounds__(1024) void sum_parts_kernel(const float* partial, float* out, uint32_t groups, uint32_t cols) {
   __shared__ float box[64][17];
-  const uint32_t turn = threadIdx.x >> 4, lane = threadIdx.x & 15, c = blockIdx.x * 16 + lane;
+  const uint32_t turn = threadIdx.x >> 4, lane = threadIdx.x & 15, c = group_number() * 16 + lane;
   float s = 0.0f;
   if (c < cols) {
 #pragma unroll 16
@@ -647,7 +647,7 @@ int launch_rms_norm_grad(NormGradArgs a, uint32_t sum_type, uint32_t type, void*
     }); }); });
     if (const hipError_t e = hipGetLastError()) return e;
   }
-  sum_parts_kernel<<<(a.cols - 1) / 16 + 1, 1024, 0, st>>>(a.partial, a.dweight, groups, a.cols);
+  sum_parts_kernel<<<in_layers((a.cols - 1) / 16 + 1), 1024, 0, st>>>(a.partial, a.dweight, groups, a.cols);
   return hipGetLastError();
 }
 int launch_gated(const GatedArgs& a, uint32_t type, uint32_t n_cu, void* stream) {

@@ -10,6 +10,15 @@
 namespace stq {
 namespace {
 
+// Workgroups of launches that grow with a matrix' size, in layers of 2^21: HIP counts the threads along an axis in 32 bits, and beyond
+// that leaves workgroups out without an error.  Those of the last layer whose number is too large have nothing to do.
+constexpr uint32_t kLgLayer = 21;
+inline dim3 in_layers(uint64_t groups, uint32_t y = 1) {
+  const uint64_t most = 1u << kLgLayer;
+  return dim3(static_cast<uint32_t>(groups < most ? groups : most), y, static_cast<uint32_t>((groups + most - 1) >> kLgLayer));
+}
+__device__ __forceinline__ uint32_t group_number() { return blockIdx.z << kLgLayer | blockIdx.x; }
+
 template <uint32_t TY> struct Elem;
 template <> struct Elem<kF32> { using type = float; };
 template <> struct Elem<kBF16> { using type = __bf16; };

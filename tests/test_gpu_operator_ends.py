@@ -18,6 +18,12 @@ def ctx():
     c.close()
 
 
+@pytest.fixture(autouse=True)
+def memory_back():
+    yield
+    torch.cuda.empty_cache()
+
+
 # ------------------------------------------------------------------------------------------------ gated activation
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("cols", [8, 100, 600, 4096, 20000])
@@ -52,3 +58,100 @@ def test_gates_that_are_not_finite(ctx):
         y = Codes(3, 64)
         ctx.gated_silu(matrix(gate), matrix(torch.ones_like(gate)), y.mat, None, None, stream())
         assert torch.isnan(y.s[:, 0]).tolist() == [False, True, False] and (y.q.t[1] == 0).all()
+
+
+# ------------------------------------------------------------------------------------------------ sizes whose launches pass 2^32 threads
+PERIOD = 1021  # rows repeat, so that results can be known without a product of the whole size
+
+
+def repeated(base, rows):
+    t = torch.empty(rows, *base.shape[1:], dtype=base.dtype, device="cuda")
+    whole = rows // PERIOD
+    t[:whole * PERIOD].view(whole, *base.shape).copy_(base)
+    t[whole * PERIOD:].copy_(base[:rows - whole * PERIOD])
+    return t
+
+
+def repeats(t, base):
+    whole = len(t) // PERIOD
+    return all(bool((p == base).all()) for p in t[:whole * PERIOD].view(whole, *base.shape).split(1 << 16)) and torch.equal(
+        t[whole * PERIOD:], base[:len(t) - whole * PERIOD])
+
+
+def codes_and_scales(seed, rows, cols):
+    g = torch.Generator("cuda").manual_seed(seed)
+    return (torch.randint(-127, 128, (rows, cols), device="cuda", generator=g, dtype=torch.int8), torch.rand(rows, 1, device="cuda", generator=g) + 0.5)
+
+
+def product(ctx, x, w, dtype=torch.bfloat16):
+    out = torch.empty(len(x[0]), len(w[0]), dtype=dtype, device="cuda")
+    ctx.matmul(matrix(*x), matrix(*w), matrix(out), stream())
+    return out
+
+
+@pytest.mark.parametrize("tokens,outputs", [(1, (1 << 27) + 5), (17, (1 << 28) + 37), (40, (1 << 27) + 3)])
+def test_few_tokens_by_many_outputs(ctx, tokens, outputs):
+    """40 tokens: by rows too far apart for tiles, of which this kernel then takes up to 64."""
+    x, w = codes_and_scales(1, tokens, 16), codes_and_scales(2, PERIOD, 16)
+    if tokens > 32:
+        apart = torch.zeros(tokens, 1 << 22, dtype=torch.int8, device="cuda")
+        apart[:, :16] = x[0]
+        x = (apart[:, :16], x[1])
+    want = product(ctx, x, w).t().contiguous()
+    exact = (w[0].double() @ x[0].double().t()) * w[1].double() * x[1].double().t()
+    assert ((want.double() - exact).abs() <= 2.0 ** -8 * exact.abs()).all()
+    out = product(ctx, x, (repeated(w[0], outputs), repeated(w[1], outputs)))
+    for t in range(tokens):
+        assert repeats(out[t], want[:, t])
+
+
+def test_many_tokens_by_one_output(ctx):
+    """Tiles of 256 x 256 at the largest number of rows."""
+    tokens = (1 << 31) - 1
+    x, w = codes_and_scales(3, PERIOD, 16), codes_and_scales(4, 1, 16)
+    want = product(ctx, x, w)
+    exact = (x[0].double() @ w[0].double().t()) * w[1].double() * x[1].double()
+    assert ((want.double() - exact).abs() <= 2.0 ** -8 * exact.abs()).all()
+    assert repeats(product(ctx, (repeated(x[0], tokens), repeated(x[1], tokens)), w), want)
+
+
+def test_gradient_of_many_tokens(ctx):
+    """Tiles of the gradients at the largest number of rows."""
+    tokens = (1 << 31) - 1
+    dy = torch.randn(PERIOD, 8, device="cuda", generator=torch.Generator("cuda").manual_seed(5)).bfloat16()
+    w = codes_and_scales(6, 8, 8)
+
+    def grad(dy):
+        dx = torch.empty(len(dy), 8, dtype=torch.bfloat16, device="cuda")
+        ctx.matmul_grad_input(matrix(dy), matrix(*w), matrix(dx), stream())
+        return dx
+    want = grad(dy)
+    values = w[0].double() * w[1].double()
+    exact, size = dy.double() @ values, dy.double().abs() @ values.abs()
+    assert ((want.double() - exact).abs() <= 2.0 ** -8 * exact.abs() + 2.0 ** -16 * (1 + 2.0 ** -7) * size).all()
+    assert repeats(grad(repeated(dy, tokens)), want)
+
+
+def test_gradient_of_many_inputs(ctx):
+    """Narrow gradients, one token of one output: dx = dy * scale * code."""
+    inputs = (1 << 29) + 77
+    q, s = codes_and_scales(7, PERIOD, 1)[0].view(-1), torch.full((1, 1), 0.75, device="cuda")
+    dy, dx = torch.full((1, 1), 3.0, device="cuda"), torch.empty(1, inputs, device="cuda")
+    ctx.matmul_grad_input(matrix(dy), matrix(repeated(q, inputs).view(1, inputs), s), matrix(dx), stream())
+    assert repeats(dx[0], q.float() * 2.25)
+
+
+def test_norm_gradients_of_many_columns(ctx):
+    cols = (1 << 26) + 19
+    g = torch.Generator("cuda").manual_seed(8)
+    x, dy = (torch.randn(1, cols, device="cuda", generator=g).bfloat16() for _ in range(2))
+    w, rstd = torch.ones(cols, device="cuda"), torch.ones(1, device="cuda")
+    dx, dw = torch.empty_like(dy), torch.full((cols,), 9.0, device="cuda")
+    n = stq.rms_norm_grad_bytes(1, cols)
+    work = torch.empty(n, dtype=torch.uint8, device="cuda")
+    ctx.rms_norm_grad(matrix(x), w.data_ptr(), rstd.data_ptr(), matrix(dy), None, matrix(dx), dw.data_ptr(), work.data_ptr(), n, stream())
+    assert torch.equal(dw, (dy.float() * x.float())[0])  # one row: a product of 16 significant bits
+    mean = (dy.double() * x.double()).mean()
+    want = dy.double() - x.double() * mean
+    # the sum of 8192 products and ten levels more in each lane, in fp32, and the result's own rounding
+    assert ((dx.double() - want).abs() <= 2.0 ** -8 * want.abs() + 8300 * 8 * U * (dy.double() * x.double()).abs().mean() * x.double().abs() + 8 * U * want.abs()).all()
