@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2604_06836_amd as stq
-from test_gpu_operators import U, Codes, check_codes, matrix, silu, stream
+from test_gpu_operators import B, TYPES, U, Codes, check_codes, matrix, silu, stream
 
 pytestmark = pytest.mark.gpu
 
@@ -58,6 +58,81 @@ def test_gates_that_are_not_finite(ctx):
         y = Codes(3, 64)
         ctx.gated_silu(matrix(gate), matrix(torch.ones_like(gate)), y.mat, None, None, stream())
         assert torch.isnan(y.s[:, 0]).tolist() == [False, True, False] and (y.q.t[1] == 0).all()
+
+
+# ------------------------------------------------------------------------------------------------ gradients
+SHAPES = [(4099, 4111, 100), (4096, 4096, 64), (2049, 2050, 601), (2056, 2040, 640), (333, 999, 777), (1000, 1000, 24), (31, 641, 13), (32, 640, 8),
+          (64, 64, 2048), (100, 99, 3001), (3, 5, 200)]  # results i x j over a sum of c, for each tile, whole and ragged
+
+
+def sums(ctx, which, dy, q, s, kind):
+    """The gradient whose rows are dy's [i][c] (transposed for a weight's) over codes [c][j]."""
+    i, j = len(dy), q.shape[1]
+    out = torch.empty(i, j, dtype=TYPES[kind], device="cuda")
+    if which == "input":
+        ctx.matmul_grad_input(matrix(dy), matrix(q, s), matrix(out), stream())
+        return out
+    n = stq.matmul_grad_weight_bytes(len(q), i, j)
+    work = torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
+    across = dy.t().contiguous()
+    ctx.matmul_grad_weight(matrix(across), matrix(q, s), matrix(out), work.data_ptr(), n, stream())
+    return out
+
+
+def operands(i, j, c):
+    """Small gradients, codes of -1, 0 and 1, scales of powers of two: sums that large elements do not leave fp32's range with."""
+    g = torch.Generator("cuda").manual_seed(i + 2 * j + 3 * c)
+    dy = torch.randn(i, c, device="cuda", generator=g)
+    q = torch.randint(-1, 2, (c, j), device="cuda", generator=g, dtype=torch.int8)
+    return dy, q, torch.exp2(torch.randint(-2, 1, (c, 1), device="cuda", generator=g).float())
+
+
+@pytest.mark.parametrize("which", ["input", "weight"])
+@pytest.mark.parametrize("i,j,c", SHAPES)
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("of", ["bf16", "fp32"])
+def test_infinities_of_gradients(ctx, which, i, j, c, kind, of):
+    """An infinity of dy, or of a scale, is one in the results: NaN only where it meets a code of zero, or another sign."""
+    dy, q, s = operands(i, j, c)
+    dy = dy.to(TYPES[of])
+    at, at2 = (i - 1, c // 2), (i // 2, c - 1)
+    dy[at], dy[at2], dy[0, 0] = math.inf, -math.inf, math.nan
+    got = sums(ctx, which, dy, q, s, kind).double()
+    for row, col in (at, at2):
+        want = dy[row, col].double() * q[col].double()  # the other elements are finite
+        assert torch.equal(torch.isnan(got[row]), torch.isnan(want)) and torch.equal(got[row][q[col] != 0], want[q[col] != 0])
+    assert torch.isnan(got[0]).all()
+    rest = torch.ones(i, dtype=torch.bool, device="cuda")
+    rest[[0, at[0], at2[0]]] = False
+    assert torch.isfinite(got[rest]).all()
+    dy[0, 0] = dy[at] = dy[at2] = 1.0
+    s[c // 3] = math.inf
+    got = sums(ctx, which, dy, q, s, kind).double()
+    want = (dy[:, c // 3].double() * math.inf)[:, None] * q[c // 3].double()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got[~torch.isnan(want)], want[~torch.isnan(want)])
+
+
+@pytest.mark.parametrize("which", ["input", "weight"])
+@pytest.mark.parametrize("i,j,c", SHAPES)
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+def test_gradients_beyond_the_largest_bf16(ctx, which, i, j, c, kind):
+    """dy * s between bf16's largest number and fp32's: a finite factor as any other."""
+    dy, q, s = operands(i, j, c)
+    big, a, b = 3.4025e38, c // 4, c // 2
+    s[a] = s[b] = 1.0
+    q[b] = q[a]
+    dy[i - 1, a], dy[i - 1, b], dy[0, a], dy[0, b] = big, -big, -big, 0.0
+    got = sums(ctx, which, dy, q, s, kind).double()
+    d = dy.double() * s.double().t()
+    want, size = d @ q.double(), d.abs() @ q.double().abs()
+    if kind == "bf16":
+        assert torch.isfinite(got[i - 1]).all()
+        hit = q[a] != 0
+        assert torch.equal(torch.isinf(got[0]), hit) and torch.equal(got[0][hit].sign(), want[0][hit].sign())  # rounded to bf16
+        got, want, size = got[1:], want[1:], size[1:]
+    # a factor's own rounding, its terms' (24 bits, or 16), a sum's, the result's
+    bound = (U + (2.0 ** -16 if kind == "bf16" else 2.0 ** -24) + (c + 2) * U) * size + (B if kind == "bf16" else U) * want.abs()
+    assert ((got - want).abs() <= bound).all()
 
 
 # ------------------------------------------------------------------------------------------------ sizes whose launches pass 2^32 threads
