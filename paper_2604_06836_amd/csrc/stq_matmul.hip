@@ -72,6 +72,13 @@ __device__ __forceinline__ void store_piece(const Mat& out, uint32_t row, uint32
       if (col + i < end) p[i] = e[i];
   }
 }
+// What the lanes of a wave have put into LDS is there for the others after this, and what they have read may be written over: LDS takes a
+// wave's accesses in their order, so that only the compiler has to keep it.
+__device__ __forceinline__ void lanes_meet() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 // A wave's result, FI x FJ fragments of 32 x 32 from row0, col0 on, into an output of rows x cols, by way of 32 rows of LDS of its own
 // (`box`, 4096 FJ bytes for fp32), so that whole pieces of rows are stored, neighbouring ones together.  value(i, j, p, e): column
 // 8 p + 4 (lane / 32) + e of row lane % 32 of fragment i, j.  Pieces lie at the places that their number and the row's give by
@@ -92,6 +99,7 @@ __device__ __forceinline__ void store_tile(const Mat& out, uint32_t row0, uint32
         const uint32_t byte = (j * 32 + p * 8 + (lane >> 5) * 4) * kSize;
         pack4<TO>(v, box + place(lane & 31, byte / 16) + byte % 16);
       }
+    lanes_meet();
 #pragma unroll
     for (uint32_t h = 0; h < 32 * kPieces / 64; ++h) {
       const uint32_t row = h * (64 / kPieces) + lane / kPieces, piece = lane % kPieces;
@@ -100,6 +108,7 @@ __device__ __forceinline__ void store_tile(const Mat& out, uint32_t row0, uint32
       const uint32_t r = row0 + i * 32 + row, c = col0 + piece * (16 / kSize);
       if (r < rows && c < cols) store_piece<TO>(out, r, c, cols, v);
     }
+    lanes_meet();
   }
 }
 // Four elements where they are: for kernels whose results are few.

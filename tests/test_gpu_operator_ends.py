@@ -135,6 +135,23 @@ def test_gradients_beyond_the_largest_bf16(ctx, which, i, j, c, kind):
     assert ((got - want).abs() <= bound).all()
 
 
+# ------------------------------------------------------------------------------------------------ places
+@pytest.mark.parametrize("m,n", [(4096, 4096), (4000, 4091), (2048, 2048), (2000, 2045), (200, 300), (131, 77), (30, 70)])
+def test_every_element_in_its_place(ctx, m, n):
+    """Results that name their row and column, exact in fp32, through the LDS of each tile's waves."""
+    x, w = (torch.ones(r, 1, dtype=torch.int8, device="cuda") for r in (m, n))
+    row, col = 1.0 + torch.arange(m, device="cuda"), (1.0 + torch.arange(n, device="cuda")) / 4096
+    got = product(ctx, (x, row[:, None].contiguous()), (w, col[:, None].contiguous()), torch.float32)
+    assert torch.equal(got, row[:, None] * col)
+    at = torch.arange(n, device="cuda")
+    q = torch.zeros(8, n, dtype=torch.int8, device="cuda")
+    q[1], q[6] = (at % 127).to(torch.int8), (at // 127).to(torch.int8)
+    dy = torch.zeros(m, 8, device="cuda")
+    dy[:, 1], dy[:, 6] = row, 127 * row
+    for which in ("input", "weight"):
+        assert torch.equal(sums(ctx, which, dy, q, torch.ones(8, 1, device="cuda"), "fp32"), row[:, None] * at)
+
+
 # ------------------------------------------------------------------------------------------------ sizes whose launches pass 2^32 threads
 PERIOD = 1021  # rows repeat, so that results can be known without a product of the whole size
 
