@@ -382,8 +382,9 @@ int stq_dequantize_rows(stq_ctx* ctx, const stq_matrix* codes, const stq_matrix*
  *   rstd[row] = 1 / sqrt(mean(sum^2) + eps),  y = sum * rstd * weight, written as codes with a scale for each row
  * x, residual: fp32 or bf16, one type.  weight: device, fp32[cols].  eps > 0, finite.  sum: x's type, may be NULL, and may be
  * x's or residual's own buffer.  y: STQ_Q8, block 0.  saved (may be NULL): the sum in 8 bits, any block, for
- * stq_rms_norm_grad.  rstd: device, fp32[rows], may be NULL.  A row whose squares add up to more than fp32 holds counts as not
- * finite: its scale and rstd are NaN. */
+ * stq_rms_norm_grad.  rstd: device, fp32[rows], may be NULL.  The least magnitude that a row of y counts as is 2^-100 of sum * weight as
+ * of y: a = max(max|y|, rstd * 2^-100, 2^-100), so that a row of zeros has the scale rstd * 2^-100 / 127 where rstd is above 1.  A row whose
+ * squares add up to more than fp32 holds counts as not finite: its scale and rstd are NaN. */
 int stq_rms_norm(stq_ctx* ctx, const stq_matrix* x, const stq_matrix* residual, const float* weight, float eps,
                  const stq_matrix* sum, const stq_matrix* y, const stq_matrix* saved, float* rstd, void* hip_stream);
 

@@ -306,7 +306,7 @@ STQ_ROWS_KERNEL rms_norm_kernel(const NormArgs a) {
     const bool finite = magnitude(squares) < kInf;
     const float rstd = finite ? 1.0f / __fsqrt_rn(squares / static_cast<float>(a.cols) + a.eps) : __builtin_nanf("");
     const Coder ks = coder_of(largest);
-    uint32_t largest_y = f2u(rstd * kLeast);  // a row of zeros has a scale that is in the rows' measure
+    uint32_t largest_y = f2u(rstd * kLeast);  // 2^-100 in the measure of h w, so that a row of zeros has a scale in it
     const auto again = [&](uint32_t c, int at) {  // h and weight of a vector that is not held; the sum may have taken x's or residual's place
       if (V) return;
       if (!a.sum.p) return add(c, at);

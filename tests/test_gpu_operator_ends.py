@@ -60,6 +60,27 @@ def test_gates_that_are_not_finite(ctx):
         assert torch.isnan(y.s[:, 0]).tolist() == [False, True, False] and (y.q.t[1] == 0).all()
 
 
+# ------------------------------------------------------------------------------------------------ conversion
+LEAST = 2.0 ** -100
+
+
+@pytest.mark.parametrize("cols", [7, 512, 1600, 4096, 20000])
+@pytest.mark.parametrize("eps", [1e-5, 0.25, 4.0, 1e10])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_norm_of_nothing_and_little(ctx, cols, eps, dtype):
+    """Codes and scales of rows of zeros, of less than 2^-100 and of little more, bit for bit: a = max(max|y|, rstd 2^-100, 2^-100)."""
+    x = torch.randn(6, cols, device="cuda", generator=torch.Generator("cuda").manual_seed(cols)).to(dtype)
+    x *= torch.tensor([0, 1e-36, 1e-32, 1e-29, 1e-27, 1], device="cuda").to(dtype)[:, None]
+    w = torch.linspace(0.5, 1.5, cols, device="cuda")
+    y, rstd = Codes(6, cols), torch.empty(6, device="cuda")
+    ctx.rms_norm(matrix(x), None, w.data_ptr(), eps, None, y.mat, None, rstd.data_ptr(), stream())
+    v = x.float() * rstd[:, None] * w
+    a = torch.maximum(v.abs().amax(1), rstd * LEAST).clamp_min(LEAST)
+    assert torch.equal(y.s[:, 0], a * torch.tensor(1 / 127, dtype=torch.float32, device="cuda"))
+    assert torch.equal(y.q.t, torch.round(v * (127.0 * (1.0 / a))[:, None]).to(torch.int8))
+    assert (y.q.t[0] == 0).all() and torch.equal(rstd[0], (1 / torch.sqrt(torch.tensor(eps, device="cuda"))))
+
+
 # ------------------------------------------------------------------------------------------------ gradients
 SHAPES = [(4099, 4111, 100), (4096, 4096, 64), (2049, 2050, 601), (2056, 2040, 640), (333, 999, 777), (1000, 1000, 24), (31, 641, 13), (32, 640, 8),
           (64, 64, 2048), (100, 99, 3001), (3, 5, 200)]  # results i x j over a sum of c, for each tile, whole and ragged
