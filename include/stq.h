@@ -350,8 +350,9 @@ int stq_engine_destroy(stq_engine* e);
  * 8 bits (STQ_Q8): int8 codes q and fp32 scales s, value s * q.  block = 0: one scale for each row, at
  * scales[row]; block = 64, 128 or 256: one for each `block` columns of a row (the last may cover fewer), at
  * scales[row * ceil(cols / block) + col / block].  Written codes are q = rint(x * (127 * (1 / a))), s = a * (1 / 127)
- * with a = max(max|x|, 2^-100) over the scale's elements (fp32, each step rounded; ties to even; -127 <= q <= 127).  Where one of these
- * elements is not finite, s is NaN and the codes are 0: everything computed from them is NaN then.
+ * with a = max(max|x|, 2^-100) over the scale's elements (fp32, each step rounded, 1 / a to 24 bits also below fp32's normal
+ * numbers; ties to even; -127 <= q <= 127).  Where one of these elements is not finite, s is NaN and the codes are 0: everything
+ * computed from them is NaN then.
  *
  * Gradients pass through the conversion as if it were the identity; they are those of the values that the
  * codes stand for. */

@@ -64,6 +64,24 @@ def test_gates_that_are_not_finite(ctx):
 LEAST = 2.0 ** -100
 
 
+@pytest.mark.parametrize("block", [0, 64])
+@pytest.mark.parametrize("size", [2.0 ** -90, 2.0 ** 63, 2.0 ** 64, 2.0 ** 120, 2.0 ** 125, 2.0 ** 126, 2.0 ** 127])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_codes_of_large_numbers(ctx, block, size, dtype):
+    """Bit for bit up to fp32's largest numbers, of which 1 / a has 24 bits although it is below fp32's normal ones."""
+    x = (torch.rand(300, 128, device="cuda", generator=torch.Generator("cuda").manual_seed(3)) * 3.9 - 1.95).to(dtype)
+    x[:, 5], x[:, 100] = 1.95 * torch.rand(300, device="cuda", generator=torch.Generator("cuda").manual_seed(4)), 1.95
+    codes, v = Codes(300, 128, block), x.float() * size
+    ctx.quantize_rows(matrix(v.to(dtype)), codes.mat, stream())
+    assert torch.isfinite(v).all() and torch.equal(v.to(dtype).float(), v)
+    width = block or 128
+    a = v.view(300, -1, width).abs().amax(2, keepdim=True)
+    small = a * 2.0 ** -64 if size > 1 else a
+    inv = 127.0 * (1.0 / small)
+    q = torch.round(v.view(300, -1, width) * (inv * 2.0 ** -64 if size > 1 else inv))
+    assert torch.equal(codes.s, (a * torch.tensor(1 / 127, dtype=torch.float32, device="cuda")).squeeze(2)) and torch.equal(codes.q.t, q.view(300, 128).to(torch.int8))
+
+
 @pytest.mark.parametrize("cols", [7, 512, 1600, 4096, 20000])
 @pytest.mark.parametrize("eps", [1e-5, 0.25, 4.0, 1e10])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
