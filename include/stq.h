@@ -400,14 +400,16 @@ int stq_rms_norm_grad(stq_ctx* ctx, const stq_matrix* sum, const float* weight, 
                       uint64_t workspace_bytes, void* hip_stream);
 int stq_rms_norm_grad_bytes(uint64_t rows, uint64_t cols, uint64_t* bytes); /* host only */
 
-/* Gated activation y = silu(gate) * up, silu(g) = g / (1 + exp(-g)), written as codes with a scale for each row (y: STQ_Q8,
- * block 0).  gate, up: fp32 or bf16, one type, the same size (two halves of one matrix, for instance).  saved_gate,
- * saved_up (NULL both, or neither): gate and up in 8 bits, one block, for stq_gated_silu_grad. */
+/* Gated activation y = silu(gate) * up, silu(g) = g / (1 + exp(-g)) with an exponential of fp32's precision and every step rounded
+ * (0 where it passes fp32's range, for gates below -88.7), written as codes with a scale for each row (y: STQ_Q8, block 0).  gate,
+ * up: fp32 or bf16, one type, the same size (two halves of one matrix, for instance).  saved_gate, saved_up (NULL both, or
+ * neither): gate and up in 8 bits, one block, for stq_gated_silu_grad. */
 int stq_gated_silu(stq_ctx* ctx, const stq_matrix* gate, const stq_matrix* up, const stq_matrix* y,
                    const stq_matrix* saved_gate, const stq_matrix* saved_up, void* hip_stream);
 
 /* Its gradients: dgate = dy * up * (s + gate * s * (1 - s)), s = 1 / (1 + exp(-gate)), and dup = dy * gate * s.  gate, up: one
- * type and block, fp32, bf16 or 8 bits.  dy, dgate, dup: fp32 or bf16, one type; dgate or dup may be dy's own buffer. */
+ * type and block, fp32, bf16 or 8 bits.  dy, dgate, dup: fp32 or bf16, one type; dgate or dup may be dy's own buffer.  s comes from
+ * the hardware's exponential and reciprocal: off by up to (2 |gate| + 10) 2^-24 of itself, and perhaps 0 where it is below 2^-126. */
 int stq_gated_silu_grad(stq_ctx* ctx, const stq_matrix* gate, const stq_matrix* up, const stq_matrix* dy,
                         const stq_matrix* dgate, const stq_matrix* dup, void* hip_stream);
 

@@ -457,6 +457,7 @@ __global__ __launch_bounds__(1024) void sum_parts_kernel(const float* partial, f
 }
 
 // ---------------------------------------------------------------------------------------------- gated activation
+// (the gradients': off by up to (2 |x| + 10) 2^-24, since the exponential's argument is rounded)
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
 // The forward pass rounds as its formula x / (1 + exp(-x)) is written, where codes are decided by the last bit: the exponential to fp32's
 // precision, and a quotient that is rounded after one step, of a quarter of both sides, so that the reciprocal of a finite denominator is
