@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2604_06836_amd as stq
-from test_gpu_operators import B, TYPES, U, Codes, check_codes, matrix, silu, stream
+from test_gpu_operators import B, LEAST, TYPES, U, Codes, check_codes, matrix, silu, stream
 
 pytestmark = pytest.mark.gpu
 
@@ -50,6 +50,22 @@ def test_rows_of_large_negative_gates(ctx, dtype, cols, keep):
     assert (dg[:len(ends)] == 0).all() and (du[:len(ends)] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("cols", [500, 1000, 4096, 10000, 20000])
+def test_codes_of_the_gated_activation(ctx, dtype, cols):
+    """Rows of gates of one size each, -80 to 80, so that codes follow the least bits of their exponentials.  In units of 2^-24: y is off by
+    the exponential's last place (2), the sum, the quotient and the product, 5; its largest by as much; 1 / a, 127 and the product, 3."""
+    g = torch.Generator("cuda").manual_seed(cols)
+    gate = torch.linspace(-80, 80, 161, device="cuda")[:, None] + torch.rand(161, cols, device="cuda", generator=g)
+    gate, up = gate.to(dtype), torch.randn(161, cols, device="cuda", generator=g).to(dtype)
+    y = Codes(161, cols)
+    ctx.gated_silu(matrix(gate), matrix(up), y.mat, None, None, stream())
+    v = silu(gate.double()) * up.double()
+    a = v.abs().amax(1, keepdim=True).clamp_min(LEAST)
+    assert ((y.s.double() - a / 127).abs() <= 8 * U * a / 127).all()
+    assert ((y.q.t.double() - v * 127 / a).abs() <= 0.5 + 127 * 14 * U).all()
+
+
 def test_gates_that_are_not_finite(ctx):
     """x / (1 + exp(-x)) of infinities and NaN: none of them has a code."""
     for bad in (math.inf, -math.inf, math.nan):
@@ -61,9 +77,6 @@ def test_gates_that_are_not_finite(ctx):
 
 
 # ------------------------------------------------------------------------------------------------ conversion
-LEAST = 2.0 ** -100
-
-
 @pytest.mark.parametrize("block", [0, 64])
 @pytest.mark.parametrize("size", [2.0 ** -90, 2.0 ** 63, 2.0 ** 64, 2.0 ** 120, 2.0 ** 125, 2.0 ** 126, 2.0 ** 127])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
@@ -149,6 +162,30 @@ def test_infinities_of_gradients(ctx, which, i, j, c, kind, of):
     got = sums(ctx, which, dy, q, s, kind).double()
     want = (dy[:, c // 3].double() * math.inf)[:, None] * q[c // 3].double()
     assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got[~torch.isnan(want)], want[~torch.isnan(want)])
+
+
+@pytest.mark.parametrize("which", ["input", "weight"])
+@pytest.mark.parametrize("i,j,c", SHAPES)
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+def test_terms_of_gradients(ctx, which, i, j, c, kind):
+    """dy * s with all of its 24 bits in fp32 results, and with 16 in bf16 ones.  Two elements of dy in a row and no others, so that there is
+    little of the sum's own rounding: of six terms or four, and one of dy * s.  They cancel to a part of 2^-5 and less, which leaves little
+    of a bf16 result's rounding."""
+    dy, q, s = operands(i, j, c)
+    g = torch.Generator("cuda").manual_seed(1)
+    q = torch.randint(-127, 128, (c, j), device="cuda", generator=g, dtype=torch.int8)
+    a, b = c // 3, c - 1
+    q[b] = q[a]
+    s[a], s[b] = 0.7, 0.9
+    first = torch.randn(i, device="cuda", generator=g)
+    dy.zero_()
+    dy[:, a], dy[:, b] = first / s[a], -first * (1 + torch.rand(i, device="cuda", generator=g) / 32) / s[b]
+    got = sums(ctx, which, dy, q, s, kind).double()
+    d = dy.double() * s.double().t()
+    want, size = d @ q.double(), d.abs() @ q.double().abs()
+    # a last place, two units, for each addition of the matrix cores; three terms hold all of dy * s (two are off by up to 2^-16)
+    bound = ((1 + 2 * 6) * U + (0 if kind == "fp32" else 2.0 ** -16)) * size + (U if kind == "fp32" else B) * want.abs()
+    assert ((got - want).abs() <= bound).all()
 
 
 @pytest.mark.parametrize("which", ["input", "weight"])
