@@ -141,8 +141,8 @@ __device__ __forceinline__ TileAt tile_at(uint32_t id, uint32_t rows, uint32_t c
 // Rows beyond the matrix' end repeat its last one; a step that goes beyond the rows' end comes through registers, with zeros there.
 // PIECES: whether the rows lie in 16-byte pieces; others come through registers altogether, loaded a step ahead.
 // 256 x 256 with eight waves of 128 x 64: as much of w and x in registers as two waves on a SIMD can hold, so that LDS is read for a step
-// in less time than the matrix cores take for it.  16384 x 11008 x 4096: 655 us, 2.25 Pop/s, which is what this card's library product of
-// int8 codes reaches (2.28); of zeros 3.3, so that what bounds it is the card's power.
+// in less time than the matrix cores take for it.  16384 x 11008 x 4096: 656 to 685 us, 2.25 to 2.16 Pop/s, little below this card's library
+// product of int8 codes (2.28 to 2.37 for 8192^3); of zeros 3.3, so that what bounds it is the card's power.
 [[maybe_unused]] constexpr uint32_t kStepK = 128;
 
 template <uint32_t TO, int TM, int TN, int WM, int WN, bool PIECES>
@@ -381,7 +381,7 @@ __global__ __launch_bounds__(256) void matmul_each_kernel(const MatmulArgs a) {
 // A workgroup has TI x TJ of the result, its WI x WJ waves a part each, and takes STEP of c at a time: what a step needs is loaded
 // into registers two steps ahead, turned into bf16 and put into one of two LDS buffers one step ahead.  Operands whose rows run along
 // i or j are read out of LDS transposed, four rows of 16 columns at a time.  256 x 256 with eight waves of 128 x 64, as above: dx 8192 x
-// 4096 x 11008 in bf16 in 1240 to 1295 us, 1.19 to 1.14 Pflop/s of the matrix cores (this card's library reaches 1.33 for a product of two bf16 matrices,
+// 4096 x 11008 in bf16 in 1216 to 1301 us, 1.21 to 1.14 Pflop/s of the matrix cores (this card's library reaches 1.33 to 1.41 for a product of two bf16 matrices,
 // and would need both factors and both terms in memory first).  What bounds it is the card's power.
 // A [c][x] tile: rows of X elements, 64 bytes more apart than that, so that the four rows of a transposed read meet every bank once.
 template <uint32_t X> constexpr uint32_t kRowX = X + 32;
@@ -646,7 +646,8 @@ __global__ __launch_bounds__(WC * WI * WJ * 64) void grad_kernel(const MatmulArg
 }
 
 // Results or sums of fewer than eight along a side, or rows too far apart for the offsets of a tile: 32 columns of a row to a workgroup,
-// with eight threads for each that share c.
+// with eight threads for each that share c.  2 outputs by 4096 inputs over 16384 tokens: dw in fp32 635 us, dx in bf16 567 (the bytes would take
+// 11 and 23).
 template <bool WEIGHT, uint32_t TY, uint32_t TO>
 __global__ __launch_bounds__(256) void grad_each_kernel(const MatmulArgs a, const GradShape g) {
   __shared__ float part[8][32];

@@ -257,7 +257,7 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const RowsArgs a, uint3
 // ---------------------------------------------------------------------------------------------- norm
 // Two exchanges a row, of the squares and then of max|y|.  (The codes are free of rstd, and with max|h w| in place of max|y| one exchange
 // would do, in the same time; but its roundings are others than the formula's, and so are codes next to a half.)  Bound by memory: 16384 x
-// 4096 in bf16 with the residual, the sum kept in 8 bits, 104 us, 5.2 TB/s (a large copy reaches 5.4).
+// 4096 in bf16 with the residual, the sum kept in 8 bits, 104 us, 5.2 TB/s (an addition in place of 4 GiB reaches 5.9).
 template <uint32_t TY, class R>
 STQ_ROWS_KERNEL rms_norm_kernel(const NormArgs a) {
   constexpr int V = R::V;
@@ -468,7 +468,7 @@ __device__ __forceinline__ float silu(float x) {
 }
 
 // The vector unit more than memory: about 40 instructions an element, a third of them the exponential and the quotient as rounded.  8192 x
-// 11008 in bf16 with both inputs kept: 159 us, 4.0 TB/s (126 with a silu and codes to a few units in the last place).  No
+// 11008 in bf16 with both inputs kept: 161 us, 4.0 TB/s (126 with a silu and codes to a few units in the last place).  No
 // row is loaded ahead here: more waves hide more than a row of each would (164 us with, 141 without, when codes were divisions).
 template <class R> constexpr uint32_t kGatedWaves = R::V == 2 ? 6 : 8;  // of a SIMD
 template <uint32_t TY, class R>
