@@ -419,8 +419,8 @@ int stq_matmul(stq_ctx* ctx, const stq_matrix* x, const stq_matrix* w, const stq
 
 /* Gradient of x: dx[token][i] = sum over o of dy[token][o] * w.scales[o] * w.q[o][i].  dy, dx: fp32 or bf16.  The factors
  * dy * scale enter the matrix cores as the sum of two bfloat16, and of three, which hold all of their 24 bits (and take as much
- * longer), where dx is fp32.  Sums are fp32.  Infinities and NaN come out as the formula has them; parts of the result that
- * hold a NaN take a second time as long. */
+ * longer), where dx is fp32.  Sums are fp32.  Infinities and NaN come out as the formula has them; tiles of the result
+ * that hold a NaN are summed twice. */
 int stq_matmul_grad_input(stq_ctx* ctx, const stq_matrix* dy, const stq_matrix* w, const stq_matrix* dx, void* hip_stream);
 
 /* Gradient of w: dw[o][i] = sum over tokens of dy[token][o] * x.scales[token] * x.q[token][i], from the activations' codes as
