@@ -602,8 +602,8 @@ __global__ __launch_bounds__(WC * WI * WJ * 64) void grad_kernel(const MatmulArg
   if (threadIdx.x == 0) any_nan = 0;
   take(std::false_type{}, first);
   // A factor beyond bf16's largest number, as its first term an infinity, has made its whole row NaN: then the tile again, with LARGE terms,
-  // as long as before, or six times where that does not fit the registers (fp32 dy of odd sizes to fp32).  (In every step these would be 2 to 7 % of the time of dx 8192 x 4096 x 11008; so it is 0.2 %, and 1 to 3 %
-  // of the time of small results.)
+  // as long as before, or six times where that does not fit the registers (fp32 dy of odd sizes to fp32).  (In every step these would be
+  // 2 to 7 % of the time of dx 8192 x 4096 x 11008; so it is 0.2 %, and 1 to 3 % of the time of small results.)
   bool nan = false;
 #pragma unroll
   for (uint32_t e = 0; e < FI * FJ * 16; ++e) nan |= __builtin_isnan(acc[e / 16 / FJ][e / 16 % FJ][e % 16]);
