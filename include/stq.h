@@ -9,7 +9,9 @@
  * changes a layer's bit-width, the host-side decision itself, and the same loop
  * with the decision and the bit plan resident on the device (stq_engine_*).  Beside
  * it stand the operators of a layer whose weights and activations are held in 8 bits
- * (stq_quantize_rows ... stq_matmul_grad_weight), which make the step's gradients.
+ * (stq_quantize_rows ... stq_matmul_grad_weight), which make the step's gradients, the loss
+ * that they begin with (stq_cross_entropy, stq_cross_entropy_grad), and the norm and
+ * clipping of all gradients before the step (stq_grad_norm, stq_clip_grads).
  *
  * Conventions
  *   - Every function returns STQ_OK (0) or a negative STQ_E* code.  Nothing
@@ -230,6 +232,29 @@ int stq_step_transition(stq_ctx* ctx, const stq_tensor* tensors, uint32_t n,
 int stq_grad_stats(stq_ctx* ctx, const stq_tensor* tensors, uint32_t n, uint32_t block,
                    uint32_t grad_dtype, void* hip_stream);
 
+/* A gradient of stq_grad_norm and stq_clip_grads. */
+typedef struct {
+  const void* grad; /* device, fp32[numel] or bf16[numel], aligned to its elements (16 bytes are faster); NULL if numel is 0 */
+  void* out;        /* where stq_clip_grads writes it: grad itself or NULL (in place), or memory that overlaps no gradient */
+  uint64_t numel;   /* 0 is possible                                                              */
+  uint32_t dtype;   /* 0 = fp32, 1 = bf16: of each tensor by itself                               */
+} stq_grad;
+
+/* The global norm of n gradients (host array, read before the call returns; n may be 0, and not above the context's max_tensors):
+ *   norm[0] = the sum of the squares of all elements of all n,  norm[1] = its square root
+ * norm: device, double[2], 8-byte aligned, overwritten.  Squares and sums are fp64, where those of fp32 numbers neither overflow nor
+ * vanish: the sum is infinite or NaN only if an element is.  They are added in an order that depends on the sizes alone (the same calls
+ * give the same bits).  Asynchronous; a tensor table as of stq_step, which stq_clip_grads of the same arguments shares.  Where gradients
+ * are spread over several processes, their norm[0] can be added up in place before stq_clip_grads. */
+int stq_grad_norm(stq_ctx* ctx, const stq_grad* grads, uint32_t n, double* norm, void* hip_stream);
+
+/* Clip n gradients to a global norm of max_norm (> 0, finite):
+ *   c = max_norm / (sqrt(norm[0]) + 1e-6) in fp64, and in fp32 if it is below 1, else 1;  out = round(grad * c)
+ * norm: device, as stq_grad_norm leaves it; norm[0] alone is read (norm[1] may be anything).  The product is rounded to fp32, and for
+ * bf16 once more.  With c = 1 gradients that are clipped in place are neither read nor written, and others are copied.  A norm of
+ * infinity or NaN gives what the formula does: 0 (NaN for the infinities themselves), or NaN in every element. */
+int stq_clip_grads(stq_ctx* ctx, const stq_grad* grads, uint32_t n, const double* norm, double max_norm, void* hip_stream);
+
 /* Copy accumulators 0..n-1 to `out` (host, n entries), synchronise, and clear
  * them on the device.  Sums are order-dependent in the last bits; the maxima
  * are exact. */
@@ -430,6 +455,32 @@ int stq_matmul_grad_input(stq_ctx* ctx, const stq_matrix* dy, const stq_matrix* 
 int stq_matmul_grad_weight(stq_ctx* ctx, const stq_matrix* dy, const stq_matrix* x, const stq_matrix* dw, void* workspace,
                            uint64_t workspace_bytes, void* hip_stream);
 int stq_matmul_grad_weight_bytes(uint64_t tokens, uint64_t outputs, uint64_t inputs, uint64_t* bytes); /* host only */
+
+/* Softmax cross entropy of a classifier over 8-bit codes, without its logits in memory:
+ *   z[token][c] = x.scales[token] * w.scales[c] * sum over i of x.q[token][i] * w.q[c][i], in fp32 as stq_matmul's
+ *   lse[token] = log sum over the classes of exp(z),  loss[token] = lse - z[token][target]
+ * x: [tokens][in], w: [classes][in], both STQ_Q8 with block 0, in <= STQ_MAX_INNER.  targets: device, int64[tokens], 8-byte aligned.  A
+ * token of a negative target has a loss of 0; a target of `classes` or more gives a loss of NaN.  loss, lse: device, fp32[tokens].  The loss
+ * is log(1 + exp(d)), d = log sum over the other classes of exp(z) - z[token][target], so that it keeps its relative precision where
+ * the target's probability is next to 1.
+ * workspace: device, 16-byte aligned, of at least stq_cross_entropy_bytes bytes, free again when the call's work is done. */
+int stq_cross_entropy(stq_ctx* ctx, const stq_matrix* x, const stq_matrix* w, const int64_t* targets, float* loss, float* lse,
+                      void* workspace, uint64_t workspace_bytes, void* hip_stream);
+int stq_cross_entropy_bytes(uint64_t tokens, uint64_t classes, uint64_t inputs, uint64_t* bytes); /* host only */
+
+/* Its gradients.  loss, lse: as the forward pass left them; dloss: device, fp32[tokens], the gradients of the losses; dlse (may be NULL: zeros):
+ * those of lse.  With p = exp(z - lse) and
+ *   g[token][c] = (dloss + dlse) * p, at the target dlse * p + dloss * (p - 1), where p - 1 is taken from the loss
+ *   dx[token][i] = sum over c of g[token][c] * w.scales[c] * w.q[c][i],  dw[c][i] = sum over tokens of g[token][c] * x.scales[token] * x.q[token][i]
+ * dx, dw: fp32 or bf16, each of its own type, overwritten; one of them may be NULL.  For a token without a target dloss is taken as 0.  A
+ * token whose dloss and dlse are both 0 (as every one without a target, if dlse is NULL) has a dx of 0 and no part in dw, whatever its logits
+ * are; a target of `classes` or more makes dx of its token and all of dw NaN.
+ * The classes are taken in pieces: g of a piece lies in the workspace in fp32.  An exponential below 2^-126 may come out as 0.
+ * workspace: device, 16-byte aligned, of at least stq_cross_entropy_grad_bytes bytes, free again when the call's work is done. */
+int stq_cross_entropy_grad(stq_ctx* ctx, const stq_matrix* x, const stq_matrix* w, const int64_t* targets, const float* loss,
+                           const float* lse, const float* dloss, const float* dlse, const stq_matrix* dx, const stq_matrix* dw,
+                           void* workspace, uint64_t workspace_bytes, void* hip_stream);
+int stq_cross_entropy_grad_bytes(uint64_t tokens, uint64_t classes, uint64_t inputs, uint64_t* bytes); /* host only */
 
 /* The library's own quantizer tables, for inspection (host only, no context):
  *   which 0: G[j] = fl32(2^(-j/32)), j < 511 (bits ignored)

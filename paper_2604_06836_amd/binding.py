@@ -78,6 +78,10 @@ TENSOR_DTYPE = np.dtype([("param", "<u8"), ("grad", "<u8"), ("numel", "<u8"), ("
 BITS_DTYPE = np.dtype([("m_bits", "u1"), ("v_bits", "u1")])
 
 
+class Grad(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("numel", C.c_uint64), ("dtype", C.c_uint32)]
+
+
 class Codes(C.Structure):
     _fields_ = [("m_codes", C.c_void_p), ("v_codes", C.c_void_p)]
 
@@ -87,11 +91,12 @@ class Matrix(C.Structure):
                 ("stride", C.c_uint64), ("dtype", C.c_uint32), ("block", C.c_uint32)]
 
 
-EXPORTS = ["stq_init", "stq_set_schedule", "stq_destroy", "stq_state_bytes", "stq_zero_state", "stq_step", "stq_step_static", "stq_step_transition", "stq_grad_stats", "stq_stats",
+EXPORTS = ["stq_init", "stq_set_schedule", "stq_destroy", "stq_state_bytes", "stq_zero_state", "stq_step", "stq_step_static", "stq_step_transition", "stq_grad_stats", "stq_grad_norm", "stq_clip_grads", "stq_stats",
            "stq_repack", "stq_repack_many", "stq_decide", "stq_decide_due", "stq_engine_create", "stq_engine_set_next", "stq_engine_step",
            "stq_engine_read", "stq_engine_destroy", "stq_quantize_rows", "stq_dequantize_rows", "stq_rms_norm", "stq_rms_norm_grad",
            "stq_rms_norm_grad_bytes", "stq_gated_silu", "stq_gated_silu_grad", "stq_matmul", "stq_matmul_grad_input",
-           "stq_matmul_grad_weight", "stq_matmul_grad_weight_bytes", "stq_table", "stq_strerror"]
+           "stq_matmul_grad_weight", "stq_matmul_grad_weight_bytes", "stq_cross_entropy", "stq_cross_entropy_bytes", "stq_cross_entropy_grad",
+           "stq_cross_entropy_grad_bytes", "stq_table", "stq_strerror"]
 
 _lib = None
 
@@ -119,6 +124,8 @@ def load_library():
     L.stq_step_transition.argtypes = [vp, C.POINTER(Tensor), u32, C.POINTER(Bits), C.POINTER(Bits),
                                       C.POINTER(Codes), C.POINTER(HParams), vp]
     L.stq_grad_stats.argtypes = [vp, C.POINTER(Tensor), u32, u32, u32, vp]
+    L.stq_grad_norm.argtypes = [vp, C.POINTER(Grad), u32, vp, vp]
+    L.stq_clip_grads.argtypes = [vp, C.POINTER(Grad), u32, vp, C.c_double, vp]
     L.stq_stats.argtypes = [vp, C.POINTER(LayerStats), u32, vp]
     L.stq_repack.argtypes = [vp, u64, u32, C.c_int, vp, u32, vp, u32, vp]
     L.stq_repack_many.argtypes = [vp, C.POINTER(RepackJob), u32, u32, vp]
@@ -145,6 +152,10 @@ def load_library():
     L.stq_matmul_grad_input.argtypes = [vp, mat, mat, mat, vp]
     L.stq_matmul_grad_weight.argtypes = [vp, mat, mat, mat, vp, u64, vp]
     L.stq_matmul_grad_weight_bytes.argtypes = [u64, u64, u64, C.POINTER(u64)]
+    L.stq_cross_entropy.argtypes = [vp, mat, mat, vp, vp, vp, vp, u64, vp]
+    L.stq_cross_entropy_bytes.argtypes = [u64, u64, u64, C.POINTER(u64)]
+    L.stq_cross_entropy_grad.argtypes = [vp, mat, mat, vp, vp, vp, vp, vp, mat, mat, vp, u64, vp]
+    L.stq_cross_entropy_grad_bytes.argtypes = [u64, u64, u64, C.POINTER(u64)]
     for name in EXPORTS[:-1]:
         getattr(L, name).restype = C.c_int
     L.stq_strerror.argtypes = [C.c_int]
@@ -220,6 +231,29 @@ def matmul_grad_weight_bytes(tokens: int, outputs: int, inputs: int) -> int:
     return n.value
 
 
+def cross_entropy_bytes(tokens: int, classes: int, inputs: int) -> int:
+    """Bytes of workspace that Context.cross_entropy needs."""
+    n = C.c_uint64()
+    _check(load_library().stq_cross_entropy_bytes(tokens, classes, inputs, C.byref(n)), "stq_cross_entropy_bytes")
+    return n.value
+
+
+def cross_entropy_grad_bytes(tokens: int, classes: int, inputs: int) -> int:
+    """Bytes of workspace that Context.cross_entropy_grad needs."""
+    n = C.c_uint64()
+    _check(load_library().stq_cross_entropy_grad_bytes(tokens, classes, inputs, C.byref(n)), "stq_cross_entropy_grad_bytes")
+    return n.value
+
+
+def make_grads(items: Iterable[dict]):
+    """items: dicts with grad (address), numel, dtype (STQ_F32 or STQ_BF16) and, for clipping to another place, out (address)."""
+    items = list(items)
+    arr = (Grad * len(items))()
+    for a, it in zip(arr, items):
+        a.grad, a.out, a.numel, a.dtype = it.get("grad"), it.get("out"), it["numel"], it["dtype"]
+    return arr
+
+
 def decide_due(step: int, update_every: int) -> bool:
     return bool(load_library().stq_decide_due(step, update_every))
 
@@ -287,6 +321,13 @@ class Context:
         _check(self._lib.stq_grad_stats(self._h, tensors, len(tensors), block, grad_dtype, C.c_void_p(stream)),
                "stq_grad_stats")
 
+    def grad_norm(self, grads, norm: int, stream: int = 0):
+        """grads: from make_grads; norm: address of two doubles on the device, the sum of squares and its root."""
+        _check(self._lib.stq_grad_norm(self._h, grads, len(grads), norm, C.c_void_p(stream)), "stq_grad_norm")
+
+    def clip_grads(self, grads, norm: int, max_norm: float, stream: int = 0):
+        _check(self._lib.stq_clip_grads(self._h, grads, len(grads), norm, max_norm, C.c_void_p(stream)), "stq_clip_grads")
+
     def stats(self, n: int, stream: int = 0):
         out = (LayerStats * n)()
         _check(self._lib.stq_stats(self._h, out, n, C.c_void_p(stream)), "stq_stats")
@@ -342,6 +383,16 @@ class Context:
     def matmul_grad_weight(self, dy: Matrix, x: Matrix, dw: Matrix, workspace: Optional[int] = None,
                            workspace_bytes: int = 0, stream: int = 0):
         _check(self._lib.stq_matmul_grad_weight(self._h, dy, x, dw, workspace, workspace_bytes, stream), "stq_matmul_grad_weight")
+
+    def cross_entropy(self, x: Matrix, w: Matrix, targets: int, loss: int, lse: int, workspace: Optional[int], workspace_bytes: int,
+                      stream: int = 0):
+        """targets: address of int64[tokens]; loss, lse: of fp32[tokens]."""
+        _check(self._lib.stq_cross_entropy(self._h, x, w, targets, loss, lse, workspace, workspace_bytes, stream), "stq_cross_entropy")
+
+    def cross_entropy_grad(self, x: Matrix, w: Matrix, targets: int, loss: int, lse: int, dloss: int, dlse: Optional[int], dx: Optional[Matrix],
+                           dw: Optional[Matrix], workspace: Optional[int], workspace_bytes: int, stream: int = 0):
+        _check(self._lib.stq_cross_entropy_grad(self._h, x, w, targets, loss, lse, dloss, dlse, dx, dw, workspace, workspace_bytes, stream),
+               "stq_cross_entropy_grad")
 
     def engine(self, tensors, second, plan, capacity_bits: int, block: int, *, alpha=0.1, tau=1000.0, phi=7.2,
                eps=1e-12, v_offset=0.0, flags=0, thr=(6.8, 12.0, 24.0), bits=(4, 8, 16, 32),

@@ -157,6 +157,8 @@ int stq_init(stq_ctx** out, int device, uint32_t max_tensors) {
   ok = ok && hipMalloc(&c->d_stats, sizeof(double) * kStatSlots * max_tensors) == hipSuccess;
   ok = ok && hipMalloc(&c->d_sched, 4 * kSchedWords * (kRecordedTable + 1)) == hipSuccess;
   ok = ok && hipMemset(c->d_sched, 0, 4 * kSchedWords * (kRecordedTable + 1)) == hipSuccess;
+  ok = ok && hipMalloc(&c->d_norm, sizeof(double) * kNormWords * (kRecordedTable + 1)) == hipSuccess;
+  ok = ok && hipMemset(c->d_norm, 0, sizeof(double) * kNormWords * (kRecordedTable + 1)) == hipSuccess;
   ok = ok && hipHostMalloc(&c->h_stats, sizeof(double) * kStatSlots * max_tensors, hipHostMallocDefault) == hipSuccess;
   ok = ok && hipHostMalloc(&c->h_stage, sizeof(TensorDesc) * max_tensors * kRing, hipHostMallocDefault) == hipSuccess;
   ok = ok && hipHostMalloc(&c->h_jobs, sizeof(RepackJob) * 2 * max_tensors * kRing, hipHostMallocDefault) == hipSuccess;
@@ -202,6 +204,7 @@ int stq_destroy(stq_ctx* c) {
   if (c->d_desc[0]) (void)hipFree(c->d_desc[0]);
   if (c->d_stats) (void)hipFree(c->d_stats);
   if (c->d_sched) (void)hipFree(c->d_sched);
+  if (c->d_norm) (void)hipFree(c->d_norm);
   if (c->h_stats) (void)hipHostFree(c->h_stats);
   if (c->d_luts) (void)hipFree(c->d_luts);
   if (c->d_jobs) (void)hipFree(c->d_jobs);
@@ -389,6 +392,32 @@ int mode_of(const TensorDesc* descs, uint32_t n, bool changes) {
   return changes ? 1 : 0;
 }
 
+// Descriptors of n gradients (n > 0), and their tiles.
+int build_grads(stq_ctx* ctx, const stq_grad* g, uint32_t n, uint32_t* total_tiles) {
+  if (!g || n > ctx->max_tensors) return STQ_EINVAL;
+  ctx->descs.resize(n);
+  uint64_t tiles = 0;
+  for (uint32_t l = 0; l < n; ++l) {
+    if (g[l].dtype > 1) return STQ_EDTYPE;
+    if (g[l].numel && !g[l].grad) return STQ_EINVAL;
+    const uintptr_t size = g[l].dtype ? 2 : 4;
+    if (!aligned(g[l].grad, size) || !aligned(g[l].out, size)) return STQ_EALIGN;
+    const uint64_t nt = g[l].numel / kTile + (g[l].numel % kTile != 0);
+    if (nt > 0xFFFFFFFFull || tiles + nt > 0xFFFFFFFFull) return STQ_EINVAL;
+    TensorDesc& d = ctx->descs[l];
+    d = TensorDesc{};
+    d.grad = g[l].grad;
+    d.param = static_cast<float*>(g[l].out ? g[l].out : const_cast<void*>(g[l].grad));
+    d.numel = g[l].numel;
+    d.tile_begin = static_cast<uint32_t>(tiles);
+    d.n_tiles = static_cast<uint32_t>(nt);
+    d.bm = g[l].dtype;
+    tiles += nt;
+  }
+  *total_tiles = static_cast<uint32_t>(tiles);
+  return STQ_OK;
+}
+
 // One launch of the step kernel.  new_plan/new_codes are null for the in-place step.
 int step_impl(stq_ctx* ctx, const stq_tensor* tensors, uint32_t n, const stq_bits* plan,
               const stq_bits* new_plan, const stq_codes* new_codes, const stq_hparams* hp, void* stream) {
@@ -492,6 +521,36 @@ int stq_grad_stats(stq_ctx* ctx, const stq_tensor* tensors, uint32_t n, uint32_t
     return STQ_EHIP;
   for (uint32_t l = 0; l < n; ++l) ctx->stat_count[l] += tensors[l].numel;
   return STQ_OK;
+}
+
+int stq_grad_norm(stq_ctx* ctx, const stq_grad* grads, uint32_t n, double* norm, void* stream) {
+  if (!ctx || !norm) return STQ_EINVAL;
+  if (!aligned(norm, 8)) return STQ_EALIGN;
+  uint32_t total = 0;
+  int table = 0;
+  if (n)
+    if (int e = build_grads(ctx, grads, n, &total)) return e;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return STQ_EHIP;
+  if (total)
+    if (int e = resident_table(ctx, ctx->descs, static_cast<hipStream_t>(stream), &table)) return e;
+  return launch_grad_norm(ctx->d_desc[table], n, total, ctx->d_norm + static_cast<size_t>(table) * kNormWords, norm, ctx->n_cu, stream) == 0
+             ? STQ_OK : STQ_EHIP;
+}
+
+int stq_clip_grads(stq_ctx* ctx, const stq_grad* grads, uint32_t n, const double* norm, double max_norm, void* stream) {
+  if (!ctx || !norm) return STQ_EINVAL;
+  if (!aligned(norm, 8)) return STQ_EALIGN;
+  if (!(max_norm > 0.0) || !std::isfinite(max_norm)) return STQ_EINVAL;
+  if (n == 0) return STQ_OK;
+  uint32_t total = 0;
+  int table = 0;
+  if (int e = build_grads(ctx, grads, n, &total)) return e;
+  if (total == 0) return STQ_OK;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return STQ_EHIP;
+  if (int e = resident_table(ctx, ctx->descs, static_cast<hipStream_t>(stream), &table)) return e;
+  return launch_clip(ctx->d_desc[table], n, total, norm, max_norm, ctx->n_cu, stream) == 0 ? STQ_OK : STQ_EHIP;
 }
 
 int stq_stats(stq_ctx* ctx, stq_layer_stats* out, uint32_t n, void* stream) {

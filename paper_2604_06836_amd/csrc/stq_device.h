@@ -93,6 +93,11 @@ constexpr uint64_t kRepackOnceBytes = 350ull << 20;  // see launch_repack_many
 int launch_repack_many(RepackManyArgs a, uint64_t code_bytes, void* stream);  // code_bytes: read and written
 int launch_grad_stats(const TensorDesc* desc, uint32_t n_tensors, uint32_t total_tiles, double* stats, bool grad_bf16,
                       uint32_t n_cu, void* stream);
+// The norm's sums: kNormGroups doubles and a counter (zero between launches) in kNormWords doubles at `partial`.  Descriptors of
+// gradients: grad, param (where a clipped one goes, never null), numel, bm = 1 for bf16.
+constexpr uint32_t kNormGroups = 2048, kNormWords = kNormGroups + 32;
+int launch_grad_norm(const TensorDesc* desc, uint32_t n_tensors, uint32_t total_tiles, double* partial, double* norm, uint32_t n_cu, void* stream);
+int launch_clip(const TensorDesc* desc, uint32_t n_tensors, uint32_t total_tiles, const double* norm, double most, uint32_t n_cu, void* stream);
 int launch_take_stats(double* host, double* acc, uint64_t n, void* stream);
 int launch_upload(void* dst, const void* pinned, uint64_t bytes, void* stream);  // a multiple of 16 bytes
 int launch_upload_by_value(void* dst, const void* host, uint64_t bytes, void* stream);  // the same, for a stream being recorded

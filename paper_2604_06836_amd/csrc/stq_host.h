@@ -32,6 +32,7 @@ struct stq_ctx {
   double* d_stats = nullptr;
   uint32_t* d_sched = nullptr;   // ticket counters of the step kernel (zero between launches), kSchedWords for each of d_desc:
                                  // launches that overlap although they should not then have counters of their own
+  double* d_norm = nullptr;      // sums of stq_grad_norm, kNormWords for each of d_desc
   stq::TensorDesc* h_stage = nullptr;        // pinned, kRing slots of max_tensors
   hipEvent_t stage_done[stq::kRingGroups] = {};
   int ring_pos = 0;

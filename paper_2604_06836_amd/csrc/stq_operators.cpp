@@ -257,4 +257,84 @@ int stq_matmul_grad_weight(stq_ctx* ctx, const stq_matrix* dy, const stq_matrix*
   return launched(launch_matmul_grad_weight(a, dy->dtype, dw->dtype, need ? static_cast<float*>(workspace) : nullptr, stream));
 }
 
+int stq_cross_entropy_bytes(uint64_t tokens, uint64_t classes, uint64_t inputs, uint64_t* bytes) {
+  if (!bytes) return STQ_EINVAL;
+  if (tokens > kMost || classes == 0 || classes > kMost || inputs == 0 || inputs > STQ_MAX_INNER) return STQ_ESHAPE;
+  *bytes = loss_bytes(tokens, classes);
+  return STQ_OK;
+}
+
+int stq_cross_entropy(stq_ctx* ctx, const stq_matrix* x, const stq_matrix* w, const int64_t* targets, float* loss, float* lse,
+                      void* workspace, uint64_t workspace_bytes, void* stream) {
+  if (!ctx) return STQ_EINVAL;
+  if (int e = check_size(x)) return e;
+  if (int e = check_size(w)) return e;
+  if (w->rows == 0 || x->cols > STQ_MAX_INNER) return STQ_ESHAPE;
+  LossArgs a;
+  if (int e = take(x, codes(x->rows, x->cols, true), &a.x)) return e;
+  if (int e = take(w, codes(w->rows, x->cols, true), &a.w)) return e;
+  if (!x->rows) return STQ_OK;
+  if (int e = check_buffer(targets, 8)) return e;
+  if (int e = check_buffer(loss, 4)) return e;
+  if (int e = check_buffer(lse, 4)) return e;
+  uint64_t need = 0;
+  if (int e = stq_cross_entropy_bytes(x->rows, w->rows, x->cols, &need)) return e;
+  if (workspace_bytes < need) return STQ_EINVAL;
+  if (int e = check_buffer(workspace, 16)) return e;
+  a.targets = targets;
+  a.loss = loss;
+  a.lse = lse;
+  a.tokens = static_cast<uint32_t>(x->rows);
+  a.classes = static_cast<uint32_t>(w->rows);
+  a.inputs = static_cast<uint32_t>(x->cols);
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return STQ_EHIP;
+  return launched(launch_loss(a, workspace, ctx->n_cu, stream));
+}
+
+int stq_cross_entropy_grad_bytes(uint64_t tokens, uint64_t classes, uint64_t inputs, uint64_t* bytes) {
+  if (!bytes) return STQ_EINVAL;
+  if (tokens > kMost || classes == 0 || classes > kMost || inputs == 0 || inputs > STQ_MAX_INNER) return STQ_ESHAPE;
+  *bytes = loss_grad_bytes(tokens, classes, inputs);
+  return STQ_OK;
+}
+
+int stq_cross_entropy_grad(stq_ctx* ctx, const stq_matrix* x, const stq_matrix* w, const int64_t* targets, const float* loss,
+                           const float* lse, const float* dloss, const float* dlse, const stq_matrix* dx, const stq_matrix* dw,
+                           void* workspace, uint64_t workspace_bytes, void* stream) {
+  if (!ctx) return STQ_EINVAL;
+  if (int e = check_size(x)) return e;
+  if (int e = check_size(w)) return e;
+  if (w->rows == 0 || x->cols > STQ_MAX_INNER) return STQ_ESHAPE;
+  LossGradArgs a{};
+  if (int e = take(x, codes(x->rows, x->cols, true), &a.x)) return e;
+  if (int e = take(w, codes(w->rows, x->cols, true), &a.w)) return e;
+  if (!dx && !dw) return STQ_EINVAL;
+  if (int e = take_optional(dx, floats(x->rows, x->cols), &a.dx)) return e;
+  if (int e = take_optional(dw, floats(w->rows, x->cols), &a.dw)) return e;
+  if (x->rows) {
+    if (int e = check_buffer(targets, 8)) return e;
+    if (int e = check_buffer(loss, 4)) return e;
+    if (int e = check_buffer(lse, 4)) return e;
+    if (int e = check_buffer(dloss, 4)) return e;
+    if (!aligned(dlse, 4)) return STQ_EALIGN;
+    uint64_t need = 0;
+    if (int e = stq_cross_entropy_grad_bytes(x->rows, w->rows, x->cols, &need)) return e;
+    if (workspace_bytes < need) return STQ_EINVAL;
+    if (int e = check_buffer(workspace, 16)) return e;
+  }
+  a.targets = targets;
+  a.loss = loss;
+  a.lse = lse;
+  a.dloss = dloss;
+  a.dlse = dlse;
+  a.tokens = static_cast<uint32_t>(x->rows);
+  a.classes = static_cast<uint32_t>(w->rows);
+  a.inputs = static_cast<uint32_t>(x->cols);
+  if (!a.tokens && !dw) return STQ_OK;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return STQ_EHIP;
+  return launched(launch_loss_grad(a, dx ? dx->dtype : 0u, dw ? dw->dtype : 0u, workspace, ctx->n_cu, stream));
+}
+
 }  // extern "C"

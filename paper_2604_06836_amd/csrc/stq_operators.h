@@ -48,6 +48,26 @@ struct MatmulArgs {
   uint32_t m, n, k;
 };
 
+// The cross entropy: x [tokens][inputs] and w [classes][inputs] in codes.
+struct LossArgs {
+  Mat x, w;
+  const int64_t* targets;
+  float* loss;
+  float* lse;
+  uint32_t tokens, classes, inputs;
+};
+struct LossGradArgs {
+  Mat x, w, dx, dw;  // dx or dw with p null: not there
+  const int64_t* targets;
+  const float* loss;
+  const float* lse;
+  const float* dloss;
+  const float* dlse;  // or null
+  void* token;    // parts of the workspace, set by the launcher
+  float* scale;
+  uint32_t tokens, classes, inputs;
+};
+
 // Workgroups of the norm's gradients, each of which leaves a part of dweight: as many as have 16 waves on each of 256 CUs.
 inline uint32_t norm_grad_groups(uint64_t rows, uint32_t cols) {
   const uint64_t at_once = cols <= 512 ? 4 : 1, need = (rows + at_once - 1) / at_once;  // (rows of a workgroup, see with_rows)
@@ -66,5 +86,9 @@ int launch_matmul(const MatmulArgs& a, uint32_t out_type, uint32_t n_cu, void* s
 int launch_matmul_grad_input(const MatmulArgs& a, uint32_t dy_type, uint32_t out_type, void* stream);
 int launch_matmul_grad_weight(const MatmulArgs& a, uint32_t dy_type, uint32_t out_type, float* workspace, void* stream);
 uint64_t grad_weight_bytes(uint64_t m, uint64_t n, uint64_t k);
+int launch_loss(const LossArgs& a, void* workspace, uint32_t n_cu, void* stream);
+uint64_t loss_bytes(uint64_t tokens, uint64_t classes);
+int launch_loss_grad(LossGradArgs a, uint32_t dx_type, uint32_t dw_type, void* workspace, uint32_t n_cu, void* stream);
+uint64_t loss_grad_bytes(uint64_t tokens, uint64_t classes, uint64_t inputs);
 
 }  // namespace stq
