@@ -4,7 +4,7 @@
 
 #include <cstdint>
 
-#include "stq_vectors.h"
+#include "stq_tiles.h"
 
 #pragma clang fp contract(off)
 
@@ -12,7 +12,7 @@ namespace stq {
 namespace {
 
 constexpr uint32_t kNoTarget = 0xFFFFFFFFu;
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // The class of a token's target, or kNoTarget; one beyond the classes comes out as no class either, and is told apart by `beyond`.
 __device__ __forceinline__ uint32_t target_of(const int64_t* targets, uint32_t token, uint32_t classes, bool* beyond) {
@@ -21,62 +21,153 @@ __device__ __forceinline__ uint32_t target_of(const int64_t* targets, uint32_t t
   return t < 0 || *beyond ? kNoTarget : static_cast<uint32_t>(t);
 }
 
-// Largest element and sum over a workgroup of four waves.
-__device__ __forceinline__ float group_max(float x, float* held) {
-  for (int o = 1; o < 64; o *= 2) x = fmaxf(x, __shfl_xor(x, o));
-  if ((threadIdx.x & 63) == 0) held[threadIdx.x >> 6] = x;
-  __syncthreads();
-  x = fmaxf(fmaxf(held[0], held[1]), fmaxf(held[2], held[3]));
-  __syncthreads();
-  return x;
-}
-__device__ __forceinline__ float group_sum(float x, float* held) {
-  for (int o = 1; o < 64; o *= 2) x += __shfl_xor(x, o);
-  if ((threadIdx.x & 63) == 0) held[threadIdx.x >> 6] = x;
-  __syncthreads();
-  x = (held[0] + held[1]) + (held[2] + held[3]);
-  __syncthreads();
-  return x;
-}
-
-// A workgroup to a token's logits of a piece, classes first .. first + n - 1: their maximum and the sum of exp(z - maximum), both without
-// the target, and the target's logit if it is one of them.
-__global__ __launch_bounds__(256) void piece_kernel(const float* z, uint32_t first, uint32_t n, uint32_t classes, const int64_t* targets, float2* part, float* at_target) {
-  __shared__ float held[4];
-  const uint32_t token = blockIdx.x;
-  bool beyond;
-  const uint32_t target = target_of(targets, token, classes, &beyond) - first;
-  const STQ_GLOBAL float* row = as_global(z) + static_cast<uint64_t>(token) * n;
-  float most = -INFINITY;
-  bool nan = false;
-  for (uint32_t c = threadIdx.x; c < n; c += 256) {
-    const float x = row[c];
-    nan |= __builtin_isnan(x);
-    if (c == target) at_target[token] = x;
-    else most = fmaxf(most, x);
+// Several sums of exponentials, each (maximum, sum of exp2(z - maximum)), as one.
+template <class P>
+__device__ __forceinline__ float2 joined(P part, uint64_t apart, uint32_t n) {
+  float most = -INFINITY, sum = 0.0f;
+  for (uint32_t k = 0; k < n; ++k) most = fmaxf(most, part[k * apart].x);
+  for (uint32_t k = 0; k < n; ++k) {
+    const float2 v = part[k * apart];
+    sum += v.y * (v.x == most ? 1.0f : __builtin_amdgcn_exp2f(v.x - most));
   }
-  most = group_max(most, held);
-  float sum = 0.0f;
-  for (uint32_t c = threadIdx.x; c < n; c += 256)
-    if (c != target) sum += __builtin_amdgcn_exp2f((row[c] - most) * kLog2e);
-  if (nan) sum = NAN;
-  sum = group_sum(sum, held);
-  if (threadIdx.x == 0) part[token] = make_float2(most, most == -INFINITY && !__builtin_isnan(sum) ? 0.0f : sum);
+  return make_float2(most, sum);
 }
 
-// The parts of each token's sum in one order, its loss and its log-sum.
+// ---------------------------------------------------------------------------------------------- the loss
+// A tile of the logits stays in registers and leaves, for each of its tokens, a maximum (times log2 e) and the sum of exp(z - maximum),
+// both without the target's logit, which goes to at_target.  By itself, in front of the products' 1870 us at 16384 x 32000 x 4096, that is
+// a seventh of the tile's time.
+template <int TM, int TN, int WM, int WN, bool PIECES>
+__global__ __launch_bounds__(WM * WN * 64) void loss_tile_kernel(const MatmulArgs a, const int64_t* targets, float2* part, float* at_target, uint32_t tiles_m,
+                                                                 uint32_t tiles_n) {
+  constexpr uint32_t FM = TM / WM / 32, FN = TN / WN / 32;
+  code_tile<TM, TN, WM, WN, PIECES>(a, tiles_m, tiles_n, [&](const auto& acc, const CodeTile& t) __attribute__((always_inline)) {
+    float2* const held = reinterpret_cast<float2*>(t.room);  // [WN][TM]
+    const uint32_t half = t.lane >> 5, first = t.n0 + t.wn + 4 * half, there = a.n - t.n0 - t.wn;  // (beyond the classes: above 2^31)
+#pragma unroll
+    for (uint32_t i = 0; i < FM; ++i) {
+      const uint32_t row = t.wm + i * 32 + (t.lane & 31), token = t.m0 + row;
+      bool beyond;
+      const uint32_t at = target_of(targets, min(token, a.m - 1), a.n, &beyond) - first;  // column 32 j + 8 p + e of the lane's
+      const float s = t.sm[row];
+      float z[FN * 16];
+#pragma unroll
+      for (uint32_t j = 0; j < FN; ++j)
+#pragma unroll
+        for (uint32_t k = 0; k < 16; ++k) z[j * 16 + k] = static_cast<float>(acc[i][j][k]) * s * t.sn[t.wn + 4 * half + j * 32 + k / 4 * 8 + k % 4];
+      if (there < FN * 32 || static_cast<int32_t>(there) < 0) {
+#pragma unroll
+        for (uint32_t k = 0; k < FN * 16; ++k)
+          if (first + k / 16 * 32 + k % 16 / 4 * 8 + k % 4 >= a.n) z[k] = -INFINITY;
+      }
+      if (__builtin_amdgcn_ballot_w64(at < FN * 32)) {
+#pragma unroll
+        for (uint32_t k = 0; k < FN * 16; ++k)
+          if (at == k / 16 * 32 + k % 16 / 4 * 8 + k % 4) {
+            if (token < a.m) at_target[token] = z[k];
+            z[k] = -INFINITY;
+          }
+      }
+      float most = z[0];
+#pragma unroll
+      for (uint32_t k = 1; k < FN * 16; ++k) most = fmaxf(most, z[k]);
+      most = fmaxf(most, __shfl_xor(most, 32));
+      const float top = most * kLog2e, ref = most == -INFINITY ? 0.0f : top;
+      float sum = 0.0f;
+#pragma unroll
+      for (uint32_t k = 0; k < FN * 16; ++k) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(z[k], kLog2e, -ref));
+      sum += __shfl_xor(sum, 32);
+      if (half == 0) held[t.wave % WN * TM + row] = make_float2(top, sum);
+    }
+    __syncthreads();
+    for (uint32_t r = threadIdx.x; r < TM; r += WM * WN * 64) {
+      const float2 v = joined(held + r, TM, WN);
+      if (t.m0 + r < a.m) part[static_cast<uint64_t>(t.n0 / TN) * a.m + t.m0 + r] = v;
+    }
+  });
+}
+
+// Few tokens: sixteen classes to a part.
+template <int G, int R, int A>
+__global__ __launch_bounds__(512) void loss_few_kernel(const MatmulArgs a, const int64_t* targets, float2* part, float* at_target) {
+  code_few<G, R, A>(a, [&](const v4i& sum, uint32_t m, uint32_t n) __attribute__((always_inline)) {
+    const uint32_t token = min(m, a.m - 1);
+    const float s = as_global(a.a.s)[token];
+    bool beyond;
+    const uint32_t target = target_of(targets, token, a.n, &beyond);
+    float z[4];
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) z[e] = static_cast<float>(sum[e]) * s * as_global(a.b.s)[min(n + e, a.n - 1)];
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) {
+      if (n + e == target && m < a.m) at_target[token] = z[e];
+      if (n + e >= a.n || n + e == target) z[e] = -INFINITY;
+    }
+    float most = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    const float top = most * kLog2e, ref = most == -INFINITY ? 0.0f : top;
+    float all = 0.0f;
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) all += __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], kLog2e, -ref));
+    all += __shfl_xor(all, 16);
+    all += __shfl_xor(all, 32);
+    if ((threadIdx.x & 63) < 16 && m < a.m && n < a.n) part[static_cast<uint64_t>(n / 16) * a.m + m] = make_float2(top, all);
+  });
+}
+
+// Operands of fewer than 16 codes, or of rows too far apart for the offsets of a tile: 256 classes of a token to a workgroup, a logit to a thread.
+__device__ __forceinline__ float logit(const MatmulArgs& a, uint64_t m, uint64_t n) {
+  const STQ_GLOBAL int8_t* x = as_global(static_cast<const int8_t*>(a.a.p)) + m * a.a.stride;
+  const STQ_GLOBAL int8_t* w = as_global(static_cast<const int8_t*>(a.b.p)) + n * a.b.stride;
+  int32_t sum = 0;
+  for (uint32_t k = 0; k < a.k; ++k) sum += x[k] * w[k];
+  return static_cast<float>(sum) * as_global(a.a.s)[m] * as_global(a.b.s)[n];
+}
+__global__ __launch_bounds__(256) void loss_each_kernel(const MatmulArgs a, const int64_t* targets, float2* part, float* at_target, uint32_t groups_n) {
+  __shared__ float2 held[4];
+  const uint64_t groups = static_cast<uint64_t>(a.m) * groups_n;
+  for (uint64_t g = blockIdx.x; g < groups; g += gridDim.x) {
+    const uint32_t token = static_cast<uint32_t>(g / groups_n), c = static_cast<uint32_t>(g % groups_n) * 256 + threadIdx.x;
+    bool beyond;
+    const uint32_t target = target_of(targets, token, a.n, &beyond);
+    float z = c < a.n ? logit(a, token, c) : -INFINITY;
+    if (c < a.n && c == target) {
+      at_target[token] = z;
+      z = -INFINITY;
+    }
+    float most = z;
+    for (int o = 1; o < 64; o *= 2) most = fmaxf(most, __shfl_xor(most, o));
+    const float top = most * kLog2e, ref = most == -INFINITY ? 0.0f : top;
+    float sum = __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, -ref));
+    for (int o = 1; o < 64; o *= 2) sum += __shfl_xor(sum, o);
+    if ((threadIdx.x & 63) == 0) held[threadIdx.x >> 6] = make_float2(top, sum);
+    __syncthreads();
+    if (threadIdx.x == 0) part[(g % groups_n) * a.m + token] = joined(held, 1, 4);
+    __syncthreads();
+  }
+}
+
+// The parts of each token's sum, its loss and its log-sum.  Q threads of a workgroup share a token's parts.
+template <uint32_t Q>
 __global__ __launch_bounds__(256) void join_kernel(const float2* part, const float* at_target, uint32_t parts, uint32_t tokens, uint32_t classes, const int64_t* targets,
                                                    float* loss, float* lse) {
-  const uint32_t token = blockIdx.x * 256 + threadIdx.x;
-  if (token >= tokens) return;
-  float most = -INFINITY;
-  for (uint32_t p = 0; p < parts; ++p) most = fmaxf(most, part[static_cast<uint64_t>(p) * tokens + token].x);
-  float sum = 0.0f;
-  for (uint32_t p = 0; p < parts; ++p) {
-    const float2 v = part[static_cast<uint64_t>(p) * tokens + token];
-    sum += v.y * (v.x == most ? 1.0f : __builtin_amdgcn_exp2f((v.x - most) * kLog2e));
+  constexpr uint32_t kTokens = 256 / Q;
+  __shared__ float2 held[256];
+  const uint32_t turn = threadIdx.x / kTokens, token = blockIdx.x * kTokens + threadIdx.x % kTokens;
+  if (token < tokens && turn < parts) held[threadIdx.x] = joined(part + static_cast<uint64_t>(turn) * tokens + token, static_cast<uint64_t>(Q) * tokens, (parts - turn + Q - 1) / Q);
+  else held[threadIdx.x] = make_float2(-INFINITY, 0.0f);
+  __syncthreads();
+  if (Q >= 64) {  // (in two steps)
+    float2 v;
+    if (threadIdx.x < 16 * kTokens) v = joined(held + threadIdx.x, 16 * kTokens, Q / 16);
+    __syncthreads();
+    if (threadIdx.x < 16 * kTokens) held[threadIdx.x] = v;
+    __syncthreads();
   }
-  const float others = sum == 0.0f ? -INFINITY : most + logf(sum);
+  if (turn || token >= tokens) return;
+  const float2 v = joined(held + threadIdx.x, kTokens, Q < 16 ? Q : 16);
+  const float others = v.y == 0.0f ? -INFINITY : (v.x + log2f(v.y)) * kLn2;
   bool beyond;
   if (target_of(targets, token, classes, &beyond) == kNoTarget) {
     lse[token] = others;
@@ -166,25 +257,51 @@ Mat rows_from(const Mat& m, uint64_t row) {
 
 }  // namespace
 
+// The least classes of a part of a token's sum.
+constexpr uint32_t kFewTokens = 64;
+uint32_t least_part(uint64_t tokens) { return tokens <= kFewTokens ? 16 : 64; }
+
 uint64_t loss_bytes(uint64_t tokens, uint64_t classes) {
-  const uint64_t piece = piece_of(tokens, classes), parts = (classes + piece - 1) / piece;
-  return tokens ? whole(8 * parts * tokens) + whole(4 * tokens) + whole(4 * piece * tokens) : 0;
+  return tokens ? whole(8 * tokens * ((classes + least_part(tokens) - 1) / least_part(tokens))) + whole(4 * tokens) : 0;
 }
 
-int launch_loss(const LossArgs& a, void* workspace, uint32_t n_cu, void* stream) {
+int launch_loss(const LossArgs& l, void* workspace, uint32_t n_cu, void* stream) {
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const uint32_t piece = static_cast<uint32_t>(piece_of(a.tokens, a.classes)), parts = (a.classes + piece - 1) / piece;
   Arena arena{static_cast<char*>(workspace)};
-  float2* const part = arena.take<float2>(static_cast<uint64_t>(parts) * a.tokens);
-  float* const at_target = arena.take<float>(a.tokens);
-  float* const z = arena.take<float>(static_cast<uint64_t>(piece) * a.tokens);
-  for (uint32_t p = 0; p < parts; ++p) {
-    const uint32_t first = p * piece, n = a.classes - first < piece ? a.classes - first : piece;
-    const MatmulArgs m{a.x, rows_from(a.w, first), Mat{z, nullptr, n, 0, 0}, a.tokens, n, a.inputs};
-    if (int e = launch_matmul(m, kF32, n_cu, stream)) return e;
-    piece_kernel<<<a.tokens, 256, 0, st>>>(z, first, n, a.classes, a.targets, part + static_cast<uint64_t>(p) * a.tokens, at_target);
+  float2* const part = arena.take<float2>(static_cast<uint64_t>(tiles_of(l.classes, least_part(l.tokens))) * l.tokens);
+  float* const at_target = arena.take<float>(l.tokens);
+  const MatmulArgs a{l.x, l.w, Mat{}, l.tokens, l.classes, l.inputs};
+  const auto size = [&](uint32_t rows, const Mat& x) { return (rows - 1) * x.stride + a.k; };
+  uint32_t parts;
+  // The rules of stq_matmul, whose tiles these are.
+  const bool tiles = near(a.a) && near(a.b), wide = tiles_of(a.n, 16) > 2 * n_cu;
+  const bool few = a.m <= 32 || (a.m <= kFewTokens && (!tiles || tiles_of(a.n, 64) * 2 < n_cu));
+  if (size(a.m, a.a) < 16 || size(a.n, a.b) < 16 || (!few && !tiles)) {
+    parts = tiles_of(a.n, 256);
+    const uint64_t groups = static_cast<uint64_t>(a.m) * parts;
+    loss_each_kernel<<<static_cast<uint32_t>(groups < 65536 ? groups : 65536), 256, 0, st>>>(a, l.targets, part, at_target, parts);
+  } else if (few) {
+    parts = tiles_of(a.n, 16);
+    if (a.m <= 16 && wide) loss_few_kernel<1, 1, 2><<<in_layers(parts), 512, 0, st>>>(a, l.targets, part, at_target);
+    else if (a.m <= 16) loss_few_kernel<1, 1, 4><<<in_layers(parts), 512, 0, st>>>(a, l.targets, part, at_target);
+    else if (a.m <= 32 && wide) loss_few_kernel<2, 2, 2><<<in_layers(tiles_of(a.n, 32)), 512, 0, st>>>(a, l.targets, part, at_target);
+    else if (a.m <= 32) loss_few_kernel<2, 1, 2><<<in_layers(parts), 512, 0, st>>>(a, l.targets, part, at_target);
+    else loss_few_kernel<4, 1, 2><<<in_layers(parts), 512, 0, st>>>(a, l.targets, part, at_target);
+  } else {
+    const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(a.m, t)) * tiles_of(a.n, t); };
+    const bool pieces = in_pieces(a.a) && in_pieces(a.b);
+    const uint32_t t = pieces && count(256) * 4 >= 3 * n_cu ? 256 : (count(128) >= n_cu ? 128 : 64), rows = tiles_of(a.m, t), cols = tiles_of(a.n, t);
+    const dim3 grid = in_layers(count(t));
+    parts = cols;
+    if (t == 256) loss_tile_kernel<256, 256, 2, 4, true><<<grid, 512, 0, st>>>(a, l.targets, part, at_target, rows, cols);
+    else if (t == 128 && pieces) loss_tile_kernel<128, 128, 2, 2, true><<<grid, 256, 0, st>>>(a, l.targets, part, at_target, rows, cols);
+    else if (t == 128) loss_tile_kernel<128, 128, 2, 2, false><<<grid, 256, 0, st>>>(a, l.targets, part, at_target, rows, cols);
+    else if (pieces) loss_tile_kernel<64, 64, 2, 2, true><<<grid, 256, 0, st>>>(a, l.targets, part, at_target, rows, cols);
+    else loss_tile_kernel<64, 64, 2, 2, false><<<grid, 256, 0, st>>>(a, l.targets, part, at_target, rows, cols);
   }
-  join_kernel<<<(a.tokens + 255) / 256, 256, 0, st>>>(part, at_target, parts, a.tokens, a.classes, a.targets, a.loss, a.lse);
+  // Threads for a token: as many as there are parts for, and no more than fill the card.
+  if (l.tokens <= 1024 && parts > 64) join_kernel<256><<<l.tokens, 256, 0, st>>>(part, at_target, parts, l.tokens, l.classes, l.targets, l.loss, l.lse);
+  else join_kernel<8><<<tiles_of(l.tokens, 32), 256, 0, st>>>(part, at_target, parts, l.tokens, l.classes, l.targets, l.loss, l.lse);
   return hipGetLastError();
 }
 

@@ -21,81 +21,16 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul_tile_kernel(const MatmulA
   });
 }
 
-// Few tokens: what counts is how fast w's codes arrive.  A workgroup has 16 R of w's rows and up to 16 G tokens; its eight waves share
-// the inner dimension, a run of 128 codes each in turn, read straight into the fragments, and add up at the end.  The loads of A runs
-// are under way together.  One token through 11008 x 4096: 11.0 us, of which the codes would take 8.4 at the rate of a large copy; a
-// launch and its end are most of the rest (32000 x 4096: 4.8 TB/s).  (Workgroups beyond w's rows, in launches of several layers, repeat its
-// last one and store nothing: a way out for them took 0.2 us of every call.)
 template <uint32_t TO, int G, int R, int A>
 __global__ __launch_bounds__(512) void matmul_few_kernel(const MatmulArgs a) {
-  __shared__ __align__(16) v4i part[8][G * R][64];
-  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t n0 = group_number() * 16 * R, row = lane & 15, piece = (lane >> 4) * 16;
-  const int8_t* const px = static_cast<const int8_t*>(a.a.p);
-  const int8_t* const pw = static_cast<const int8_t*>(a.b.p);
-  uint64_t ox[G], ow[R];
+  code_few<G, R, A>(a, [&](const v4i& sum, uint32_t m, uint32_t n) __attribute__((always_inline)) {
+    if (m >= a.m) return;
+    const float s = as_global(a.a.s)[m];
+    float v[4];
 #pragma unroll
-  for (uint32_t g = 0; g < G; ++g) ox[g] = min(g * 16 + row, a.m - 1) * a.a.stride + piece;
-#pragma unroll
-  for (uint32_t r = 0; r < R; ++r) ow[r] = min(n0 + r * 16 + row, a.n - 1) * a.b.stride + piece;
-  v4i acc[R][G] = {};
-  for (uint32_t k0 = wave * 128; k0 < a.k; k0 += A * 1024) {
-    v4i fw[A][2][R], fx[A][2][G];
-#pragma unroll
-    for (uint32_t t = 0; t < A; ++t) {
-      const uint32_t k = k0 + t * 1024;
-      if (k + 128 > a.k) break;
-#pragma unroll
-      for (uint32_t h = 0; h < 2; ++h) {
-#pragma unroll
-        for (uint32_t r = 0; r < R; ++r) fw[t][h][r] = load_fragment(pw + ow[r] + k + h * 64);
-#pragma unroll
-        for (uint32_t g = 0; g < G; ++g) fx[t][h][g] = load_fragment(px + ox[g] + k + h * 64);
-      }
-    }
-#pragma unroll
-    for (uint32_t t = 0; t < A; ++t) {
-      if (k0 + t * 1024 + 128 > a.k) break;
-#pragma unroll
-      for (uint32_t h = 0; h < 2; ++h)
-#pragma unroll
-        for (uint32_t r = 0; r < R; ++r)
-#pragma unroll
-          for (uint32_t g = 0; g < G; ++g) acc[r][g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[t][h][r], fx[t][h][g], acc[r][g], 0, 0, 0);
-    }
-  }
-  if (const uint32_t k = a.k & ~127u; k < a.k && k / 128 % 8 == wave) {  // a run that is no whole one
-    const int64_t total_x = static_cast<int64_t>((a.m - 1) * a.a.stride + a.k), total_w = static_cast<int64_t>((a.n - 1) * a.b.stride + a.k);
-#pragma unroll
-    for (uint32_t h = 0; h < 2; ++h) {
-      const int32_t valid = static_cast<int32_t>(a.k) - static_cast<int32_t>(k + h * 64 + piece);
-      v4i fw[R], fx[G];
-#pragma unroll
-      for (uint32_t r = 0; r < R; ++r) fw[r] = load_last(pw, ow[r] + k + h * 64, total_w, valid);
-#pragma unroll
-      for (uint32_t g = 0; g < G; ++g) fx[g] = load_last(px, ox[g] + k + h * 64, total_x, valid);
-#pragma unroll
-      for (uint32_t r = 0; r < R; ++r)
-#pragma unroll
-        for (uint32_t g = 0; g < G; ++g) acc[r][g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[r], fx[g], acc[r][g], 0, 0, 0);
-    }
-  }
-#pragma unroll
-  for (uint32_t r = 0; r < R; ++r)
-#pragma unroll
-    for (uint32_t g = 0; g < G; ++g) part[wave][r * G + g][lane] = acc[r][g];
-  __syncthreads();
-  if (wave >= G * R) return;
-  v4i sum = part[0][wave][lane];
-#pragma unroll
-  for (uint32_t w = 1; w < 8; ++w) sum += part[w][wave][lane];
-  const uint32_t m = wave % G * 16 + row, n = n0 + wave / G * 16 + (lane >> 4) * 4;
-  if (m >= a.m) return;
-  const float s = as_global(a.a.s)[m];
-  float v[4];
-#pragma unroll
-  for (uint32_t e = 0; e < 4; ++e) v[e] = static_cast<float>(sum[e]) * s * as_global(a.b.s)[min(n + e, a.n - 1)];
-  store4<TO>(a.out, m, n, a.n, v);
+    for (uint32_t e = 0; e < 4; ++e) v[e] = static_cast<float>(sum[e]) * s * as_global(a.b.s)[min(n + e, a.n - 1)];
+    store4<TO>(a.out, m, n, a.n, v);
+  });
 }
 
 // Operands of fewer than 16 codes, or of rows too far apart for the offsets of a tile: an element to a thread.
