@@ -23,7 +23,7 @@ DEVICE_FLAGS = ["--offload-arch=gfx950", "-ffp-contract=off",
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,
           "-Wall", "-Wextra", "-Wno-unused-parameter"]
 
-SOURCES = ["stq_step.hip", "stq_kernels.hip", "stq_engine.hip", "stq_rows.hip", "stq_matmul.hip", "stq_clip.hip", "stq_loss.hip",
+SOURCES = ["stq_step.hip", "stq_kernels.hip", "stq_engine.hip", "stq_rows.hip", "stq_matmul.hip", "stq_clip.hip", "stq_loss.hip", "stq_loss_grad.hip",
            "stq_api.cpp", "stq_operators.cpp", "stq_tables.cpp", "stq_decide.cpp"]
 
 

@@ -1,25 +1,15 @@
-// gfx950 kernels of the softmax cross entropy over 8-bit codes.  The classes are taken in pieces, of which the logits lie in the
-// workspace: each leaves a maximum and a sum for every token, which a last kernel joins.
+// gfx950 kernels of the softmax cross entropy over 8-bit codes: the products' tiles, whose logits stay in registers and leave a maximum
+// and a sum for each of their tokens, and a kernel that joins these.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
 
-#include "stq_tiles.h"
+#include "stq_loss.h"
 
 #pragma clang fp contract(off)
 
 namespace stq {
 namespace {
-
-constexpr uint32_t kNoTarget = 0xFFFFFFFFu;
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-
-// The class of a token's target, or kNoTarget; one beyond the classes comes out as no class either, and is told apart by `beyond`.
-__device__ __forceinline__ uint32_t target_of(const int64_t* targets, uint32_t token, uint32_t classes, bool* beyond) {
-  const int64_t t = as_global(targets)[token];
-  *beyond = t >= static_cast<int64_t>(classes);
-  return t < 0 || *beyond ? kNoTarget : static_cast<uint32_t>(t);
-}
 
 // Several sums of exponentials, each (maximum, sum of exp2(z - maximum)), as one.
 template <class P>
@@ -117,13 +107,6 @@ __global__ __launch_bounds__(512) void loss_few_kernel(const MatmulArgs a, const
 }
 
 // Operands of fewer than 16 codes, or of rows too far apart for the offsets of a tile: 256 classes of a token to a workgroup, a logit to a thread.
-__device__ __forceinline__ float logit(const MatmulArgs& a, uint64_t m, uint64_t n) {
-  const STQ_GLOBAL int8_t* x = as_global(static_cast<const int8_t*>(a.a.p)) + m * a.a.stride;
-  const STQ_GLOBAL int8_t* w = as_global(static_cast<const int8_t*>(a.b.p)) + n * a.b.stride;
-  int32_t sum = 0;
-  for (uint32_t k = 0; k < a.k; ++k) sum += x[k] * w[k];
-  return static_cast<float>(sum) * as_global(a.a.s)[m] * as_global(a.b.s)[n];
-}
 __global__ __launch_bounds__(256) void loss_each_kernel(const MatmulArgs a, const int64_t* targets, float2* part, float* at_target, uint32_t groups_n) {
   __shared__ float2 held[4];
   const uint64_t groups = static_cast<uint64_t>(a.m) * groups_n;
@@ -180,81 +163,6 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* part, const flo
   lse[token] = d == d ? fmaxf(others, z) + small : d;
 }
 
-// What a token's gradients need: lse, dloss + dlse, the gradient of the target's logit and the target's class; and the scale of its
-// codes, or 0 where the token takes no part.
-__global__ __launch_bounds__(256) void tokens_kernel(LossGradArgs a) {
-  const uint32_t token = blockIdx.x * 256 + threadIdx.x;
-  if (token >= a.tokens) return;
-  bool beyond;
-  const uint32_t target = target_of(a.targets, token, a.classes, &beyond);
-  const float dlse = a.dlse ? as_global(a.dlse)[token] : 0.0f, dloss = beyond ? NAN : (target == kNoTarget ? 0.0f : as_global(a.dloss)[token]);
-  const float loss = as_global(a.loss)[token];
-  const bool part = !(dlse == 0.0f && dloss == 0.0f);
-  static_cast<float4*>(a.token)[token] = make_float4(as_global(a.lse)[token], part ? dloss + dlse : 0.0f, dlse * expf(-loss) + dloss * expm1f(-loss), u2f(part ? target : kNoTarget));
-  a.scale[token] = part ? as_global(a.x.s)[token] : 0.0f;
-}
-
-// Logits of a piece to their gradients.
-__global__ __launch_bounds__(256) void softmax_grad_kernel(float* z, uint32_t first, uint32_t n, const float4* tokens) {
-  const float4 t = tokens[blockIdx.x];
-  const uint32_t target = f2u(t.w) - first;
-  float* row = z + static_cast<uint64_t>(blockIdx.x) * n;
-  for (uint32_t c = threadIdx.x; c < n; c += 256) {
-    const float g = t.y * __builtin_amdgcn_exp2f((row[c] - t.x) * kLog2e);
-    row[c] = t.y == 0.0f ? 0.0f : g;
-    if (c == target) row[c] = t.z;
-  }
-}
-
-// out[i][j] (+)= sum over c of g(i, c) * s(c) * q(c, j), a thread to an element: with respect to x i is the token and c the class, with
-// respect to w (WEIGHT) i is the class and c the token.  g: [tokens][n].
-template <bool WEIGHT, uint32_t TO>
-__global__ __launch_bounds__(256) void product_kernel(const float* g, uint32_t n, const Mat q, const Mat out, float* sum, bool first, bool last, uint32_t ni, uint32_t nj, uint32_t nc) {
-  using T = typename Elem<TO>::type;
-  const uint64_t total = static_cast<uint64_t>(ni) * nj;
-  for (uint64_t t = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; t < total; t += static_cast<uint64_t>(gridDim.x) * 256) {
-    const uint64_t i = t / nj, j = t % nj;
-    float v = first ? 0.0f : sum[t];
-    for (uint64_t c = 0; c < nc; ++c)
-      v = fmaf(as_global(g)[WEIGHT ? c * n + i : i * n + c] * as_global(q.s)[c], static_cast<float>(as_global(static_cast<const int8_t*>(q.p))[c * q.stride + j]), v);
-    if (last) as_global(static_cast<T*>(out.p))[i * out.stride + j] = static_cast<T>(v);
-    else sum[t] = v;
-  }
-}
-template <bool WEIGHT>
-void product(uint32_t to, const float* g, uint32_t n, const Mat& q, const Mat& out, float* sum, bool first, bool last, uint32_t ni, uint32_t nj, uint32_t nc, hipStream_t st) {
-  const uint64_t groups = (static_cast<uint64_t>(ni) * nj + 255) / 256;
-  const uint32_t grid = static_cast<uint32_t>(groups < 65536 ? groups : 65536);
-  if (to == kF32) product_kernel<WEIGHT, kF32><<<grid, 256, 0, st>>>(g, n, q, out, sum, first, last, ni, nj, nc);
-  else product_kernel<WEIGHT, kBF16><<<grid, 256, 0, st>>>(g, n, q, out, sum, first, last, ni, nj, nc);
-}
-
-// Classes of a piece: of as many logits as 256 MiB hold in fp32, and of one size.
-constexpr uint64_t kPieceLogits = 1ull << 26, kLeastPiece = 1024;
-uint64_t piece_of(uint64_t tokens, uint64_t classes) {
-  uint64_t most = kPieceLogits / (tokens ? tokens : 1);
-  if (most < kLeastPiece) most = kLeastPiece;
-  const uint64_t pieces = (classes + most - 1) / most, each = (classes + pieces - 1) / pieces;
-  return each < classes ? (each + 255) / 256 * 256 : classes;
-}
-uint64_t whole(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
-
-struct Arena {  // parts of the workspace
-  char* at;
-  template <class T>
-  T* take(uint64_t n) {
-    T* const p = reinterpret_cast<T*>(at);
-    at += whole(n * sizeof(T));
-    return p;
-  }
-};
-Mat rows_from(const Mat& m, uint64_t row) {
-  Mat r = m;
-  r.p = static_cast<int8_t*>(m.p) + row * m.stride;
-  r.s = m.s + row;
-  return r;
-}
-
 }  // namespace
 
 // The least classes of a part of a token's sum.
@@ -271,12 +179,11 @@ int launch_loss(const LossArgs& l, void* workspace, uint32_t n_cu, void* stream)
   float2* const part = arena.take<float2>(static_cast<uint64_t>(tiles_of(l.classes, least_part(l.tokens))) * l.tokens);
   float* const at_target = arena.take<float>(l.tokens);
   const MatmulArgs a{l.x, l.w, Mat{}, l.tokens, l.classes, l.inputs};
-  const auto size = [&](uint32_t rows, const Mat& x) { return (rows - 1) * x.stride + a.k; };
   uint32_t parts;
   // The rules of stq_matmul, whose tiles these are.
   const bool tiles = near(a.a) && near(a.b), wide = tiles_of(a.n, 16) > 2 * n_cu;
   const bool few = a.m <= 32 || (a.m <= kFewTokens && (!tiles || tiles_of(a.n, 64) * 2 < n_cu));
-  if (size(a.m, a.a) < 16 || size(a.n, a.b) < 16 || (!few && !tiles)) {
+  if (!enough_codes(a) || (!few && !tiles)) {
     parts = tiles_of(a.n, 256);
     const uint64_t groups = static_cast<uint64_t>(a.m) * parts;
     loss_each_kernel<<<static_cast<uint32_t>(groups < 65536 ? groups : 65536), 256, 0, st>>>(a, l.targets, part, at_target, parts);
@@ -302,39 +209,6 @@ int launch_loss(const LossArgs& l, void* workspace, uint32_t n_cu, void* stream)
   // Threads for a token: as many as there are parts for, and no more than fill the card.
   if (l.tokens <= 1024 && parts > 64) join_kernel<256><<<l.tokens, 256, 0, st>>>(part, at_target, parts, l.tokens, l.classes, l.targets, l.loss, l.lse);
   else join_kernel<8><<<tiles_of(l.tokens, 32), 256, 0, st>>>(part, at_target, parts, l.tokens, l.classes, l.targets, l.loss, l.lse);
-  return hipGetLastError();
-}
-
-uint64_t loss_grad_bytes(uint64_t tokens, uint64_t classes, uint64_t inputs) {
-  const uint64_t piece = piece_of(tokens, classes);
-  return tokens ? whole(16 * tokens) + whole(4 * tokens) + whole(4 * piece * tokens) + whole(4 * tokens * inputs) : 0;
-}
-
-int launch_loss_grad(LossGradArgs a, uint32_t dx_type, uint32_t dw_type, void* workspace, uint32_t n_cu, void* stream) {
-  const hipStream_t st = static_cast<hipStream_t>(stream);
-  const uint32_t piece = static_cast<uint32_t>(piece_of(a.tokens, a.classes)), parts = (a.classes + piece - 1) / piece;
-  Arena arena{static_cast<char*>(workspace)};
-  a.token = arena.take<float4>(a.tokens);
-  a.scale = arena.take<float>(a.tokens);
-  float* const z = arena.take<float>(static_cast<uint64_t>(piece) * a.tokens);
-  float* const sum = arena.take<float>(static_cast<uint64_t>(a.tokens) * a.inputs);
-  if (a.tokens) tokens_kernel<<<(a.tokens + 255) / 256, 256, 0, st>>>(a);
-  Mat x = a.x;
-  x.s = a.scale;
-  for (uint32_t p = 0; p < parts; ++p) {
-    const uint32_t first = p * piece, n = a.classes - first < piece ? a.classes - first : piece;
-    const Mat g{z, nullptr, n, 0, 0}, w = rows_from(a.w, first);
-    if (a.tokens) {
-      if (int e = launch_matmul(MatmulArgs{a.x, w, g, a.tokens, n, a.inputs}, kF32, n_cu, stream)) return e;
-      softmax_grad_kernel<<<a.tokens, 256, 0, st>>>(z, first, n, static_cast<const float4*>(a.token));
-    }
-    if (a.dx.p && a.tokens) product<false>(dx_type, z, n, w, a.dx, sum, p == 0, p + 1 == parts, a.tokens, a.inputs, n, st);
-    if (a.dw.p) {
-      Mat dw = a.dw;
-      dw.p = static_cast<char*>(a.dw.p) + static_cast<uint64_t>(first) * a.dw.stride * (dw_type == kF32 ? 4 : 2);
-      product<true>(dw_type, z, n, x, dw, nullptr, true, true, n, a.inputs, a.tokens, st);
-    }
-  }
   return hipGetLastError();
 }
 

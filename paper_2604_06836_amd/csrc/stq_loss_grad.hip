@@ -1,0 +1,686 @@
+// gfx950 kernels of the gradients of the softmax cross entropy over 8-bit codes.
+//
+// g[t][v], the gradient of a logit, is computed in tiles of the logits as the forward pass has them, a piece of the classes at a time, and
+// written twice: times the classes' scales as the factors of dx, times the tokens' as those of dw.  The products take these factors as
+// fp16, as one term of 11 bits for results in bf16 and as two, 22 bits, for results in fp32, after a power of two for each row of the
+// result that brings the row's largest into [2^14, 2^15): what lies 2^-29 below that loses bits, and what lies 2^-39 below it counts as 0.
+// For dx a bound on the row's largest is known beforehand (|g| <= |dloss + dlse| (1 - p) but at the target), so that its factors are
+// written in fp16; for dw it is gathered while g is written, in fp32.  Codes are exact in fp16.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "stq_loss.h"
+
+#pragma clang fp contract(off)
+
+namespace stq {
+namespace {
+
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+
+// A power of two that brings numbers of a magnitude up to `most` below 2^15, and the largest to 2^14 at least where that is within fp32's
+// range; below all of them, if `most` is not finite.  most: bits of a number >= 0.
+__device__ __forceinline__ uint32_t factor_exponent(uint32_t most) {
+  const uint32_t e = most >> 23;
+  return e >= 255 ? 7u : min(268u - e, 253u);
+}
+__device__ __forceinline__ float factor(uint32_t most) { return u2f(factor_exponent(most) << 23); }
+[[maybe_unused]] __device__ __forceinline__ float back(uint32_t most) { return u2f((254u - factor_exponent(most)) << 23); }
+
+// What the tiles of the logits need of a token.
+struct Token {
+  float lse2;       // log-sum times log2 e
+  float c;          // dloss + dlse
+  float at_target;  // the gradient of the target's logit
+  uint32_t target;  // its class, or kNoTarget
+};
+struct GradWork {  // parts of the workspace
+  Token* token;      // [tokens, padded]
+  float* scale;      // [tokens, padded]: of the codes, or 0 for a token that takes no part
+  float* most;       // [tokens, padded]: a bound on |g| of the row
+  uint32_t* most_w;  // the largest of the classes' scales (bits)
+  uint32_t* most_v;  // [classes]: the largest |g * scale| of a class (bits)
+  _Float16* x;       // [tokens, padded][inputs, padded]: codes, zeros beyond the matrix
+  _Float16* w;       // [classes of a piece, padded][inputs, padded]
+  _Float16* gx[2];   // [tokens, padded][classes of a piece, padded]: factors of dx, one or two terms
+  float* gw;         // the same: factors of dw
+  float* sum;        // [tokens][inputs]: of dx, where there are several pieces
+  float* partial;    // parts of a product that is taken in several
+};
+
+// ---------------------------------------------------------------------------------------------- preparation
+// Codes as fp16, eight to a thread, into rows of `cols` (a multiple of eight) with zeros beyond the matrix.
+constexpr uint32_t kConvert = 4;  // vectors of a thread
+struct Convert {
+  Mat from;
+  _Float16* to;
+  uint32_t rows, inputs, cols;
+  uint64_t vectors;  // of the padded matrix
+  __device__ __forceinline__ void operator()(uint64_t group) const {
+    const uint32_t per_row = cols / 8;
+    const uint64_t first = group * (256 * kConvert), row0 = first / per_row;
+    const uint32_t in_row = static_cast<uint32_t>(first % per_row) + threadIdx.x;
+#pragma unroll
+    for (uint32_t k = 0; k < kConvert; ++k) {
+      const uint32_t v = in_row + 256 * k, row_in = v / per_row, col = (v - row_in * per_row) * 8;
+      const uint64_t row = row0 + row_in;
+      if (first + threadIdx.x + 256 * k >= vectors) return;
+      v8h h{};
+      if (row < rows) {
+        const Packed<int8_t> q = load_ending(static_cast<const int8_t*>(from.p) + row * from.stride, col, inputs);
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) h[e] = static_cast<_Float16>(q.at(e));
+      }
+      __builtin_memcpy(as_global(to) + row * cols + col, &h, 16);
+    }
+  }
+};
+__global__ __launch_bounds__(256) void convert_kernel(const Convert w) { w(group_number()); }
+
+// In one launch what is there before the first piece: the tokens' data, the largest scale of a class, zeros in place of the classes'
+// largest, x and the first piece of w in fp16.
+struct Prepare {
+  LossGradArgs a;
+  GradWork g;
+  Convert x, w;
+  uint32_t tokens_padded;
+  uint32_t groups_t, groups_v;
+  uint64_t groups_x;
+};
+__global__ __launch_bounds__(256) void prepare_kernel(const Prepare p) {
+  const LossGradArgs& a = p.a;
+  uint64_t group = group_number();
+  if (group == 0) {
+    __shared__ uint32_t held[4];
+    uint32_t most = 0;
+    for (uint32_t c = threadIdx.x * 4; c < a.classes; c += 1024) {
+      uint32_t s[4];
+      if (c + 4 <= a.classes) {
+        __builtin_memcpy(s, as_global(a.w.s) + c, 16);
+      } else {
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) s[e] = f2u(as_global(a.w.s)[min(c + e, a.classes - 1)]);
+      }
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e) most = max(most, s[e] & 0x7FFFFFFFu);
+    }
+    for (int o = 1; o < 64; o *= 2) most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), o)));
+    if ((threadIdx.x & 63) == 0) held[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) *p.g.most_w = max(max(held[0], held[1]), max(held[2], held[3]));
+  } else if (--group < p.groups_t) {
+    const uint32_t token = static_cast<uint32_t>(group) * 256 + threadIdx.x;
+    if (token >= p.tokens_padded) return;
+    Token t{0.0f, 0.0f, 0.0f, kNoTarget};
+    float scale = 0.0f, most = 0.0f;
+    if (token < a.tokens) {
+      bool beyond;
+      const uint32_t target = target_of(a.targets, token, a.classes, &beyond);
+      const float dlse = a.dlse ? as_global(a.dlse)[token] : 0.0f, dloss = beyond ? NAN : (target == kNoTarget ? 0.0f : as_global(a.dloss)[token]);
+      if (!(dlse == 0.0f && dloss == 0.0f)) {
+        const float loss = as_global(a.loss)[token], others = target == kNoTarget ? 1.0f : -expm1f(-loss);  // probability of the other classes
+        t = Token{as_global(a.lse)[token] * kLog2e, dloss + dlse, dlse * expf(-loss) - dloss * others, target};
+        scale = as_global(a.x.s)[token];
+        most = u2f(max(f2u(t.c * others) & 0x7FFFFFFFu, target == kNoTarget ? 0u : f2u(t.at_target) & 0x7FFFFFFFu));
+      }
+    }
+    p.g.token[token] = t;
+    p.g.scale[token] = scale;
+    p.g.most[token] = most;
+  } else if ((group -= p.groups_t) < p.groups_v) {
+    for (uint32_t e = 0; e < 4; ++e)
+      if (const uint64_t c = group * 1024 + e * 256 + threadIdx.x; c < a.classes) p.g.most_v[c] = 0;
+  } else if ((group -= p.groups_v) < p.groups_x) {
+    p.x(group);
+  } else if ((group -= p.groups_x) * (256 * kConvert) < p.w.vectors) {
+    p.w(group);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- gradients of the logits
+struct LogitGrads {
+  GradWork g;
+  uint32_t first;                    // class of the piece
+  uint32_t tokens_padded, n_padded;  // rows and columns that are written, zeros beyond the matrices
+};
+__device__ __forceinline__ float grad_of(float z, const Token& t) { return t.c * __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, -t.lse2)); }
+template <int TERMS>
+__device__ __forceinline__ float term(float x, int k) { return TERMS == 2 && k ? x - static_cast<float>(static_cast<_Float16>(x)) : x; }
+
+// a.a.s: the scales of GradWork, a.b and a.n: of the piece.  In front of the products: 11 of 100 parts of the time.
+template <int TERMS, int TM, int TN, int WM, int WN, bool PIECES>
+__global__ __launch_bounds__(WM * WN * 64) void grad_tile_kernel(const MatmulArgs a, const LogitGrads l, uint32_t tiles_m, uint32_t tiles_n) {
+  constexpr uint32_t FM = TM / WM / 32, FN = TN / WN / 32;
+  code_tile<TM, TN, WM, WN, PIECES>(a, tiles_m, tiles_n, [&](auto& acc, const CodeTile& t) __attribute__((always_inline)) {
+    const uint32_t half = t.lane >> 5, first = t.n0 + t.wn + 4 * half, there = a.n - t.n0 - t.wn;  // (beyond the classes: above 2^31)
+    const float most_w = u2f(*l.g.most_w);
+    float scale[FM], times[FM];
+    const float* const sn = t.sn + t.wn + 4 * half;
+#pragma unroll
+    for (uint32_t i = 0; i < FM; ++i) {
+      const uint32_t row = t.wm + i * 32 + (t.lane & 31), token = t.m0 + row;
+      const Token k = l.g.token[min(token, l.tokens_padded - 1)];
+      scale[i] = token < a.m ? t.sm[row] : 0.0f;
+      times[i] = factor(f2u(l.g.most[min(token, l.tokens_padded - 1)] * most_w));
+      const uint32_t at = k.target - l.first - first;  // column 32 j + 8 p + e of the lane's
+      float v[FN * 16];
+#pragma unroll
+      for (uint32_t j = 0; j < FN; ++j)
+#pragma unroll
+        for (uint32_t c = 0; c < 16; ++c) v[j * 16 + c] = grad_of(static_cast<float>(acc[i][j][c]) * scale[i] * sn[j * 32 + c / 4 * 8 + c % 4], k);
+      if (__builtin_amdgcn_ballot_w64(at < FN * 32)) {
+#pragma unroll
+        for (uint32_t c = 0; c < FN * 16; ++c)
+          if (at == c / 16 * 32 + c % 16 / 4 * 8 + c % 4) v[c] = k.at_target;
+      }
+      if (there < FN * 32 || static_cast<int32_t>(there) < 0) {
+#pragma unroll
+        for (uint32_t c = 0; c < FN * 16; ++c)
+          if (first + c / 16 * 32 + c % 16 / 4 * 8 + c % 4 >= a.n) v[c] = 0.0f;
+      }
+#pragma unroll
+      for (uint32_t j = 0; j < FN; ++j)
+#pragma unroll
+        for (uint32_t c = 0; c < 16; ++c) acc[i][j][c] = static_cast<int>(f2u(v[j * 16 + c]));
+      __builtin_amdgcn_sched_barrier(0);  // (one row's at a time, for the registers)
+    }
+    const auto g = [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return u2f(static_cast<uint32_t>(acc[i][j][p * 4 + e])); };
+#pragma unroll
+    for (int k = 0; k < TERMS; ++k)
+      store_tile<kF16, FM, FN>(Mat{l.g.gx[k], nullptr, l.n_padded, 0, 0}, t.m0 + t.wm, t.n0 + t.wn, l.tokens_padded, l.n_padded, t.box, t.lane,
+                               [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return term<TERMS>(g(i, j, p, e) * sn[j * 32 + p * 8 + e] * times[i], k); });
+    // the largest of each column, from the pieces of rows on their way: four columns to a lane
+    uint32_t most[4] = {0, 0, 0, 0};
+    store_tile<kF32, FM, FN>(Mat{l.g.gw, nullptr, l.n_padded, 0, 0}, t.m0 + t.wm, t.n0 + t.wn, l.tokens_padded, l.n_padded, t.box, t.lane,
+                             [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return g(i, j, p, e) * scale[i]; },
+                             [&](const Piece& v) {
+#pragma unroll
+                               for (uint32_t e = 0; e < 4; ++e) most[e] = max(most[e], v.w[e] & 0x7FFFFFFFu);
+                             });
+    constexpr uint32_t kPieces = FN * 8;
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) {
+#pragma unroll
+      for (uint32_t o = kPieces; o < 64; o *= 2) most[e] = max(most[e], static_cast<uint32_t>(__shfl_xor(static_cast<int>(most[e]), o)));
+      const uint32_t c = t.n0 + t.wn + t.lane * 4 + e;
+      if (t.lane < kPieces && c < a.n && most[e]) atomicMax(l.g.most_v + l.first + c, most[e]);
+    }
+    if constexpr (TM < 128) {  // rows and columns of zeros that no tile covers
+      const uint32_t row_end = t.m0 + TM, col_end = t.n0 + TN;
+      const bool last_row = row_end >= a.m, last_col = col_end >= a.n;
+      for (uint32_t k = threadIdx.x; k < TM * TN; k += WM * WN * 64) {
+        const uint32_t r = k / TN, c = k % TN;
+        if (last_row && row_end + r < l.tokens_padded && t.n0 + c < l.n_padded) l.g.gw[static_cast<uint64_t>(row_end + r) * l.n_padded + t.n0 + c] = 0.0f;
+        if (last_col && col_end + c < l.n_padded && t.m0 + r < l.tokens_padded)
+          for (int i = 0; i < TERMS; ++i) l.g.gx[i][static_cast<uint64_t>(t.m0 + r) * l.n_padded + col_end + c] = static_cast<_Float16>(0.0f);
+      }
+    }
+  });
+}
+
+// The same of a thread's own logits: operands of fewer than 16 codes, or of rows too far apart for the offsets of a tile.
+template <int TERMS>
+__global__ __launch_bounds__(256) void grad_each_kernel(const MatmulArgs a, const LogitGrads l) {
+  const uint64_t total = static_cast<uint64_t>(l.tokens_padded) * l.n_padded;
+  const float most_w = u2f(*l.g.most_w);
+  for (uint64_t at = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; at < total; at += static_cast<uint64_t>(gridDim.x) * 256) {
+    const uint32_t token = static_cast<uint32_t>(at / l.n_padded), c = static_cast<uint32_t>(at % l.n_padded);
+    float gx = 0.0f, gw = 0.0f;
+    if (token < a.m && c < a.n) {
+      const Token k = l.g.token[token];
+      const float g = k.target == l.first + c ? k.at_target : grad_of(a.a.s[token] == 0.0f ? 0.0f : logit(a, token, c), k);
+      gx = g * a.b.s[c] * factor(f2u(l.g.most[token] * most_w));
+      gw = g * a.a.s[token];
+      if (const uint32_t m = f2u(gw) & 0x7FFFFFFFu) atomicMax(l.g.most_v + l.first + c, m);
+    }
+#pragma unroll
+    for (int k = 0; k < TERMS; ++k) l.g.gx[k][at] = static_cast<_Float16>(term<TERMS>(gx, k));
+    l.g.gw[at] = gw;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- products
+// out[i][j] = sum over c of g(i, c) * q(c, j): with respect to x (WEIGHT false) i is the token and c the class, with respect to w i is the
+// class and c the token.
+struct ProductArgs {
+  const _Float16* gx[2];  // [ni, padded][nc]
+  const float* gw;        // [nc][ni, padded]
+  const _Float16* q;      // [nc][nj, padded]
+  uint64_t g_stride;
+  const uint32_t* most;   // [ni]: bits of a row's largest, or of a bound on it ...
+  const uint32_t* times;  // ... which this is a factor of (null: 1)
+  Mat out;
+  float* sum;             // [ni][nj]: what is added (with `add`), and where the result goes that is not the last part
+  bool add, last;
+  uint32_t ni, nj, nc;    // sizes of the sum; nc is a multiple of two steps
+  uint32_t ni_padded, nj_padded;
+  uint32_t tiles_i, tiles_j;
+  uint32_t splits, each;  // parts of c, and their length (a multiple of two steps)
+  float* partial;         // [splits][ni][nj] where there are several
+};
+
+// A [c][x] tile in LDS: rows of X elements, of which pieces of eight lie at the places that their number and the row's give by exclusive or, so
+// that the four rows of a transposed read meet every bank once.
+template <uint32_t X>
+__device__ __forceinline__ uint32_t swizzle_x(uint32_t row) { return X >= 128 ? (row & 3) << 2 : (row >> 1 & 1) << 2; }
+// An [i][c] tile of C elements a row, 32 or 64, for reads of one piece of 32 rows.
+template <uint32_t C>
+__device__ __forceinline__ uint32_t swizzle_c(uint32_t row) { return C == 32 ? row >> 2 & 3 : row >> 1 & 7; }
+
+// The fragment of columns x0 .. x0+31 and rows c0 .. c0+15 of a [c][x] tile: eight neighbouring rows of one column to a lane.
+template <uint32_t X>
+__device__ __forceinline__ v8h transposed(const _Float16* tile, uint32_t c0, uint32_t x0, uint32_t lane) {
+  const uint32_t row = c0 + (lane >> 5) * 8 + ((lane & 15) >> 2), piece = (x0 / 8 ^ swizzle_x<X>((lane & 15) >> 2)) + (lane & 16) / 8 + (lane & 3) / 2;
+  const _Float16* p = tile + row * X + piece * 8 + (lane & 1) * 4;
+  const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((STQ_LDS v4s*)(p));
+  const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((STQ_LDS v4s*)(p + 4 * X));
+  v8h r;
+  __builtin_memcpy(&r, &lo, 8);
+  __builtin_memcpy(reinterpret_cast<char*>(&r) + 8, &hi, 8);
+  return r;
+}
+
+[[maybe_unused]] __device__ __forceinline__ void store_floats(float* p, const float (&v)[4]) { __builtin_memcpy(as_global(p), v, 16); }
+
+// A wave's sums, by way of LDS (`box`, 32 rows in fp32), to where they go, with what is added to them.
+template <uint32_t TO, uint32_t FI, uint32_t FJ, class F>
+__device__ __forceinline__ void store_sums(const ProductArgs& a, uint32_t row0, uint32_t col0, char* box, uint32_t lane, F value) {
+  constexpr uint32_t kRow = FJ * 128, kPieces = kRow / 16, kShift = kRow == 256 ? 0 : 1;
+  const auto place = [&](uint32_t row, uint32_t piece) { return row * kRow + ((piece ^ (row >> kShift)) & (kPieces - 1)) * 16; };
+  float* const to = a.splits > 1 ? a.partial + static_cast<uint64_t>(blockIdx.y) * a.ni * a.nj : a.sum;
+  const bool last = a.last && a.splits == 1, add = a.add && a.splits == 1;
+#pragma unroll
+  for (uint32_t i = 0; i < FI; ++i) {
+#pragma unroll
+    for (uint32_t j = 0; j < FJ; ++j)
+#pragma unroll
+      for (uint32_t p = 0; p < 4; ++p) {
+        float v[4];
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) v[e] = value(i, j, p, e);
+        __builtin_memcpy(box + place(lane & 31, j * 8 + p * 2 + (lane >> 5)), v, 16);
+      }
+    lanes_meet();
+#pragma unroll
+    for (uint32_t h = 0; h < 32 * kPieces / 64; ++h) {
+      const uint32_t row = h * (64 / kPieces) + lane / kPieces, piece = lane % kPieces;
+      float v[4];
+      __builtin_memcpy(v, box + place(row, piece), 16);
+      const uint32_t r = row0 + i * 32 + row, c = col0 + piece * 4;
+      if (r >= a.ni || c >= a.nj) continue;
+      const uint64_t at = static_cast<uint64_t>(r) * a.nj + c;
+      if (add) {
+        if (c + 4 <= a.nj) {
+          const v4i w = load_fragment(reinterpret_cast<const int8_t*>(a.sum + at));
+#pragma unroll
+          for (uint32_t e = 0; e < 4; ++e) v[e] += u2f(static_cast<uint32_t>(w[e]));
+        } else {
+#pragma unroll
+          for (uint32_t e = 0; e < 4; ++e)
+            if (c + e < a.nj) v[e] += as_global(a.sum)[at + e];
+        }
+      }
+      if (last) {
+        using T = typename Elem<TO>::type;
+        STQ_GLOBAL T* p = as_global(static_cast<T*>(a.out.p)) + r * a.out.stride + c;
+        if (c + 4 <= a.nj) {
+          Piece o;
+          pack4<TO>(v, &o);
+          __builtin_memcpy(p, &o, TO == kF32 ? 16 : 8);
+        } else {
+#pragma unroll
+          for (uint32_t e = 0; e < 4; ++e)
+            if (c + e < a.nj) p[e] = static_cast<T>(v[e]);
+        }
+      } else if (c + 4 <= a.nj) {
+        store_floats(to + at, v);
+      } else {
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e)
+          if (c + e < a.nj) as_global(to)[at + e] = v[e];
+      }
+    }
+    lanes_meet();
+  }
+}
+
+// A workgroup has TI x TJ of the result, its WI x WJ waves a part each, and takes STEP of c at a time, out of one of two LDS buffers while the
+// other is filled: codes and the factors of dx are loaded straight into LDS, those of dw by way of registers, where they become fp16.
+template <bool WEIGHT, uint32_t TO, int TERMS, int TI, int TJ, int WI, int WJ, int STEP>
+__global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const ProductArgs a) {
+#ifdef __HIP_DEVICE_COMPILE__  // (the host's compiler has no buffer descriptors)
+  constexpr uint32_t kThreads = WI * WJ * 64, FI = TI / WI / 32, FJ = TJ / WJ / 32;
+  constexpr uint32_t kSizeA = TI * STEP, kSizeB = STEP * TJ;
+  constexpr uint32_t LA = kSizeA / 8 / kThreads, LB = kSizeB / 8 / kThreads;  // pieces of eight of a thread
+  static_assert(LA * kThreads * 8 == kSizeA && LB * kThreads * 8 == kSizeB, "whole loads");
+  __shared__ __align__(1024) _Float16 a0[TERMS][kSizeA], b0[kSizeB], a1[TERMS][kSizeA], b1[kSizeB];
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (group_number() >= a.tiles_i * a.tiles_j) return;
+  const TileAt at = tile_at(group_number(), a.tiles_i, a.tiles_j);
+  const uint32_t i0 = at.row * TI, j0 = at.col * TJ;
+  const uint32_t first = blockIdx.y * a.each, end = min(a.nc, first + a.each);
+  // load i of a wave fills 64 pieces of LDS, in lane order, from (i * waves + wave) * 64 on
+  uint32_t ob[LB], oa[LA];
+#pragma unroll
+  for (uint32_t i = 0; i < LB; ++i) {
+    const uint32_t n = (i * (kThreads / 64) + wave) * 64 + lane, row = n / (TJ / 8), piece = (n % (TJ / 8)) ^ swizzle_x<TJ>(row);
+    ob[i] = (row * a.nj_padded + min(j0 + piece * 8, a.nj_padded - 8)) * 2;
+  }
+  if constexpr (!WEIGHT) {
+#pragma unroll
+    for (uint32_t i = 0; i < LA; ++i) {
+      const uint32_t n = (i * (kThreads / 64) + wave) * 64 + lane, row = n / (STEP / 8), piece = (n % (STEP / 8)) ^ swizzle_c<STEP>(row);
+      oa[i] = (min(i0 + row, a.ni_padded - 1) - i0) * static_cast<uint32_t>(a.g_stride) * 2 + piece * 16;
+    }
+  }
+  const auto load_b = [&](uint32_t c, _Float16* to) __attribute__((always_inline)) {
+    if (c >= end) return;
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(a.q) + static_cast<uint64_t>(c) * a.nj_padded, 0, 0x7FFFFFFF, 0x00020000);
+#pragma unroll
+    for (uint32_t i = 0; i < LB; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (STQ_LDS void*)(to + (i * (kThreads / 64) + wave) * 512), 16, ob[i], 0, 0, 0);
+  };
+  const auto load_a = [&](uint32_t c, _Float16 (*to)[kSizeA]) __attribute__((always_inline)) {
+    if (c >= end) return;
+#pragma unroll
+    for (int k = 0; k < TERMS; ++k) {
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(a.gx[k]) + static_cast<uint64_t>(i0) * a.g_stride + c, 0, 0x7FFFFFFF, 0x00020000);
+#pragma unroll
+      for (uint32_t i = 0; i < LA; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (STQ_LDS void*)(to[k] + (i * (kThreads / 64) + wave) * 512), 16, oa[i], 0, 0, 0);
+    }
+  };
+  // dw: vectors of eight classes of one token, kThreads / (TI / 8) tokens apart
+  constexpr uint32_t kApart = kThreads / (TI / 8);
+  const uint32_t ar = threadIdx.x / (TI / 8), ac = threadIdx.x % (TI / 8);
+  const uint32_t ao = ar * static_cast<uint32_t>(a.g_stride) + min(i0 + ac * 8, a.ni_padded - 8);
+  Packed<float> va[WEIGHT ? LA : 1];
+  float times[WEIGHT ? 8 : 1];
+  const auto most_of = [&](uint32_t i) {
+    const uint32_t m = as_global(a.most)[min(i, a.ni - 1)];
+    return a.times ? f2u(u2f(m) * u2f(*a.times)) : m;
+  };
+  if constexpr (WEIGHT) {
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) times[e] = factor(most_of(i0 + ac * 8 + e));
+  }
+  const auto load_regs = [&](uint32_t c) __attribute__((always_inline)) {
+    if (c >= end) return;
+#pragma unroll
+    for (uint32_t h = 0; h < LA; ++h) va[h] = load_packed(a.gw + (static_cast<uint64_t>(c) + kApart * h) * a.g_stride + ao);
+  };
+  const auto put = [&](uint32_t h, _Float16 (*to)[kSizeA]) __attribute__((always_inline)) {
+    const uint32_t row = ar + kApart * h;
+    v8h t[TERMS];
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) {
+      const float x = va[h].at(e) * times[e];
+#pragma unroll
+      for (int k = 0; k < TERMS; ++k) t[k][e] = static_cast<_Float16>(term<TERMS>(x, k));
+    }
+#pragma unroll
+    for (int k = 0; k < TERMS; ++k) __builtin_memcpy(&to[k][row * TI + (ac ^ swizzle_x<TI>(row)) * 8], &t[k], 16);
+  };
+  v16f acc[FI][FJ] = {};
+  const uint32_t wi = wave / WJ * (TI / WI), wj = wave % WJ * (TJ / WJ);
+  // A step out of ta, tb, in units of one fragment of g.  A unit's fragments are read kAhead units ahead, so that those of the last kAhead are
+  // there when the workgroup meets: from then on the next step's buffers are full and this step's are free.
+  constexpr uint32_t kUnits = STEP / 16 * TERMS * FI, kAhead = FI < 4 || TERMS == 2 ? 2 : 4;
+  static_assert(kUnits > kAhead, "units in front of the meeting");
+  v8h fa[kAhead], fb[2][FJ];
+  const auto read = [&](uint32_t u, const _Float16 (*ta)[kSizeA], const _Float16* tb) __attribute__((always_inline)) {
+    const uint32_t s = u / (TERMS * FI), k = u / FI % TERMS, i = u % FI;
+    if constexpr (WEIGHT) {
+      fa[u % kAhead] = transposed<TI>(ta[k], s * 16, wi + i * 32, lane);
+    } else {
+      const uint32_t row = wi + i * 32 + (lane & 31);
+      __builtin_memcpy(&fa[u % kAhead], &ta[k][row * STEP + ((s * 2 + (lane >> 5)) ^ swizzle_c<STEP>(row)) * 8], 16);
+    }
+    if (u % (TERMS * FI)) return;
+#pragma unroll
+    for (uint32_t j = 0; j < FJ; ++j) fb[s & 1][j] = transposed<TJ>(tb, s * 16, wj + j * 32, lane);
+  };
+  const auto work = [&](uint32_t c, _Float16 (*ta)[kSizeA], _Float16* tb, _Float16 (*na)[kSizeA], _Float16* nb) __attribute__((always_inline)) {
+#pragma unroll
+    for (uint32_t u = 0; u < kUnits; ++u) {
+      if (u == kUnits - kAhead) {
+        __syncthreads();
+        load_b(c + 2 * STEP, tb);
+        if constexpr (WEIGHT) load_regs(c + 2 * STEP);
+        else load_a(c + 2 * STEP, ta);
+      }
+#pragma unroll
+      for (uint32_t j = 0; j < FJ; ++j) acc[u % FI][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fb[u / (TERMS * FI) & 1][j], fa[u % kAhead], acc[u % FI][j], 0, 0, 0);
+      if (u + kAhead < kUnits) read(u + kAhead, ta, tb);
+      else read(u + kAhead - kUnits, na, nb);
+      if constexpr (WEIGHT) {  // the next step's factors, late in the step
+        constexpr uint32_t kFrom = kUnits - kAhead > LA ? kUnits - kAhead - LA : 0;
+#pragma unroll
+        for (uint32_t h = 0; h < LA; ++h)
+          if (u == min(kFrom + h, kUnits - kAhead - 1)) put(h, na);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  load_b(first, b0);
+  if constexpr (WEIGHT) {
+    load_regs(first);
+#pragma unroll
+    for (uint32_t h = 0; h < LA; ++h) put(h, a0);
+    load_regs(first + STEP);
+  } else {
+    load_a(first, a0);
+  }
+  __syncthreads();
+  load_b(first + STEP, b1);
+  if constexpr (!WEIGHT) load_a(first + STEP, a1);
+#pragma unroll
+  for (uint32_t u = 0; u < kAhead; ++u) read(u, a0, b0);
+  // (what the last step reads ahead is not used)
+  for (uint32_t c = first; c < end; c += 2 * STEP) {
+    work(c, a0, b0, a1, b1);
+    work(c + STEP, a1, b1, a0, b0);
+  }
+  float undo[FI];
+#pragma unroll
+  for (uint32_t i = 0; i < FI; ++i) undo[i] = back(most_of(i0 + wi + i * 32 + (lane & 31)));
+  __syncthreads();
+  constexpr uint32_t kBox = 32 * FJ * 32 * 4, kHalf = WI * WJ / 2;
+  char* const box = wave < kHalf ? reinterpret_cast<char*>(a0) + wave * kBox : reinterpret_cast<char*>(a1) + (wave - kHalf) * kBox;
+  static_assert(kHalf * kBox <= sizeof(a0), "boxes of the first half of the waves in a0, of the second in a1");
+  store_sums<TO, FI, FJ>(a, i0 + wi, j0 + wj, box, lane, [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return acc[i][j][p * 4 + e] * undo[i]; });
+#endif
+}
+
+// The parts of a sum that was taken in parts, in one order, and what is added to them.
+template <uint32_t TO>
+__global__ __launch_bounds__(256) void join_parts_kernel(const ProductArgs a) {
+  const uint64_t size = static_cast<uint64_t>(a.ni) * a.nj;
+  for (uint64_t t = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; t < size; t += static_cast<uint64_t>(gridDim.x) * 256) {
+    float v = a.add ? a.sum[t] : 0.0f;
+    for (uint32_t k = 0; k < a.splits; ++k) v += as_global(a.partial)[k * size + t];
+    using T = typename Elem<TO>::type;
+    if (a.last) as_global(static_cast<T*>(a.out.p))[t / a.nj * a.out.stride + t % a.nj] = static_cast<T>(v);
+    else a.sum[t] = v;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- on the host
+constexpr uint32_t kCus = 256;  // for sizes that must not depend on the device
+
+uint64_t padded(uint64_t n) { return (n + 127) / 128 * 128; }  // to two steps of a product
+
+// Classes of a piece: of as many logits as kPieceLogits, and of one size.
+constexpr uint64_t kPieceLogits = 1ull << 26, kLeastPiece = 1024, kMostPiece = 1ull << 20;
+uint64_t piece_of(uint64_t tokens, uint64_t classes) {
+  uint64_t most = kPieceLogits / tokens;
+  most = most < kLeastPiece ? kLeastPiece : (most > kMostPiece ? kMostPiece : most);
+  const uint64_t pieces = (classes + most - 1) / most, each = ((classes + pieces - 1) / pieces + 255) / 256 * 256;
+  return each < classes ? each : classes;
+}
+
+// Parts of the sum of a product whose result has fewer tiles of 64 x 64 than the card's CUs.
+uint32_t splits_of(uint64_t ni, uint64_t nj, uint64_t nc) {
+  const uint64_t tiles = ((ni + 63) / 64) * ((nj + 63) / 64), most = nc / 512;
+  if (tiles >= kCus || most < 2) return 1;
+  const uint64_t s = 2 * kCus / tiles;
+  return static_cast<uint32_t>(s < most ? s : most);
+}
+uint64_t partial_bytes(uint64_t ni, uint64_t nj, uint64_t nc) {
+  const uint64_t s = splits_of(ni, nj, nc);
+  return s > 1 ? whole(4 * s * ni * nj) : 0;
+}
+
+template <bool WEIGHT, uint32_t TO>
+void run_product(ProductArgs a, hipStream_t st) {
+  constexpr int kTerms = TO == kF32 ? 2 : 1;
+  const auto grid = [&](uint32_t t) {
+    a.tiles_i = tiles_of(a.ni, t);
+    a.tiles_j = tiles_of(a.nj, t);
+    return in_layers(static_cast<uint64_t>(a.tiles_i) * a.tiles_j, a.splits);
+  };
+  const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(a.ni, t)) * tiles_of(a.nj, t); };
+  a.splits = splits_of(a.ni, a.nj, a.nc);
+  a.each = tiles_of(a.nc, a.splits * 128) * 128;
+  a.splits = tiles_of(a.nc, a.each);
+  if (a.splits == 1 && count(256) > kCus / 2) {
+    const dim3 d = grid(256);
+    product_kernel<WEIGHT, TO, kTerms, 256, 256, 2, 4, 64 / kTerms><<<d, 512, 0, st>>>(a);
+  } else if (a.splits == 1 && count(128) * 2 > kCus) {
+    const dim3 d = grid(128);
+    product_kernel<WEIGHT, TO, kTerms, 128, 128, 2, 2, 64 / kTerms><<<d, 256, 0, st>>>(a);
+  } else {
+    const dim3 d = grid(64);
+    product_kernel<WEIGHT, TO, kTerms, 64, 64, 2, 2, 64><<<d, 256, 0, st>>>(a);
+    if (a.splits > 1) {
+      const uint64_t groups = (static_cast<uint64_t>(a.ni) * a.nj + 255) / 256;
+      join_parts_kernel<TO><<<static_cast<uint32_t>(groups < 4096 ? groups : 4096), 256, 0, st>>>(a);
+    }
+  }
+}
+
+template <int TERMS>
+void run_grads(const MatmulArgs& a, const LogitGrads& l, uint32_t n_cu, hipStream_t st) {
+  if (!enough_codes(a) || !near(a.a) || !near(a.b)) {
+    const uint64_t groups = (static_cast<uint64_t>(l.tokens_padded) * l.n_padded + 255) / 256;
+    grad_each_kernel<TERMS><<<static_cast<uint32_t>(groups < 65536 ? groups : 65536), 256, 0, st>>>(a, l);
+    return;
+  }
+  const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(a.m, t)) * tiles_of(a.n, t); };
+  const bool pieces = in_pieces(a.a) && in_pieces(a.b);
+  const uint32_t t = pieces && count(256) * 4 >= 3 * n_cu ? 256 : (count(128) >= n_cu ? 128 : 64), rows = tiles_of(a.m, t), cols = tiles_of(a.n, t);
+  const dim3 grid = in_layers(count(t));
+  if (t == 256) grad_tile_kernel<TERMS, 256, 256, 2, 4, true><<<grid, 512, 0, st>>>(a, l, rows, cols);
+  else if (t == 128 && pieces) grad_tile_kernel<TERMS, 128, 128, 2, 2, true><<<grid, 256, 0, st>>>(a, l, rows, cols);
+  else if (t == 128) grad_tile_kernel<TERMS, 128, 128, 2, 2, false><<<grid, 256, 0, st>>>(a, l, rows, cols);
+  else if (pieces) grad_tile_kernel<TERMS, 64, 64, 2, 2, true><<<grid, 256, 0, st>>>(a, l, rows, cols);
+  else grad_tile_kernel<TERMS, 64, 64, 2, 2, false><<<grid, 256, 0, st>>>(a, l, rows, cols);
+}
+
+template <uint32_t TO>
+__global__ __launch_bounds__(256) void zero_rows_kernel(const Mat out, uint64_t rows, uint32_t cols) {
+  using T = typename Elem<TO>::type;
+  const uint64_t size = rows * cols;
+  for (uint64_t t = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; t < size; t += static_cast<uint64_t>(gridDim.x) * 256)
+    as_global(static_cast<T*>(out.p))[t / cols * out.stride + t % cols] = static_cast<T>(0.0f);
+}
+
+}  // namespace
+
+uint64_t loss_grad_bytes(uint64_t tokens, uint64_t classes, uint64_t inputs) {
+  if (!tokens) return 0;
+  const uint64_t piece = piece_of(tokens, classes), t = padded(tokens), c = padded(piece), d = (inputs + 7) / 8 * 8;
+  const uint64_t px = partial_bytes(tokens, inputs, c), pw = partial_bytes(piece, inputs, t);
+  return whole(16 * t) + 2 * whole(4 * t) + whole(4) + whole(4 * classes) + whole(2 * t * d) + whole(2 * c * d) + 2 * whole(2 * t * c) + whole(4 * t * c) +
+         (piece < classes ? whole(4 * tokens * inputs) : 0) + (px > pw ? px : pw);
+}
+
+int launch_loss_grad(const LossGradArgs& a, uint32_t dx_type, uint32_t dw_type, void* workspace, uint32_t n_cu, void* stream) {
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  if (!a.tokens) {  // (dw is there)
+    const uint64_t groups = (static_cast<uint64_t>(a.classes) * a.inputs + 255) / 256;
+    const auto zero = dw_type == kF32 ? zero_rows_kernel<kF32> : zero_rows_kernel<kBF16>;
+    zero<<<static_cast<uint32_t>(groups < 4096 ? groups : 4096), 256, 0, st>>>(a.dw, a.classes, a.inputs);
+    return hipGetLastError();
+  }
+  const uint32_t piece = static_cast<uint32_t>(piece_of(a.tokens, a.classes)), parts = tiles_of(a.classes, piece);
+  const uint64_t t = padded(a.tokens), c = padded(piece);
+  const uint32_t d = (a.inputs + 7) / 8 * 8;
+  Arena arena{static_cast<char*>(workspace)};
+  GradWork g;
+  g.token = arena.take<Token>(t);
+  g.scale = arena.take<float>(t);
+  g.most = arena.take<float>(t);
+  g.most_w = arena.take<uint32_t>(1);
+  g.most_v = arena.take<uint32_t>(a.classes);
+  g.x = arena.take<_Float16>(t * d);
+  g.w = arena.take<_Float16>(c * d);
+  g.gx[0] = arena.take<_Float16>(t * c);
+  g.gx[1] = arena.take<_Float16>(t * c);
+  g.gw = arena.take<float>(t * c);
+  g.sum = parts > 1 ? arena.take<float>(static_cast<uint64_t>(a.tokens) * a.inputs) : nullptr;
+  g.partial = arena.take<float>(0);
+  const bool two = a.dx.p && dx_type == kF32;
+  for (uint32_t p = 0; p < parts; ++p) {
+    const uint32_t first = p * piece, n = a.classes - first < piece ? a.classes - first : piece;
+    const uint32_t n_padded = static_cast<uint32_t>(padded(n)), t_padded = static_cast<uint32_t>(t);
+    Mat w = a.w;
+    w.p = static_cast<int8_t*>(a.w.p) + first * a.w.stride;
+    w.s = a.w.s + first;
+    const Convert cw{w, g.w, n, a.inputs, d, static_cast<uint64_t>(n_padded) * (d / 8)};
+    const uint64_t groups_w = (cw.vectors + 256 * kConvert - 1) / (256 * kConvert);
+    if (p == 0) {
+      Prepare q{a, g, Convert{a.x, g.x, a.tokens, a.inputs, d, t * (d / 8)}, cw, t_padded, tiles_of(t_padded, 256), tiles_of(a.classes, 1024), 0};
+      q.groups_x = (q.x.vectors + 256 * kConvert - 1) / (256 * kConvert);
+      prepare_kernel<<<in_layers(1 + q.groups_t + q.groups_v + q.groups_x + groups_w), 256, 0, st>>>(q);
+    } else {
+      convert_kernel<<<in_layers(groups_w), 256, 0, st>>>(cw);
+    }
+    MatmulArgs m{a.x, w, Mat{}, a.tokens, n, a.inputs};
+    m.a.s = g.scale;
+    const LogitGrads l{g, first, t_padded, n_padded};
+    if (two) run_grads<2>(m, l, n_cu, st);
+    else run_grads<1>(m, l, n_cu, st);
+    ProductArgs pa{};
+    pa.gx[0] = g.gx[0];
+    pa.gx[1] = g.gx[1];
+    pa.gw = g.gw;
+    pa.g_stride = n_padded;
+    pa.nj = a.inputs;
+    pa.nj_padded = d;
+    pa.partial = g.partial;
+    if (a.dx.p) {
+      pa.q = g.w;
+      pa.most = reinterpret_cast<const uint32_t*>(g.most);
+      pa.times = g.most_w;
+      pa.out = a.dx;
+      pa.sum = g.sum;
+      pa.add = p > 0;
+      pa.last = p + 1 == parts;
+      pa.ni = a.tokens;
+      pa.nc = n_padded;
+      pa.ni_padded = t_padded;
+      if (dx_type == kF32) run_product<false, kF32>(pa, st);
+      else run_product<false, kBF16>(pa, st);
+    }
+    if (a.dw.p) {
+      pa.q = g.x;
+      pa.most = g.most_v + first;
+      pa.times = nullptr;
+      pa.out = a.dw;
+      pa.out.p = static_cast<char*>(a.dw.p) + first * a.dw.stride * (dw_type == kF32 ? 4 : 2);
+      pa.sum = nullptr;
+      pa.add = false;
+      pa.last = true;
+      pa.ni = n;
+      pa.nc = t_padded;
+      pa.ni_padded = n_padded;
+      if (dw_type == kF32) run_product<true, kF32>(pa, st);
+      else run_product<true, kBF16>(pa, st);
+    }
+  }
+  return hipGetLastError();
+}
+
+}  // namespace stq

@@ -4,7 +4,7 @@
 
 namespace stq {
 
-enum MatrixType : uint32_t { kF32 = 0, kBF16 = 1, kQ8 = 2 };
+enum MatrixType : uint32_t { kF32 = 0, kBF16 = 1, kQ8 = 2, kF16 = 3 };  // (fp16: in workspaces only)
 
 // A matrix as the kernels see it: rows of `stride` elements; the scales of an 8-bit one, `per_row` for each row, one for
 // each 2^lg columns (lg = 0: per_row = 1, one for the row).
@@ -63,8 +63,6 @@ struct LossGradArgs {
   const float* lse;
   const float* dloss;
   const float* dlse;  // or null
-  void* token;    // parts of the workspace, set by the launcher
-  float* scale;
   uint32_t tokens, classes, inputs;
 };
 
@@ -88,7 +86,7 @@ int launch_matmul_grad_weight(const MatmulArgs& a, uint32_t dy_type, uint32_t ou
 uint64_t grad_weight_bytes(uint64_t m, uint64_t n, uint64_t k);
 int launch_loss(const LossArgs& a, void* workspace, uint32_t n_cu, void* stream);
 uint64_t loss_bytes(uint64_t tokens, uint64_t classes);
-int launch_loss_grad(LossGradArgs a, uint32_t dx_type, uint32_t dw_type, void* workspace, uint32_t n_cu, void* stream);
+int launch_loss_grad(const LossGradArgs& a, uint32_t dx_type, uint32_t dw_type, void* workspace, uint32_t n_cu, void* stream);
 uint64_t loss_grad_bytes(uint64_t tokens, uint64_t classes, uint64_t inputs);
 
 }  // namespace stq

@@ -49,7 +49,8 @@ __device__ __forceinline__ void pack4(const float (&v)[4], void* to) {  // in LD
   if constexpr (TO == kF32) {
     __builtin_memcpy(to, v, 16);
   } else {
-    const __bf16 h[4] = {static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1]), static_cast<__bf16>(v[2]), static_cast<__bf16>(v[3])};
+    using T = typename Elem<TO>::type;
+    const T h[4] = {static_cast<T>(v[0]), static_cast<T>(v[1]), static_cast<T>(v[2]), static_cast<T>(v[3])};
     uint64_t w;
     __builtin_memcpy(&w, h, 8);
     __builtin_memcpy(to, &w, 8);
@@ -80,9 +81,13 @@ __device__ __forceinline__ void lanes_meet() {
 // A wave's result, FI x FJ fragments of 32 x 32 from row0, col0 on, into an output of rows x cols, by way of 32 rows of LDS of its own
 // (`box`, 4096 FJ bytes for fp32), so that whole pieces of rows are stored, neighbouring ones together.  value(i, j, p, e): column
 // 8 p + 4 (lane / 32) + e of row lane % 32 of fragment i, j.  Pieces lie at the places that their number and the row's give by
-// exclusive or.
-template <uint32_t TO, uint32_t FI, uint32_t FJ, class F>
-__device__ __forceinline__ void store_tile(const Mat& out, uint32_t row0, uint32_t col0, uint32_t rows, uint32_t cols, char* box, uint32_t lane, F value) {
+// exclusive or.  seen(v): every piece on its way, those beyond the output among them; a lane's have its number modulo a row's pieces.
+struct Unseen {
+  __device__ __forceinline__ void operator()(const Piece&) const {}
+};
+template <uint32_t TO, uint32_t FI, uint32_t FJ, class F, class SEEN = Unseen>
+__device__ __forceinline__ void store_tile(const Mat& out, uint32_t row0, uint32_t col0, uint32_t rows, uint32_t cols, char* box, uint32_t lane, F value,
+                                           SEEN seen = SEEN{}) {
   constexpr uint32_t kSize = TO == kF32 ? 4 : 2, kRow = FJ * 32 * kSize, kPieces = kRow / 16, kShift = kRow == 256 ? 0 : (kRow == 128 ? 1 : 2);
   const auto place = [&](uint32_t row, uint32_t piece) { return row * kRow + ((piece ^ (row >> kShift)) & (kPieces - 1)) * 16; };
 #pragma unroll
@@ -103,6 +108,7 @@ __device__ __forceinline__ void store_tile(const Mat& out, uint32_t row0, uint32
       const uint32_t row = h * (64 / kPieces) + lane / kPieces, piece = lane % kPieces;
       Piece v;
       __builtin_memcpy(&v, box + place(row, piece), 16);
+      seen(v);
       const uint32_t r = row0 + i * 32 + row, c = col0 + piece * (16 / kSize);
       if (r < rows && c < cols) store_piece<TO>(out, r, c, cols, v);
     }

@@ -23,6 +23,7 @@ template <uint32_t TY> struct Elem;
 template <> struct Elem<kF32> { using type = float; };
 template <> struct Elem<kBF16> { using type = __bf16; };
 template <> struct Elem<kQ8> { using type = int8_t; };
+template <> struct Elem<kF16> { using type = _Float16; };
 
 // Eight elements as they are stored, in whole words: loads that are under way must not be taken apart before they are needed.
 template <class T>

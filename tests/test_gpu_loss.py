@@ -4,7 +4,9 @@ strides, tokens without a target, tokens predicted with certainty, rows that are
 Tolerances follow from the arithmetic (u = 2^-24, b = 2^-8): a logit is off by 3 roundings; an exponential's argument by those of the logit, of its
 reference and of a difference and a product, its value by two units in the last place more; sums of n terms are taken in parts of which none
 is longer than n / 64 + 64.  Factors of the gradients' products enter with 11 significant bits (half a step: 2^-11) for results in
-bf16 and with 22 (2^-22) for results in fp32, below 2^-24 of 2^15 of a row's largest with that much absolutely."""
+bf16 and with 22 (2^-22) for results in fp32.  They are fp16 numbers, whose steps are 2^-24 at least (half of one: 2^-25), after a power of two
+that brings the largest of the result's row to 2^14 or above: 2^-39 of that largest is what any of them may be off absolutely.  The largest
+of a row of dx is what a token's own loss bounds it by, max(|dloss + dlse| (1 - p), |g at the target|), with the largest of the classes' scales."""
 import math
 
 import pytest
@@ -112,13 +114,17 @@ def check_backward(p, dx, dw, dlse=None):
         + 8 * U * (dl.abs()[there] * sure + dloss.abs()[there] * (1 - sure))
     g_off += 2.0 ** -148
     w, x = p.w.value(), p.x.value()
-    for out, f, f_off, m, scale, n in ((dx, g, g_off, w, p.w.s, p.v), (dw, g.t(), g_off.t(), x, p.x.s, p.t)):
+    largest = torch.where(there, (dloss + dl).abs() * -torch.expm1(-loss), dl.abs())
+    largest[rows] = torch.maximum(largest[rows], g[rows, p.target[there]].abs())
+    largest = largest[:, None] * p.w.s.double().max()
+    largest_of_class = (g.t().abs() * p.x.s.double().view(1, -1)).amax(1, keepdim=True)
+    for out, f, f_off, m, scale, n, most in ((dx, g, g_off, w, p.w.s, p.v, largest), (dw, g.t(), g_off.t(), x, p.x.s, p.t, largest_of_class)):
         if out is None:
             continue
         bf16 = out.t.dtype == torch.bfloat16
         term = 2.0 ** -11 if bf16 else 2.0 ** -22
         size = f.abs() @ m.abs()
-        least = (f.abs() * scale.double().view(1, -1)).amax(1, keepdim=True) * 2.0 ** -39 * m.div(scale.double()).abs().sum(0, keepdim=True)
+        least = most * 2.0 ** -39 * (1 + B) * m.div(scale.double()).abs().sum(0, keepdim=True)
         # (a factor g * scale is rounded to fp32, whose numbers below 2^-126 are 2^-149 apart)
         least = least + 2.0 ** -149 * m.div(scale.double()).abs().sum(0, keepdim=True)
         want = f @ m
