@@ -1,11 +1,11 @@
 // gfx950 kernels of the gradients of the softmax cross entropy over 8-bit codes.
 //
 // g[t][v], the gradient of a logit, is computed in tiles of the logits as the forward pass has them, a piece of the classes at a time, and
-// written twice: times the classes' scales as the factors of dx, times the tokens' as those of dw.  The products take these factors as
-// fp16, as one term of 11 bits for results in bf16 and as two, 22 bits, for results in fp32, after a power of two for each row of the
-// result that brings the row's largest into [2^14, 2^15): what lies 2^-29 below that loses bits, and what lies 2^-39 below it counts as 0.
-// For dx a bound on the row's largest is known beforehand (|g| <= |dloss + dlse| (1 - p) but at the target), so that its factors are
-// written in fp16; for dw it is gathered while g is written, in fp32.  Codes are exact in fp16.
+// written twice in fp16: times the classes' scales as the factors of dx, times the tokens' as those of dw.  Results in bf16 take one term of 11
+// bits, results in fp32 two, 22 bits.  A power of two goes with them that brings the largest into [2^14, 2^15): what lies 2^-29 below it loses
+// bits, and what lies 2^-39 below it counts as 0.  For dx it is one for each token, whose largest has a bound that is known beforehand
+// (|g| <= |dloss + dlse| (1 - p) but at the target); for dw it is one for each class and tile of tokens, and the sums change their unit
+// from tile to tile.  Codes are exact in fp16.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -25,8 +25,7 @@ __device__ __forceinline__ uint32_t factor_exponent(uint32_t most) {
   const uint32_t e = most >> 23;
   return e >= 255 ? 7u : min(268u - e, 253u);
 }
-__device__ __forceinline__ float factor(uint32_t most) { return u2f(factor_exponent(most) << 23); }
-[[maybe_unused]] __device__ __forceinline__ float back(uint32_t most) { return u2f((254u - factor_exponent(most)) << 23); }
+[[maybe_unused]] __device__ __forceinline__ float power(uint32_t exponent) { return u2f(exponent << 23); }  // 1 to 254
 
 // What the tiles of the logits need of a token.
 struct Token {
@@ -40,11 +39,11 @@ struct GradWork {  // parts of the workspace
   float* scale;      // [tokens, padded]: of the codes, or 0 for a token that takes no part
   float* most;       // [tokens, padded]: a bound on |g| of the row
   uint32_t* most_w;  // the largest of the classes' scales (bits)
-  uint32_t* most_v;  // [classes]: the largest |g * scale| of a class (bits)
   _Float16* x;       // [tokens, padded][inputs, padded]: codes, zeros beyond the matrix
   _Float16* w;       // [classes of a piece, padded][inputs, padded]
   _Float16* gx[2];   // [tokens, padded][classes of a piece, padded]: factors of dx, one or two terms
-  float* gw;         // the same: factors of dw
+  _Float16* gw[2];   // the same: factors of dw
+  uint8_t* unit;     // [tiles of tokens][classes of a piece, padded]: exponents of the powers of two that go with gw
   float* sum;        // [tokens][inputs]: of dx, where there are several pieces
   float* partial;    // parts of a product that is taken in several
 };
@@ -78,14 +77,13 @@ struct Convert {
 };
 __global__ __launch_bounds__(256) void convert_kernel(const Convert w) { w(group_number()); }
 
-// In one launch what is there before the first piece: the tokens' data, the largest scale of a class, zeros in place of the classes'
-// largest, x and the first piece of w in fp16.
+// In one launch what is there before the first piece: the tokens' data, the largest scale of a class, x and the first piece of w in fp16.
 struct Prepare {
   LossGradArgs a;
   GradWork g;
   Convert x, w;
   uint32_t tokens_padded;
-  uint32_t groups_t, groups_v;
+  uint32_t groups_t;
   uint64_t groups_x;
 };
 __global__ __launch_bounds__(256) void prepare_kernel(const Prepare p) {
@@ -128,10 +126,7 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Prepare p) {
     p.g.token[token] = t;
     p.g.scale[token] = scale;
     p.g.most[token] = most;
-  } else if ((group -= p.groups_t) < p.groups_v) {
-    for (uint32_t e = 0; e < 4; ++e)
-      if (const uint64_t c = group * 1024 + e * 256 + threadIdx.x; c < a.classes) p.g.most_v[c] = 0;
-  } else if ((group -= p.groups_v) < p.groups_x) {
+  } else if ((group -= p.groups_t) < p.groups_x) {
     p.x(group);
   } else if ((group -= p.groups_x) * (256 * kConvert) < p.w.vectors) {
     p.w(group);
@@ -148,8 +143,8 @@ __device__ __forceinline__ float grad_of(float z, const Token& t) { return t.c *
 template <int TERMS>
 __device__ __forceinline__ float term(float x, int k) { return TERMS == 2 && k ? x - static_cast<float>(static_cast<_Float16>(x)) : x; }
 
-// a.a.s: the scales of GradWork, a.b and a.n: of the piece.  In front of the products: 11 of 100 parts of the time.
-template <int TERMS, int TM, int TN, int WM, int WN, bool PIECES>
+// a.a.s: the scales of GradWork, a.b and a.n: of the piece.
+template <int TX, int TW, int TM, int TN, int WM, int WN, bool PIECES>
 __global__ __launch_bounds__(WM * WN * 64) void grad_tile_kernel(const MatmulArgs a, const LogitGrads l, uint32_t tiles_m, uint32_t tiles_n) {
   constexpr uint32_t FM = TM / WM / 32, FN = TN / WN / 32;
   code_tile<TM, TN, WM, WN, PIECES>(a, tiles_m, tiles_n, [&](auto& acc, const CodeTile& t) __attribute__((always_inline)) {
@@ -162,7 +157,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grad_tile_kernel(const MatmulArg
       const uint32_t row = t.wm + i * 32 + (t.lane & 31), token = t.m0 + row;
       const Token k = l.g.token[min(token, l.tokens_padded - 1)];
       scale[i] = token < a.m ? t.sm[row] : 0.0f;
-      times[i] = factor(f2u(l.g.most[min(token, l.tokens_padded - 1)] * most_w));
+      times[i] = power(factor_exponent(f2u(l.g.most[min(token, l.tokens_padded - 1)] * most_w)));
       const uint32_t at = k.target - l.first - first;  // column 32 j + 8 p + e of the lane's
       float v[FN * 16];
 #pragma unroll
@@ -185,58 +180,82 @@ __global__ __launch_bounds__(WM * WN * 64) void grad_tile_kernel(const MatmulArg
         for (uint32_t c = 0; c < 16; ++c) acc[i][j][c] = static_cast<int>(f2u(v[j * 16 + c]));
       __builtin_amdgcn_sched_barrier(0);  // (one row's at a time, for the registers)
     }
-    const auto g = [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return u2f(static_cast<uint32_t>(acc[i][j][p * 4 + e])); };
+    // the largest |g * scale| of the tile's columns, by way of LDS, and the powers of two that follow
+    uint32_t* const held = reinterpret_cast<uint32_t*>(t.spare);  // [WM][TN]
+    float* const powers = reinterpret_cast<float*>(held + WM * TN);
 #pragma unroll
-    for (int k = 0; k < TERMS; ++k)
-      store_tile<kF16, FM, FN>(Mat{l.g.gx[k], nullptr, l.n_padded, 0, 0}, t.m0 + t.wm, t.n0 + t.wn, l.tokens_padded, l.n_padded, t.box, t.lane,
-                               [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return term<TERMS>(g(i, j, p, e) * sn[j * 32 + p * 8 + e] * times[i], k); });
-    // the largest of each column, from the pieces of rows on their way: four columns to a lane
-    uint32_t most[4] = {0, 0, 0, 0};
-    store_tile<kF32, FM, FN>(Mat{l.g.gw, nullptr, l.n_padded, 0, 0}, t.m0 + t.wm, t.n0 + t.wn, l.tokens_padded, l.n_padded, t.box, t.lane,
-                             [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return g(i, j, p, e) * scale[i]; },
-                             [&](const Piece& v) {
+    for (uint32_t c = 0; c < FN * 16; ++c) {
+      uint32_t m = 0;
 #pragma unroll
-                               for (uint32_t e = 0; e < 4; ++e) most[e] = max(most[e], v.w[e] & 0x7FFFFFFFu);
-                             });
-    constexpr uint32_t kPieces = FN * 8;
-#pragma unroll
-    for (uint32_t e = 0; e < 4; ++e) {
-#pragma unroll
-      for (uint32_t o = kPieces; o < 64; o *= 2) most[e] = max(most[e], static_cast<uint32_t>(__shfl_xor(static_cast<int>(most[e]), o)));
-      const uint32_t c = t.n0 + t.wn + t.lane * 4 + e;
-      if (t.lane < kPieces && c < a.n && most[e]) atomicMax(l.g.most_v + l.first + c, most[e]);
+      for (uint32_t i = 0; i < FM; ++i) m = max(m, f2u(u2f(static_cast<uint32_t>(acc[i][c / 16][c % 16])) * scale[i]) & 0x7FFFFFFFu);
+      m = row_max(m);
+      m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16)));
+      if ((t.lane & 31) == c) held[t.wave / WN * TN + t.wn + c / 16 * 32 + c % 16 / 4 * 8 + half * 4 + c % 4] = m;
     }
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < TN; c += WM * WN * 64) {
+      uint32_t m = held[c];
+#pragma unroll
+      for (uint32_t w = 1; w < WM; ++w) m = max(m, held[w * TN + c]);
+      const uint32_t e = factor_exponent(m);
+      powers[c] = power(e);
+      if (t.n0 + c < l.n_padded) l.g.unit[static_cast<uint64_t>(t.m0 / TM) * l.n_padded + t.n0 + c] = static_cast<uint8_t>(e);
+    }
+    __syncthreads();
+    const auto g = [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return u2f(static_cast<uint32_t>(acc[i][j][p * 4 + e])); };
+    const float* const pn = powers + t.wn + 4 * half;
+#pragma unroll
+    for (int k = 0; k < TX; ++k)
+      store_tile<kF16, FM, FN>(Mat{l.g.gx[k], nullptr, l.n_padded, 0, 0}, t.m0 + t.wm, t.n0 + t.wn, l.tokens_padded, l.n_padded, t.box, t.lane,
+                               [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return term<TX>(g(i, j, p, e) * sn[j * 32 + p * 8 + e] * times[i], k); });
+#pragma unroll
+    for (int k = 0; k < TW; ++k)
+      store_tile<kF16, FM, FN>(Mat{l.g.gw[k], nullptr, l.n_padded, 0, 0}, t.m0 + t.wm, t.n0 + t.wn, l.tokens_padded, l.n_padded, t.box, t.lane,
+                               [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return term<TW>(g(i, j, p, e) * scale[i] * pn[j * 32 + p * 8 + e], k); });
     if constexpr (TM < 128) {  // rows and columns of zeros that no tile covers
       const uint32_t row_end = t.m0 + TM, col_end = t.n0 + TN;
       const bool last_row = row_end >= a.m, last_col = col_end >= a.n;
       for (uint32_t k = threadIdx.x; k < TM * TN; k += WM * WN * 64) {
         const uint32_t r = k / TN, c = k % TN;
-        if (last_row && row_end + r < l.tokens_padded && t.n0 + c < l.n_padded) l.g.gw[static_cast<uint64_t>(row_end + r) * l.n_padded + t.n0 + c] = 0.0f;
+        if (last_row && row_end + r < l.tokens_padded && t.n0 + c < l.n_padded) {
+          for (int i = 0; i < TW; ++i) l.g.gw[i][static_cast<uint64_t>(row_end + r) * l.n_padded + t.n0 + c] = static_cast<_Float16>(0.0f);
+          if (r == 0) l.g.unit[static_cast<uint64_t>(row_end / TM) * l.n_padded + t.n0 + c] = 253;
+        }
         if (last_col && col_end + c < l.n_padded && t.m0 + r < l.tokens_padded)
-          for (int i = 0; i < TERMS; ++i) l.g.gx[i][static_cast<uint64_t>(t.m0 + r) * l.n_padded + col_end + c] = static_cast<_Float16>(0.0f);
+          for (int i = 0; i < TX; ++i) l.g.gx[i][static_cast<uint64_t>(t.m0 + r) * l.n_padded + col_end + c] = static_cast<_Float16>(0.0f);
       }
     }
   });
 }
 
-// The same of a thread's own logits: operands of fewer than 16 codes, or of rows too far apart for the offsets of a tile.
-template <int TERMS>
+// The same of operands of fewer than 16 codes, or of rows too far apart for the offsets of a tile: a class and kEachTokens tokens to a thread.
+constexpr uint32_t kEachTokens = 64;
+template <int TX, int TW>
 __global__ __launch_bounds__(256) void grad_each_kernel(const MatmulArgs a, const LogitGrads l) {
-  const uint64_t total = static_cast<uint64_t>(l.tokens_padded) * l.n_padded;
+  const uint64_t total = static_cast<uint64_t>(l.tokens_padded / kEachTokens) * l.n_padded;
   const float most_w = u2f(*l.g.most_w);
-  for (uint64_t at = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; at < total; at += static_cast<uint64_t>(gridDim.x) * 256) {
-    const uint32_t token = static_cast<uint32_t>(at / l.n_padded), c = static_cast<uint32_t>(at % l.n_padded);
-    float gx = 0.0f, gw = 0.0f;
-    if (token < a.m && c < a.n) {
+  for (uint64_t n = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; n < total; n += static_cast<uint64_t>(gridDim.x) * 256) {
+    const uint32_t c = static_cast<uint32_t>(n % l.n_padded), from = static_cast<uint32_t>(n / l.n_padded) * kEachTokens;
+    const auto grad = [&](uint32_t token) {
+      if (token >= a.m || c >= a.n) return 0.0f;
       const Token k = l.g.token[token];
-      const float g = k.target == l.first + c ? k.at_target : grad_of(a.a.s[token] == 0.0f ? 0.0f : logit(a, token, c), k);
-      gx = g * a.b.s[c] * factor(f2u(l.g.most[token] * most_w));
-      gw = g * a.a.s[token];
-      if (const uint32_t m = f2u(gw) & 0x7FFFFFFFu) atomicMax(l.g.most_v + l.first + c, m);
-    }
+      return k.target == l.first + c ? k.at_target : grad_of(a.a.s[token] == 0.0f ? 0.0f : logit(a, token, c), k);
+    };
+    uint32_t most = 0;
+    for (uint32_t r = 0; r < kEachTokens; ++r)
+      if (from + r < a.m) most = max(most, f2u(grad(from + r) * a.a.s[from + r]) & 0x7FFFFFFFu);
+    const uint32_t e = factor_exponent(most);
+    l.g.unit[n] = static_cast<uint8_t>(e);
+    for (uint32_t r = 0; r < kEachTokens; ++r) {
+      const uint32_t token = from + r;
+      const bool in = token < a.m && c < a.n;
+      const float g = grad(token), gx = in ? g * a.b.s[c] * power(factor_exponent(f2u(l.g.most[token] * most_w))) : 0.0f, gw = in ? g * a.a.s[token] * power(e) : 0.0f;
+      const uint64_t at = static_cast<uint64_t>(token) * l.n_padded + c;
 #pragma unroll
-    for (int k = 0; k < TERMS; ++k) l.g.gx[k][at] = static_cast<_Float16>(term<TERMS>(gx, k));
-    l.g.gw[at] = gw;
+      for (int k = 0; k < TX; ++k) l.g.gx[k][at] = static_cast<_Float16>(term<TX>(gx, k));
+#pragma unroll
+      for (int k = 0; k < TW; ++k) l.g.gw[k][at] = static_cast<_Float16>(term<TW>(gw, k));
+    }
   }
 }
 
@@ -244,12 +263,13 @@ __global__ __launch_bounds__(256) void grad_each_kernel(const MatmulArgs a, cons
 // out[i][j] = sum over c of g(i, c) * q(c, j): with respect to x (WEIGHT false) i is the token and c the class, with respect to w i is the
 // class and c the token.
 struct ProductArgs {
-  const _Float16* gx[2];  // [ni, padded][nc]
-  const float* gw;        // [nc][ni, padded]
+  const _Float16* g[2];   // [ni, padded][nc], with respect to w [nc][ni, padded]
   const _Float16* q;      // [nc][nj, padded]
   uint64_t g_stride;
-  const uint32_t* most;   // [ni]: bits of a row's largest, or of a bound on it ...
-  const uint32_t* times;  // ... which this is a factor of (null: 1)
+  const float* most;      // with respect to x: [ni], and the classes' largest scale (bits), as the tiles had them
+  const uint32_t* most_w;
+  const uint8_t* unit;    // with respect to w: [nc / unit_rows][ni, padded]
+  uint32_t unit_rows;
   Mat out;
   float* sum;             // [ni][nj]: what is added (with `add`), and where the result goes that is not the last part
   bool add, last;
@@ -346,7 +366,7 @@ __device__ __forceinline__ void store_sums(const ProductArgs& a, uint32_t row0, 
 }
 
 // A workgroup has TI x TJ of the result, its WI x WJ waves a part each, and takes STEP of c at a time, out of one of two LDS buffers while the
-// other is filled: codes and the factors of dx are loaded straight into LDS, those of dw by way of registers, where they become fp16.
+// other is filled by loads straight into it.
 template <bool WEIGHT, uint32_t TO, int TERMS, int TI, int TJ, int WI, int WJ, int STEP>
 __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const ProductArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host's compiler has no buffer descriptors)
@@ -367,12 +387,11 @@ __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const ProductArgs
     const uint32_t n = (i * (kThreads / 64) + wave) * 64 + lane, row = n / (TJ / 8), piece = (n % (TJ / 8)) ^ swizzle_x<TJ>(row);
     ob[i] = (row * a.nj_padded + min(j0 + piece * 8, a.nj_padded - 8)) * 2;
   }
-  if constexpr (!WEIGHT) {
 #pragma unroll
-    for (uint32_t i = 0; i < LA; ++i) {
-      const uint32_t n = (i * (kThreads / 64) + wave) * 64 + lane, row = n / (STEP / 8), piece = (n % (STEP / 8)) ^ swizzle_c<STEP>(row);
-      oa[i] = (min(i0 + row, a.ni_padded - 1) - i0) * static_cast<uint32_t>(a.g_stride) * 2 + piece * 16;
-    }
+  for (uint32_t i = 0; i < LA; ++i) {
+    const uint32_t n = (i * (kThreads / 64) + wave) * 64 + lane, row = n / (WEIGHT ? TI / 8 : STEP / 8), slot = n % (WEIGHT ? TI / 8 : STEP / 8);
+    if (WEIGHT) oa[i] = (row * static_cast<uint32_t>(a.g_stride) + min(i0 + (slot ^ swizzle_x<TI>(row)) * 8, a.ni_padded - 8)) * 2;
+    else oa[i] = (min(i0 + row, a.ni_padded - 1) - i0) * static_cast<uint32_t>(a.g_stride) * 2 + (slot ^ swizzle_c<STEP>(row)) * 16;
   }
   const auto load_b = [&](uint32_t c, _Float16* to) __attribute__((always_inline)) {
     if (c >= end) return;
@@ -385,42 +404,11 @@ __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const ProductArgs
     if (c >= end) return;
 #pragma unroll
     for (int k = 0; k < TERMS; ++k) {
-      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(a.gx[k]) + static_cast<uint64_t>(i0) * a.g_stride + c, 0, 0x7FFFFFFF, 0x00020000);
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(a.g[k]) + (WEIGHT ? c * a.g_stride : i0 * a.g_stride + c), 0, 0x7FFFFFFF, 0x00020000);
 #pragma unroll
       for (uint32_t i = 0; i < LA; ++i)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (STQ_LDS void*)(to[k] + (i * (kThreads / 64) + wave) * 512), 16, oa[i], 0, 0, 0);
     }
-  };
-  // dw: vectors of eight classes of one token, kThreads / (TI / 8) tokens apart
-  constexpr uint32_t kApart = kThreads / (TI / 8);
-  const uint32_t ar = threadIdx.x / (TI / 8), ac = threadIdx.x % (TI / 8);
-  const uint32_t ao = ar * static_cast<uint32_t>(a.g_stride) + min(i0 + ac * 8, a.ni_padded - 8);
-  Packed<float> va[WEIGHT ? LA : 1];
-  float times[WEIGHT ? 8 : 1];
-  const auto most_of = [&](uint32_t i) {
-    const uint32_t m = as_global(a.most)[min(i, a.ni - 1)];
-    return a.times ? f2u(u2f(m) * u2f(*a.times)) : m;
-  };
-  if constexpr (WEIGHT) {
-#pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) times[e] = factor(most_of(i0 + ac * 8 + e));
-  }
-  const auto load_regs = [&](uint32_t c) __attribute__((always_inline)) {
-    if (c >= end) return;
-#pragma unroll
-    for (uint32_t h = 0; h < LA; ++h) va[h] = load_packed(a.gw + (static_cast<uint64_t>(c) + kApart * h) * a.g_stride + ao);
-  };
-  const auto put = [&](uint32_t h, _Float16 (*to)[kSizeA]) __attribute__((always_inline)) {
-    const uint32_t row = ar + kApart * h;
-    v8h t[TERMS];
-#pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) {
-      const float x = va[h].at(e) * times[e];
-#pragma unroll
-      for (int k = 0; k < TERMS; ++k) t[k][e] = static_cast<_Float16>(term<TERMS>(x, k));
-    }
-#pragma unroll
-    for (int k = 0; k < TERMS; ++k) __builtin_memcpy(&to[k][row * TI + (ac ^ swizzle_x<TI>(row)) * 8], &t[k], 16);
   };
   v16f acc[FI][FJ] = {};
   const uint32_t wi = wave / WJ * (TI / WI), wj = wave % WJ * (TJ / WJ);
@@ -447,44 +435,63 @@ __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const ProductArgs
       if (u == kUnits - kAhead) {
         __syncthreads();
         load_b(c + 2 * STEP, tb);
-        if constexpr (WEIGHT) load_regs(c + 2 * STEP);
-        else load_a(c + 2 * STEP, ta);
+        load_a(c + 2 * STEP, ta);
       }
 #pragma unroll
       for (uint32_t j = 0; j < FJ; ++j) acc[u % FI][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fb[u / (TERMS * FI) & 1][j], fa[u % kAhead], acc[u % FI][j], 0, 0, 0);
       if (u + kAhead < kUnits) read(u + kAhead, ta, tb);
       else read(u + kAhead - kUnits, na, nb);
-      if constexpr (WEIGHT) {  // the next step's factors, late in the step
-        constexpr uint32_t kFrom = kUnits - kAhead > LA ? kUnits - kAhead - LA : 0;
-#pragma unroll
-        for (uint32_t h = 0; h < LA; ++h)
-          if (u == min(kFrom + h, kUnits - kAhead - 1)) put(h, na);
-      }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
   load_b(first, b0);
-  if constexpr (WEIGHT) {
-    load_regs(first);
+  load_a(first, a0);
+  // dw: the sums are in units of 2^-unit, those of the factors at work.  A tile of factors 2^64 and more below the largest so far is taken as
+  // if it were 2^64 below, so that the sums stay within fp32: it adds nothing to them either way.
+  uint32_t unit[FI], next[FI], largest[FI];
+  const auto load_units = [&](uint32_t c) __attribute__((always_inline)) {
+    if (c >= end) return;
 #pragma unroll
-    for (uint32_t h = 0; h < LA; ++h) put(h, a0);
-    load_regs(first + STEP);
-  } else {
-    load_a(first, a0);
+    for (uint32_t i = 0; i < FI; ++i)
+      next[i] = as_global(a.unit)[static_cast<uint64_t>(c / a.unit_rows) * a.ni_padded + min(i0 + wi + i * 32 + (lane & 31), a.ni_padded - 1)];
+  };
+  const auto change_units = [&](uint32_t c) __attribute__((always_inline)) {
+    if (c % a.unit_rows || c >= end) return;
+#pragma unroll
+    for (uint32_t i = 0; i < FI; ++i) {
+      largest[i] = min(largest[i], next[i]);
+      const uint32_t to = min(next[i], largest[i] + 64);
+      const float by = power(to + 127u < unit[i] ? 0u : to + 127u - unit[i]);  // (up to 2^64; 0 for 2^-127 and below)
+      unit[i] = to;
+#pragma unroll
+      for (uint32_t j = 0; j < FJ; ++j) acc[i][j] *= by;
+    }
+    load_units(c + a.unit_rows);
+  };
+  if constexpr (WEIGHT) {
+    load_units(first);
+#pragma unroll
+    for (uint32_t i = 0; i < FI; ++i) unit[i] = largest[i] = next[i];
+    load_units(first / a.unit_rows * a.unit_rows + a.unit_rows);
   }
   __syncthreads();
   load_b(first + STEP, b1);
-  if constexpr (!WEIGHT) load_a(first + STEP, a1);
+  load_a(first + STEP, a1);
 #pragma unroll
   for (uint32_t u = 0; u < kAhead; ++u) read(u, a0, b0);
   // (what the last step reads ahead is not used)
   for (uint32_t c = first; c < end; c += 2 * STEP) {
+    if (WEIGHT && c != first) change_units(c);
     work(c, a0, b0, a1, b1);
+    if (WEIGHT) change_units(c + STEP);
     work(c + STEP, a1, b1, a0, b0);
   }
   float undo[FI];
 #pragma unroll
-  for (uint32_t i = 0; i < FI; ++i) undo[i] = back(most_of(i0 + wi + i * 32 + (lane & 31)));
+  for (uint32_t i = 0; i < FI; ++i) {
+    if constexpr (!WEIGHT) unit[i] = factor_exponent(f2u(as_global(a.most)[min(i0 + wi + i * 32 + (lane & 31), a.ni - 1)] * u2f(*a.most_w)));
+    undo[i] = power(254u - unit[i]);
+  }
   __syncthreads();
   constexpr uint32_t kBox = 32 * FJ * 32 * 4, kHalf = WI * WJ / 2;
   char* const box = wave < kHalf ? reinterpret_cast<char*>(a0) + wave * kBox : reinterpret_cast<char*>(a1) + (wave - kHalf) * kBox;
@@ -560,22 +567,24 @@ void run_product(ProductArgs a, hipStream_t st) {
   }
 }
 
-template <int TERMS>
-void run_grads(const MatmulArgs& a, const LogitGrads& l, uint32_t n_cu, hipStream_t st) {
+// The tokens of a tile.
+template <int TX, int TW>
+uint32_t run_grads(const MatmulArgs& a, const LogitGrads& l, uint32_t n_cu, hipStream_t st) {
   if (!enough_codes(a) || !near(a.a) || !near(a.b)) {
-    const uint64_t groups = (static_cast<uint64_t>(l.tokens_padded) * l.n_padded + 255) / 256;
-    grad_each_kernel<TERMS><<<static_cast<uint32_t>(groups < 65536 ? groups : 65536), 256, 0, st>>>(a, l);
-    return;
+    const uint64_t groups = (static_cast<uint64_t>(l.tokens_padded / kEachTokens) * l.n_padded + 255) / 256;
+    grad_each_kernel<TX, TW><<<static_cast<uint32_t>(groups < 65536 ? groups : 65536), 256, 0, st>>>(a, l);
+    return kEachTokens;
   }
   const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(a.m, t)) * tiles_of(a.n, t); };
   const bool pieces = in_pieces(a.a) && in_pieces(a.b);
   const uint32_t t = pieces && count(256) * 4 >= 3 * n_cu ? 256 : (count(128) >= n_cu ? 128 : 64), rows = tiles_of(a.m, t), cols = tiles_of(a.n, t);
   const dim3 grid = in_layers(count(t));
-  if (t == 256) grad_tile_kernel<TERMS, 256, 256, 2, 4, true><<<grid, 512, 0, st>>>(a, l, rows, cols);
-  else if (t == 128 && pieces) grad_tile_kernel<TERMS, 128, 128, 2, 2, true><<<grid, 256, 0, st>>>(a, l, rows, cols);
-  else if (t == 128) grad_tile_kernel<TERMS, 128, 128, 2, 2, false><<<grid, 256, 0, st>>>(a, l, rows, cols);
-  else if (pieces) grad_tile_kernel<TERMS, 64, 64, 2, 2, true><<<grid, 256, 0, st>>>(a, l, rows, cols);
-  else grad_tile_kernel<TERMS, 64, 64, 2, 2, false><<<grid, 256, 0, st>>>(a, l, rows, cols);
+  if (t == 256) grad_tile_kernel<TX, TW, 256, 256, 2, 4, true><<<grid, 512, 0, st>>>(a, l, rows, cols);
+  else if (t == 128 && pieces) grad_tile_kernel<TX, TW, 128, 128, 2, 2, true><<<grid, 256, 0, st>>>(a, l, rows, cols);
+  else if (t == 128) grad_tile_kernel<TX, TW, 128, 128, 2, 2, false><<<grid, 256, 0, st>>>(a, l, rows, cols);
+  else if (pieces) grad_tile_kernel<TX, TW, 64, 64, 2, 2, true><<<grid, 256, 0, st>>>(a, l, rows, cols);
+  else grad_tile_kernel<TX, TW, 64, 64, 2, 2, false><<<grid, 256, 0, st>>>(a, l, rows, cols);
+  return t;
 }
 
 template <uint32_t TO>
@@ -592,7 +601,7 @@ uint64_t loss_grad_bytes(uint64_t tokens, uint64_t classes, uint64_t inputs) {
   if (!tokens) return 0;
   const uint64_t piece = piece_of(tokens, classes), t = padded(tokens), c = padded(piece), d = (inputs + 7) / 8 * 8;
   const uint64_t px = partial_bytes(tokens, inputs, c), pw = partial_bytes(piece, inputs, t);
-  return whole(16 * t) + 2 * whole(4 * t) + whole(4) + whole(4 * classes) + whole(2 * t * d) + whole(2 * c * d) + 2 * whole(2 * t * c) + whole(4 * t * c) +
+  return whole(16 * t) + 2 * whole(4 * t) + whole(4) + whole(2 * t * d) + whole(2 * c * d) + 4 * whole(2 * t * c) + whole((t + 63) / 64 * c) +
          (piece < classes ? whole(4 * tokens * inputs) : 0) + (px > pw ? px : pw);
 }
 
@@ -613,15 +622,13 @@ int launch_loss_grad(const LossGradArgs& a, uint32_t dx_type, uint32_t dw_type, 
   g.scale = arena.take<float>(t);
   g.most = arena.take<float>(t);
   g.most_w = arena.take<uint32_t>(1);
-  g.most_v = arena.take<uint32_t>(a.classes);
   g.x = arena.take<_Float16>(t * d);
   g.w = arena.take<_Float16>(c * d);
-  g.gx[0] = arena.take<_Float16>(t * c);
-  g.gx[1] = arena.take<_Float16>(t * c);
-  g.gw = arena.take<float>(t * c);
+  for (_Float16** p : {&g.gx[0], &g.gx[1], &g.gw[0], &g.gw[1]}) *p = arena.take<_Float16>(t * c);
+  g.unit = arena.take<uint8_t>((t + 63) / 64 * c);
   g.sum = parts > 1 ? arena.take<float>(static_cast<uint64_t>(a.tokens) * a.inputs) : nullptr;
   g.partial = arena.take<float>(0);
-  const bool two = a.dx.p && dx_type == kF32;
+  const bool two_x = a.dx.p && dx_type == kF32, two_w = a.dw.p && dw_type == kF32;
   for (uint32_t p = 0; p < parts; ++p) {
     const uint32_t first = p * piece, n = a.classes - first < piece ? a.classes - first : piece;
     const uint32_t n_padded = static_cast<uint32_t>(padded(n)), t_padded = static_cast<uint32_t>(t);
@@ -631,29 +638,28 @@ int launch_loss_grad(const LossGradArgs& a, uint32_t dx_type, uint32_t dw_type, 
     const Convert cw{w, g.w, n, a.inputs, d, static_cast<uint64_t>(n_padded) * (d / 8)};
     const uint64_t groups_w = (cw.vectors + 256 * kConvert - 1) / (256 * kConvert);
     if (p == 0) {
-      Prepare q{a, g, Convert{a.x, g.x, a.tokens, a.inputs, d, t * (d / 8)}, cw, t_padded, tiles_of(t_padded, 256), tiles_of(a.classes, 1024), 0};
+      Prepare q{a, g, Convert{a.x, g.x, a.tokens, a.inputs, d, t * (d / 8)}, cw, t_padded, tiles_of(t_padded, 256), 0};
       q.groups_x = (q.x.vectors + 256 * kConvert - 1) / (256 * kConvert);
-      prepare_kernel<<<in_layers(1 + q.groups_t + q.groups_v + q.groups_x + groups_w), 256, 0, st>>>(q);
+      prepare_kernel<<<in_layers(1 + q.groups_t + q.groups_x + groups_w), 256, 0, st>>>(q);
     } else {
       convert_kernel<<<in_layers(groups_w), 256, 0, st>>>(cw);
     }
     MatmulArgs m{a.x, w, Mat{}, a.tokens, n, a.inputs};
     m.a.s = g.scale;
     const LogitGrads l{g, first, t_padded, n_padded};
-    if (two) run_grads<2>(m, l, n_cu, st);
-    else run_grads<1>(m, l, n_cu, st);
+    const auto grads = two_x ? (two_w ? run_grads<2, 2> : run_grads<2, 1>) : (two_w ? run_grads<1, 2> : run_grads<1, 1>);
+    const uint32_t unit_rows = grads(m, l, n_cu, st);
     ProductArgs pa{};
-    pa.gx[0] = g.gx[0];
-    pa.gx[1] = g.gx[1];
-    pa.gw = g.gw;
     pa.g_stride = n_padded;
     pa.nj = a.inputs;
     pa.nj_padded = d;
     pa.partial = g.partial;
     if (a.dx.p) {
+      pa.g[0] = g.gx[0];
+      pa.g[1] = g.gx[1];
       pa.q = g.w;
-      pa.most = reinterpret_cast<const uint32_t*>(g.most);
-      pa.times = g.most_w;
+      pa.most = g.most;
+      pa.most_w = g.most_w;
       pa.out = a.dx;
       pa.sum = g.sum;
       pa.add = p > 0;
@@ -665,9 +671,11 @@ int launch_loss_grad(const LossGradArgs& a, uint32_t dx_type, uint32_t dw_type, 
       else run_product<false, kBF16>(pa, st);
     }
     if (a.dw.p) {
+      pa.g[0] = g.gw[0];
+      pa.g[1] = g.gw[1];
       pa.q = g.x;
-      pa.most = g.most_v + first;
-      pa.times = nullptr;
+      pa.unit = g.unit;
+      pa.unit_rows = unit_rows;
       pa.out = a.dw;
       pa.out.p = static_cast<char*>(a.dw.p) + first * a.dw.stride * (dw_type == kF32 ? 4 : 2);
       pa.sum = nullptr;

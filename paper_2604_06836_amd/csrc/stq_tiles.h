@@ -81,13 +81,9 @@ __device__ __forceinline__ void lanes_meet() {
 // A wave's result, FI x FJ fragments of 32 x 32 from row0, col0 on, into an output of rows x cols, by way of 32 rows of LDS of its own
 // (`box`, 4096 FJ bytes for fp32), so that whole pieces of rows are stored, neighbouring ones together.  value(i, j, p, e): column
 // 8 p + 4 (lane / 32) + e of row lane % 32 of fragment i, j.  Pieces lie at the places that their number and the row's give by
-// exclusive or.  seen(v): every piece on its way, those beyond the output among them; a lane's have its number modulo a row's pieces.
-struct Unseen {
-  __device__ __forceinline__ void operator()(const Piece&) const {}
-};
-template <uint32_t TO, uint32_t FI, uint32_t FJ, class F, class SEEN = Unseen>
-__device__ __forceinline__ void store_tile(const Mat& out, uint32_t row0, uint32_t col0, uint32_t rows, uint32_t cols, char* box, uint32_t lane, F value,
-                                           SEEN seen = SEEN{}) {
+// exclusive or.
+template <uint32_t TO, uint32_t FI, uint32_t FJ, class F>
+__device__ __forceinline__ void store_tile(const Mat& out, uint32_t row0, uint32_t col0, uint32_t rows, uint32_t cols, char* box, uint32_t lane, F value) {
   constexpr uint32_t kSize = TO == kF32 ? 4 : 2, kRow = FJ * 32 * kSize, kPieces = kRow / 16, kShift = kRow == 256 ? 0 : (kRow == 128 ? 1 : 2);
   const auto place = [&](uint32_t row, uint32_t piece) { return row * kRow + ((piece ^ (row >> kShift)) & (kPieces - 1)) * 16; };
 #pragma unroll
@@ -108,7 +104,6 @@ __device__ __forceinline__ void store_tile(const Mat& out, uint32_t row0, uint32
       const uint32_t row = h * (64 / kPieces) + lane / kPieces, piece = lane % kPieces;
       Piece v;
       __builtin_memcpy(&v, box + place(row, piece), 16);
-      seen(v);
       const uint32_t r = row0 + i * 32 + row, c = col0 + piece * (16 / kSize);
       if (r < rows && c < cols) store_piece<TO>(out, r, c, cols, v);
     }
@@ -157,6 +152,7 @@ struct CodeTile {
   const float* sn;
   char* box;                // of the wave, for store_tile
   char* room;               // of the workgroup: all boxes of the first half of its waves
+  char* spare;              // of the workgroup: 64 bytes a row and more beside the boxes
 };
 template <int TM, int TN, int WM, int WN, bool PIECES, class END>
 __device__ __forceinline__ void code_tile(const MatmulArgs& a, uint32_t tiles_m, uint32_t tiles_n, END ending) {
@@ -286,7 +282,7 @@ __device__ __forceinline__ void code_tile(const MatmulArgs& a, uint32_t tiles_m,
   constexpr uint32_t kBox = 32 * FN * 32 * 4, kHalf = WM * WN / 2;
   static_assert(kHalf * kBox <= TM * kStepK && kHalf * kBox <= TN * kStepK, "a box for each wave");
   char* const box = wave < kHalf ? reinterpret_cast<char*>(a0) + wave * kBox : reinterpret_cast<char*>(b0) + (wave - kHalf) * kBox;
-  ending(acc, CodeTile{m0, n0, wm, wn, lane, wave, sm, sn, box, reinterpret_cast<char*>(a0)});
+  ending(acc, CodeTile{m0, n0, wm, wn, lane, wave, sm, sn, box, reinterpret_cast<char*>(a0), reinterpret_cast<char*>(sm + TM)});
 #endif
 }
 
