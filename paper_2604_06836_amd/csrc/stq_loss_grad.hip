@@ -180,38 +180,47 @@ __global__ __launch_bounds__(WM * WN * 64) void grad_tile_kernel(const MatmulArg
         for (uint32_t c = 0; c < 16; ++c) acc[i][j][c] = static_cast<int>(f2u(v[j * 16 + c]));
       __builtin_amdgcn_sched_barrier(0);  // (one row's at a time, for the registers)
     }
-    // the largest |g * scale| of the tile's columns, by way of LDS, and the powers of two that follow
-    uint32_t* const held = reinterpret_cast<uint32_t*>(t.spare);  // [WM][TN]
-    float* const powers = reinterpret_cast<float*>(held + WM * TN);
-#pragma unroll
-    for (uint32_t c = 0; c < FN * 16; ++c) {
-      uint32_t m = 0;
-#pragma unroll
-      for (uint32_t i = 0; i < FM; ++i) m = max(m, f2u(u2f(static_cast<uint32_t>(acc[i][c / 16][c % 16])) * scale[i]) & 0x7FFFFFFFu);
-      m = row_max(m);
-      m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16)));
-      if ((t.lane & 31) == c) held[t.wave / WN * TN + t.wn + c / 16 * 32 + c % 16 / 4 * 8 + half * 4 + c % 4] = m;
-    }
-    __syncthreads();
-    for (uint32_t c = threadIdx.x; c < TN; c += WM * WN * 64) {
-      uint32_t m = held[c];
-#pragma unroll
-      for (uint32_t w = 1; w < WM; ++w) m = max(m, held[w * TN + c]);
-      const uint32_t e = factor_exponent(m);
-      powers[c] = power(e);
-      if (t.n0 + c < l.n_padded) l.g.unit[static_cast<uint64_t>(t.m0 / TM) * l.n_padded + t.n0 + c] = static_cast<uint8_t>(e);
-    }
-    __syncthreads();
     const auto g = [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return u2f(static_cast<uint32_t>(acc[i][j][p * 4 + e])); };
-    const float* const pn = powers + t.wn + 4 * half;
 #pragma unroll
     for (int k = 0; k < TX; ++k)
       store_tile<kF16, FM, FN>(Mat{l.g.gx[k], nullptr, l.n_padded, 0, 0}, t.m0 + t.wm, t.n0 + t.wn, l.tokens_padded, l.n_padded, t.box, t.lane,
                                [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return term<TX>(g(i, j, p, e) * sn[j * 32 + p * 8 + e] * times[i], k); });
+    // g * scale, the largest of each of the tile's columns (by way of LDS; a NaN stays one with any power of two) and the powers of two that follow
+    float* const held = reinterpret_cast<float*>(t.spare);  // [2 WM][TN]: of sixteen lanes each
+    float* const powers = held + 2 * WM * TN;
+#pragma unroll
+    for (uint32_t j = 0; j < FN * 2; ++j) {
+      float mine = 0.0f;
+#pragma unroll
+      for (uint32_t c = 0; c < 8; ++c) {
+        const uint32_t at = j % 2 * 8 + c;
+        float m = 0.0f;
+#pragma unroll
+        for (uint32_t i = 0; i < FM; ++i) {
+          const float v = u2f(static_cast<uint32_t>(acc[i][j / 2][at])) * scale[i];
+          acc[i][j / 2][at] = static_cast<int>(f2u(v));
+          m = fmaxf(m, fabsf(v));
+        }
+        m = u2f(row_max(f2u(m)));
+        mine = (t.lane & 7) == c ? m : mine;
+      }
+      if ((t.lane & 8) == 0) held[(t.wave / WN * 2 + (t.lane >> 4 & 1)) * TN + t.wn + j * 16 + (t.lane & 4) * 2 + half * 4 + (t.lane & 3)] = mine;
+    }
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < TN; c += WM * WN * 64) {
+      float m = held[c];
+#pragma unroll
+      for (uint32_t w = 1; w < 2 * WM; ++w) m = fmaxf(m, held[w * TN + c]);
+      const uint32_t e = factor_exponent(f2u(m));
+      powers[c] = power(e);
+      if (t.n0 + c < l.n_padded) l.g.unit[static_cast<uint64_t>(t.m0 / TM) * l.n_padded + t.n0 + c] = static_cast<uint8_t>(e);
+    }
+    __syncthreads();
+    const float* const pn = powers + t.wn + 4 * half;
 #pragma unroll
     for (int k = 0; k < TW; ++k)
       store_tile<kF16, FM, FN>(Mat{l.g.gw[k], nullptr, l.n_padded, 0, 0}, t.m0 + t.wm, t.n0 + t.wn, l.tokens_padded, l.n_padded, t.box, t.lane,
-                               [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return term<TW>(g(i, j, p, e) * scale[i] * pn[j * 32 + p * 8 + e], k); });
+                               [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return term<TW>(g(i, j, p, e) * pn[j * 32 + p * 8 + e], k); });
     if constexpr (TM < 128) {  // rows and columns of zeros that no tile covers
       const uint32_t row_end = t.m0 + TM, col_end = t.n0 + TN;
       const bool last_row = row_end >= a.m, last_col = col_end >= a.n;
