@@ -288,6 +288,10 @@ struct ProductArgs {
   uint32_t splits, each;  // parts of c, and their length (a multiple of two steps)
   float* partial;         // [splits][ni][nj] where there are several
 };
+struct Products {  // those with respect to x, of which there are groups_x workgroups, and then those with respect to w
+  ProductArgs x, w;
+  uint64_t groups_x, groups;
+};
 
 // A [c][x] tile in LDS: rows of X elements, of which pieces of eight lie at the places that their number and the row's give by exclusive or, so
 // that the four rows of a transposed read meet every bank once.
@@ -314,10 +318,10 @@ __device__ __forceinline__ v8h transposed(const _Float16* tile, uint32_t c0, uin
 
 // A wave's sums, by way of LDS (`box`, 32 rows in fp32), to where they go, with what is added to them.
 template <uint32_t TO, uint32_t FI, uint32_t FJ, class F>
-__device__ __forceinline__ void store_sums(const ProductArgs& a, uint32_t row0, uint32_t col0, char* box, uint32_t lane, F value) {
+__device__ __forceinline__ void store_sums(const ProductArgs& a, uint32_t part, uint32_t row0, uint32_t col0, char* box, uint32_t lane, F value) {
   constexpr uint32_t kRow = FJ * 128, kPieces = kRow / 16, kShift = kRow == 256 ? 0 : 1;
   const auto place = [&](uint32_t row, uint32_t piece) { return row * kRow + ((piece ^ (row >> kShift)) & (kPieces - 1)) * 16; };
-  float* const to = a.splits > 1 ? a.partial + static_cast<uint64_t>(blockIdx.y) * a.ni * a.nj : a.sum;
+  float* const to = a.splits > 1 ? a.partial + static_cast<uint64_t>(part) * a.ni * a.nj : a.sum;
   const bool last = a.last && a.splits == 1, add = a.add && a.splits == 1;
 #pragma unroll
   for (uint32_t i = 0; i < FI; ++i) {
@@ -374,21 +378,21 @@ __device__ __forceinline__ void store_sums(const ProductArgs& a, uint32_t row0, 
   }
 }
 
-// A workgroup has TI x TJ of the result, its WI x WJ waves a part each, and takes STEP of c at a time, out of one of two LDS buffers while the
-// other is filled by loads straight into it.
-template <bool WEIGHT, uint32_t TO, int TERMS, int TI, int TJ, int WI, int WJ, int STEP>
-__global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const ProductArgs a) {
+// A workgroup has T x T of a result, its WI x WJ waves a part each, and takes STEP of c at a time, out of one of two LDS buffers (a0, b0 and
+// a1, b1) while the other is filled by loads straight into it.
+template <bool WEIGHT, uint32_t TO, int T, int WI, int WJ>
+__device__ __forceinline__ void product(const ProductArgs& a, uint32_t group, _Float16* a0, _Float16* b0, _Float16* a1, _Float16* b1) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host's compiler has no buffer descriptors)
+  constexpr int TERMS = TO == kF32 ? 2 : 1, TI = T, TJ = T, STEP = 64 / TERMS;
   constexpr uint32_t kThreads = WI * WJ * 64, FI = TI / WI / 32, FJ = TJ / WJ / 32;
   constexpr uint32_t kSizeA = TI * STEP, kSizeB = STEP * TJ;
   constexpr uint32_t LA = kSizeA / 8 / kThreads, LB = kSizeB / 8 / kThreads;  // pieces of eight of a thread
   static_assert(LA * kThreads * 8 == kSizeA && LB * kThreads * 8 == kSizeB, "whole loads");
-  __shared__ __align__(1024) _Float16 a0[TERMS][kSizeA], b0[kSizeB], a1[TERMS][kSizeA], b1[kSizeB];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (group_number() >= a.tiles_i * a.tiles_j) return;
-  const TileAt at = tile_at(group_number(), a.tiles_i, a.tiles_j);
+  const uint32_t tiles = a.tiles_i * a.tiles_j, part = group / tiles;
+  const TileAt at = tile_at(group - part * tiles, a.tiles_i, a.tiles_j);
   const uint32_t i0 = at.row * TI, j0 = at.col * TJ;
-  const uint32_t first = blockIdx.y * a.each, end = min(a.nc, first + a.each);
+  const uint32_t first = part * a.each, end = min(a.nc, first + a.each);
   // load i of a wave fills 64 pieces of LDS, in lane order, from (i * waves + wave) * 64 on
   uint32_t ob[LB], oa[LA];
 #pragma unroll
@@ -409,14 +413,14 @@ __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const ProductArgs
     for (uint32_t i = 0; i < LB; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (STQ_LDS void*)(to + (i * (kThreads / 64) + wave) * 512), 16, ob[i], 0, 0, 0);
   };
-  const auto load_a = [&](uint32_t c, _Float16 (*to)[kSizeA]) __attribute__((always_inline)) {
+  const auto load_a = [&](uint32_t c, _Float16* to) __attribute__((always_inline)) {
     if (c >= end) return;
 #pragma unroll
     for (int k = 0; k < TERMS; ++k) {
       const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(a.g[k]) + (WEIGHT ? c * a.g_stride : i0 * a.g_stride + c), 0, 0x7FFFFFFF, 0x00020000);
 #pragma unroll
       for (uint32_t i = 0; i < LA; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (STQ_LDS void*)(to[k] + (i * (kThreads / 64) + wave) * 512), 16, oa[i], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (STQ_LDS void*)(to + k * kSizeA + (i * (kThreads / 64) + wave) * 512), 16, oa[i], 0, 0, 0);
     }
   };
   v16f acc[FI][FJ] = {};
@@ -426,19 +430,19 @@ __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const ProductArgs
   constexpr uint32_t kUnits = STEP / 16 * TERMS * FI, kAhead = FI < 4 || TERMS == 2 ? 2 : 4;
   static_assert(kUnits > kAhead, "units in front of the meeting");
   v8h fa[kAhead], fb[2][FJ];
-  const auto read = [&](uint32_t u, const _Float16 (*ta)[kSizeA], const _Float16* tb) __attribute__((always_inline)) {
+  const auto read = [&](uint32_t u, const _Float16* ta, const _Float16* tb) __attribute__((always_inline)) {
     const uint32_t s = u / (TERMS * FI), k = u / FI % TERMS, i = u % FI;
     if constexpr (WEIGHT) {
-      fa[u % kAhead] = transposed<TI>(ta[k], s * 16, wi + i * 32, lane);
+      fa[u % kAhead] = transposed<TI>(ta + k * kSizeA, s * 16, wi + i * 32, lane);
     } else {
       const uint32_t row = wi + i * 32 + (lane & 31);
-      __builtin_memcpy(&fa[u % kAhead], &ta[k][row * STEP + ((s * 2 + (lane >> 5)) ^ swizzle_c<STEP>(row)) * 8], 16);
+      __builtin_memcpy(&fa[u % kAhead], &ta[k * kSizeA + row * STEP + ((s * 2 + (lane >> 5)) ^ swizzle_c<STEP>(row)) * 8], 16);
     }
     if (u % (TERMS * FI)) return;
 #pragma unroll
     for (uint32_t j = 0; j < FJ; ++j) fb[s & 1][j] = transposed<TJ>(tb, s * 16, wj + j * 32, lane);
   };
-  const auto work = [&](uint32_t c, _Float16 (*ta)[kSizeA], _Float16* tb, _Float16 (*na)[kSizeA], _Float16* nb) __attribute__((always_inline)) {
+  const auto work = [&](uint32_t c, _Float16* ta, _Float16* tb, _Float16* na, _Float16* nb) __attribute__((always_inline)) {
 #pragma unroll
     for (uint32_t u = 0; u < kUnits; ++u) {
       if (u == kUnits - kAhead) {
@@ -503,22 +507,52 @@ __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const ProductArgs
   }
   __syncthreads();
   constexpr uint32_t kBox = 32 * FJ * 32 * 4, kHalf = WI * WJ / 2;
+  static_assert(kHalf * kBox <= T * 128, "boxes of the first half of the waves in a0, of the second in a1");
   char* const box = wave < kHalf ? reinterpret_cast<char*>(a0) + wave * kBox : reinterpret_cast<char*>(a1) + (wave - kHalf) * kBox;
-  static_assert(kHalf * kBox <= sizeof(a0), "boxes of the first half of the waves in a0, of the second in a1");
-  store_sums<TO, FI, FJ>(a, i0 + wi, j0 + wj, box, lane, [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return acc[i][j][p * 4 + e] * undo[i]; });
+  store_sums<TO, FI, FJ>(a, part, i0 + wi, j0 + wj, box, lane, [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return acc[i][j][p * 4 + e] * undo[i]; });
 #endif
 }
+// Both products of a piece in one launch, so that the last tiles of one and the first of the other share the card.
+template <uint32_t TX, uint32_t TW, int T, int WI, int WJ>
+__global__ __launch_bounds__(WI * WJ * 64) void products_kernel(const Products p) {
+  __shared__ __align__(1024) _Float16 a0[T * 64], b0[T * 64], a1[T * 64], b1[T * 64];
+  const uint32_t group = group_number();
+  if (group < p.groups_x) product<false, TX, T, WI, WJ>(p.x, group, a0, b0, a1, b1);
+  else if (group < p.groups) product<true, TW, T, WI, WJ>(p.w, group - static_cast<uint32_t>(p.groups_x), a0, b0, a1, b1);
+}
 
-// The parts of a sum that was taken in parts, in one order, and what is added to them.
+// The parts of sums that were taken in parts, in one order, and what is added to them: four neighbouring elements to a thread.
 template <uint32_t TO>
-__global__ __launch_bounds__(256) void join_parts_kernel(const ProductArgs a) {
-  const uint64_t size = static_cast<uint64_t>(a.ni) * a.nj;
-  for (uint64_t t = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; t < size; t += static_cast<uint64_t>(gridDim.x) * 256) {
-    float v = a.add ? a.sum[t] : 0.0f;
-    for (uint32_t k = 0; k < a.splits; ++k) v += as_global(a.partial)[k * size + t];
-    using T = typename Elem<TO>::type;
-    if (a.last) as_global(static_cast<T*>(a.out.p))[t / a.nj * a.out.stride + t % a.nj] = static_cast<T>(v);
-    else a.sum[t] = v;
+__device__ __forceinline__ void join_four(const ProductArgs& a, uint64_t t) {
+  const uint32_t per_row = (a.nj + 3) / 4, row = static_cast<uint32_t>(t / per_row), col = static_cast<uint32_t>(t % per_row) * 4;
+  const uint64_t size = static_cast<uint64_t>(a.ni) * a.nj, at = static_cast<uint64_t>(row) * a.nj + col;
+  const uint32_t n = min(4u, a.nj - col);
+  float v[4] = {0, 0, 0, 0};
+  const auto add = [&](const float* p) {
+    if (n == 4) {
+      const v4i w = load_fragment(reinterpret_cast<const int8_t*>(p));
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e) v[e] += u2f(static_cast<uint32_t>(w[e]));
+    } else {
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e)
+        if (e < n) v[e] += as_global(p)[e];
+    }
+  };
+  if (a.add) add(a.sum + at);
+  for (uint32_t k = 0; k < a.splits; ++k) add(a.partial + k * size + at);
+  if (a.last) store4<TO>(a.out, row, col, a.nj, v);
+  else if (n == 4) store_floats(a.sum + at, v);
+  else
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e)
+      if (e < n) as_global(a.sum)[at + e] = v[e];
+}
+template <uint32_t TX, uint32_t TW>
+__global__ __launch_bounds__(256) void join_parts_kernel(const Products p) {  // groups_x, groups: of this launch, of elements
+  for (uint64_t t = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; t < p.groups; t += static_cast<uint64_t>(gridDim.x) * 256) {
+    if (t < p.groups_x) join_four<TX>(p.x, t);
+    else join_four<TW>(p.w, t - p.groups_x);
   }
 }
 
@@ -527,52 +561,64 @@ constexpr uint32_t kCus = 256;  // for sizes that must not depend on the device
 
 uint64_t padded(uint64_t n) { return (n + 127) / 128 * 128; }  // to two steps of a product
 
-// Classes of a piece: of as many logits as kPieceLogits, and of one size.
-constexpr uint64_t kPieceLogits = 1ull << 26, kLeastPiece = 1024, kMostPiece = 1ull << 20;
-uint64_t piece_of(uint64_t tokens, uint64_t classes) {
-  uint64_t most = kPieceLogits / tokens;
+// Classes of a piece, of one size: of as many logits as have their factors in 1 GiB, twice 2 bytes each, or 4 for results in fp32.  (8192 x 32000 x
+// 4096 in 64 MiB of logits' factors 4758 us, in 256 MiB 4586, in 512 MiB 4475, in 1 GiB 4552.)
+constexpr uint64_t kPieceLogits = 1ull << 28, kLeastPiece = 2048, kMostPiece = 1ull << 20;
+uint64_t piece_of(uint64_t tokens, uint64_t classes, bool fp32) {
+  uint64_t most = (fp32 ? kPieceLogits / 2 : kPieceLogits) / tokens;
   most = most < kLeastPiece ? kLeastPiece : (most > kMostPiece ? kMostPiece : most);
   const uint64_t pieces = (classes + most - 1) / most, each = ((classes + pieces - 1) / pieces + 255) / 256 * 256;
   return each < classes ? each : classes;
 }
 
-// Parts of the sum of a product whose result has fewer tiles of 64 x 64 than the card's CUs.
-uint32_t splits_of(uint64_t ni, uint64_t nj, uint64_t nc) {
-  const uint64_t tiles = ((ni + 63) / 64) * ((nj + 63) / 64), most = nc / 512;
-  if (tiles >= kCus || most < 2) return 1;
-  const uint64_t s = 2 * kCus / tiles;
-  return static_cast<uint32_t>(s < most ? s : most);
-}
-uint64_t partial_bytes(uint64_t ni, uint64_t nj, uint64_t nc) {
-  const uint64_t s = splits_of(ni, nj, nc);
-  return s > 1 ? whole(4 * s * ni * nj) : 0;
-}
-
-template <bool WEIGHT, uint32_t TO>
-void run_product(ProductArgs a, hipStream_t st) {
-  constexpr int kTerms = TO == kF32 ? 2 : 1;
-  const auto grid = [&](uint32_t t) {
-    a.tiles_i = tiles_of(a.ni, t);
-    a.tiles_j = tiles_of(a.nj, t);
-    return in_layers(static_cast<uint64_t>(a.tiles_i) * a.tiles_j, a.splits);
+// How the products of a piece are taken: tiles of t x t, and each sum in parts, so that no workgroup has more than half of what a CU has to do
+// (sums of 512 at least).
+struct Plan {
+  uint32_t t;
+  uint32_t splits_x, each_x, splits_w, each_w;
+};
+uint64_t tiles(uint64_t a, uint64_t b, uint64_t t) { return ((a + t - 1) / t) * ((b + t - 1) / t); }
+Plan plan_of(uint64_t tokens, uint64_t n, uint64_t inputs) {
+  const uint64_t kx = padded(n), kw = padded(tokens);
+  const auto work = [&](uint64_t t) { return tiles(tokens, inputs, t) * kx + tiles(n, inputs, t) * kw; };
+  Plan p;
+  // As large as leaves every CU a sum of 512, and as does not work for tiles that are mostly beyond the results.
+  p.t = work(256) >= 512 * kCus && work(256) * 3 <= work(128) ? 256 : (work(128) >= 512 * kCus && work(128) * 2 <= work(64) ? 128 : 64);
+  const uint64_t at_once = p.t == 256 ? kCus : (p.t == 128 ? 2 * kCus : 4 * kCus), half = work(p.t) / at_once / 2;
+  const auto split = [&](uint64_t k, uint32_t* splits, uint32_t* each) {
+    const uint64_t s = (k + (half > 512 ? half : 512) - 1) / (half > 512 ? half : 512);
+    *each = static_cast<uint32_t>(padded((k + s - 1) / s));
+    *splits = static_cast<uint32_t>((k + *each - 1) / *each);
   };
-  const auto count = [&](uint32_t t) { return static_cast<uint64_t>(tiles_of(a.ni, t)) * tiles_of(a.nj, t); };
-  a.splits = splits_of(a.ni, a.nj, a.nc);
-  a.each = tiles_of(a.nc, a.splits * 128) * 128;
-  a.splits = tiles_of(a.nc, a.each);
-  if (a.splits == 1 && count(256) > kCus / 2) {
-    const dim3 d = grid(256);
-    product_kernel<WEIGHT, TO, kTerms, 256, 256, 2, 4, 64 / kTerms><<<d, 512, 0, st>>>(a);
-  } else if (a.splits == 1 && count(128) * 2 > kCus) {
-    const dim3 d = grid(128);
-    product_kernel<WEIGHT, TO, kTerms, 128, 128, 2, 2, 64 / kTerms><<<d, 256, 0, st>>>(a);
-  } else {
-    const dim3 d = grid(64);
-    product_kernel<WEIGHT, TO, kTerms, 64, 64, 2, 2, 64><<<d, 256, 0, st>>>(a);
-    if (a.splits > 1) {
-      const uint64_t groups = (static_cast<uint64_t>(a.ni) * a.nj + 255) / 256;
-      join_parts_kernel<TO><<<static_cast<uint32_t>(groups < 4096 ? groups : 4096), 256, 0, st>>>(a);
-    }
+  split(kx, &p.splits_x, &p.each_x);
+  split(kw, &p.splits_w, &p.each_w);
+  return p;
+}
+uint64_t partial_x(const Plan& p, uint64_t tokens, uint64_t inputs) { return p.splits_x > 1 ? whole(4 * p.splits_x * tokens * inputs) : 0; }
+uint64_t partial_w(const Plan& p, uint64_t n, uint64_t inputs) { return p.splits_w > 1 ? whole(4 * p.splits_w * n * inputs) : 0; }
+
+template <uint32_t TX, uint32_t TW>
+void run_products(Products p, const Plan& plan, hipStream_t st) {
+  const auto groups = [&](ProductArgs& a, uint32_t splits, uint32_t each) {
+    if (!a.q) return static_cast<uint64_t>(0);
+    a.tiles_i = tiles_of(a.ni, plan.t);
+    a.tiles_j = tiles_of(a.nj, plan.t);
+    a.splits = splits;
+    a.each = each;
+    return static_cast<uint64_t>(a.tiles_i) * a.tiles_j * splits;
+  };
+  p.groups_x = groups(p.x, plan.splits_x, plan.each_x);
+  p.groups = p.groups_x + groups(p.w, plan.splits_w, plan.each_w);
+  const dim3 grid = in_layers(p.groups);
+  if (plan.t == 256) products_kernel<TX, TW, 256, 2, 4><<<grid, 512, 0, st>>>(p);
+  else if (plan.t == 128) products_kernel<TX, TW, 128, 2, 2><<<grid, 256, 0, st>>>(p);
+  else products_kernel<TX, TW, 64, 2, 2><<<grid, 256, 0, st>>>(p);
+  const auto fours = [](const ProductArgs& a) { return a.q && a.splits > 1 ? static_cast<uint64_t>(a.ni) * ((a.nj + 3) / 4) : 0; };
+  p.groups_x = fours(p.x);
+  p.groups = p.groups_x + fours(p.w);
+  if (p.groups) {
+    const uint64_t g = (p.groups + 255) / 256;
+    join_parts_kernel<TX, TW><<<static_cast<uint32_t>(g < 4096 ? g : 4096), 256, 0, st>>>(p);
   }
 }
 
@@ -606,12 +652,33 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(const Mat out, uint64_t 
 
 }  // namespace
 
+namespace {
+struct Need {  // of a workspace
+  uint64_t piece, t, c, d, partial, bytes;
+};
+Need need_of(uint64_t tokens, uint64_t classes, uint64_t inputs, bool fp32) {
+  Need n;
+  n.piece = piece_of(tokens, classes, fp32);
+  n.t = padded(tokens);
+  n.c = padded(n.piece);
+  n.d = (inputs + 7) / 8 * 8;
+  n.partial = 0;
+  for (const uint64_t k : {n.piece, classes % n.piece ? classes % n.piece : n.piece}) {  // (the last piece may be taken in more parts)
+    const Plan p = plan_of(tokens, k, inputs);
+    const uint64_t b = partial_x(p, tokens, inputs) + partial_w(p, k, inputs);
+    n.partial = b > n.partial ? b : n.partial;
+  }
+  const uint64_t t = n.t, c = n.c;
+  n.bytes = whole(16 * t) + 2 * whole(4 * t) + whole(4) + whole(2 * t * n.d) + whole(2 * c * n.d) + (fp32 ? 4 : 2) * whole(2 * t * c) + whole((t + 63) / 64 * c) +
+            (n.piece < classes ? whole(4 * tokens * inputs) : 0) + n.partial;
+  return n;
+}
+}  // namespace
+
 uint64_t loss_grad_bytes(uint64_t tokens, uint64_t classes, uint64_t inputs) {
   if (!tokens) return 0;
-  const uint64_t piece = piece_of(tokens, classes), t = padded(tokens), c = padded(piece), d = (inputs + 7) / 8 * 8;
-  const uint64_t px = partial_bytes(tokens, inputs, c), pw = partial_bytes(piece, inputs, t);
-  return whole(16 * t) + 2 * whole(4 * t) + whole(4) + whole(2 * t * d) + whole(2 * c * d) + 4 * whole(2 * t * c) + whole((t + 63) / 64 * c) +
-         (piece < classes ? whole(4 * tokens * inputs) : 0) + (px > pw ? px : pw);
+  const uint64_t one = need_of(tokens, classes, inputs, false).bytes, two = need_of(tokens, classes, inputs, true).bytes;
+  return one > two ? one : two;
 }
 
 int launch_loss_grad(const LossGradArgs& a, uint32_t dx_type, uint32_t dw_type, void* workspace, uint32_t n_cu, void* stream) {
@@ -622,9 +689,10 @@ int launch_loss_grad(const LossGradArgs& a, uint32_t dx_type, uint32_t dw_type, 
     zero<<<static_cast<uint32_t>(groups < 4096 ? groups : 4096), 256, 0, st>>>(a.dw, a.classes, a.inputs);
     return hipGetLastError();
   }
-  const uint32_t piece = static_cast<uint32_t>(piece_of(a.tokens, a.classes)), parts = tiles_of(a.classes, piece);
-  const uint64_t t = padded(a.tokens), c = padded(piece);
-  const uint32_t d = (a.inputs + 7) / 8 * 8;
+  const bool two_x = a.dx.p && dx_type == kF32, two_w = a.dw.p && dw_type == kF32;
+  const Need need = need_of(a.tokens, a.classes, a.inputs, two_x || two_w);
+  const uint32_t piece = static_cast<uint32_t>(need.piece), parts = tiles_of(a.classes, piece), d = static_cast<uint32_t>(need.d);
+  const uint64_t t = need.t, c = need.c;
   Arena arena{static_cast<char*>(workspace)};
   GradWork g;
   g.token = arena.take<Token>(t);
@@ -633,11 +701,13 @@ int launch_loss_grad(const LossGradArgs& a, uint32_t dx_type, uint32_t dw_type, 
   g.most_w = arena.take<uint32_t>(1);
   g.x = arena.take<_Float16>(t * d);
   g.w = arena.take<_Float16>(c * d);
-  for (_Float16** p : {&g.gx[0], &g.gx[1], &g.gw[0], &g.gw[1]}) *p = arena.take<_Float16>(t * c);
+  for (int k = 0; k < (two_x || two_w ? 2 : 1); ++k) {
+    g.gx[k] = arena.take<_Float16>(t * c);
+    g.gw[k] = arena.take<_Float16>(t * c);
+  }
   g.unit = arena.take<uint8_t>((t + 63) / 64 * c);
   g.sum = parts > 1 ? arena.take<float>(static_cast<uint64_t>(a.tokens) * a.inputs) : nullptr;
   g.partial = arena.take<float>(0);
-  const bool two_x = a.dx.p && dx_type == kF32, two_w = a.dw.p && dw_type == kF32;
   for (uint32_t p = 0; p < parts; ++p) {
     const uint32_t first = p * piece, n = a.classes - first < piece ? a.classes - first : piece;
     const uint32_t n_padded = static_cast<uint32_t>(padded(n)), t_padded = static_cast<uint32_t>(t);
@@ -658,44 +728,46 @@ int launch_loss_grad(const LossGradArgs& a, uint32_t dx_type, uint32_t dw_type, 
     const LogitGrads l{g, first, t_padded, n_padded};
     const auto grads = two_x ? (two_w ? run_grads<2, 2> : run_grads<2, 1>) : (two_w ? run_grads<1, 2> : run_grads<1, 1>);
     const uint32_t unit_rows = grads(m, l, n_cu, st);
-    ProductArgs pa{};
-    pa.g_stride = n_padded;
-    pa.nj = a.inputs;
-    pa.nj_padded = d;
-    pa.partial = g.partial;
+    Products both{};
+    const Plan plan = plan_of(a.tokens, n, a.inputs);
+    for (ProductArgs* q : {&both.x, &both.w}) {
+      q->g_stride = n_padded;
+      q->nj = a.inputs;
+      q->nj_padded = d;
+    }
     if (a.dx.p) {
-      pa.g[0] = g.gx[0];
-      pa.g[1] = g.gx[1];
-      pa.q = g.w;
-      pa.most = g.most;
-      pa.most_w = g.most_w;
-      pa.out = a.dx;
-      pa.sum = g.sum;
-      pa.add = p > 0;
-      pa.last = p + 1 == parts;
-      pa.ni = a.tokens;
-      pa.nc = n_padded;
-      pa.ni_padded = t_padded;
-      if (dx_type == kF32) run_product<false, kF32>(pa, st);
-      else run_product<false, kBF16>(pa, st);
+      ProductArgs& q = both.x;
+      q.g[0] = g.gx[0];
+      q.g[1] = g.gx[1];
+      q.q = g.w;
+      q.most = g.most;
+      q.most_w = g.most_w;
+      q.out = a.dx;
+      q.sum = g.sum;
+      q.add = p > 0;
+      q.last = p + 1 == parts;
+      q.ni = a.tokens;
+      q.nc = n_padded;
+      q.ni_padded = t_padded;
+      q.partial = g.partial;
     }
     if (a.dw.p) {
-      pa.g[0] = g.gw[0];
-      pa.g[1] = g.gw[1];
-      pa.q = g.x;
-      pa.unit = g.unit;
-      pa.unit_rows = unit_rows;
-      pa.out = a.dw;
-      pa.out.p = static_cast<char*>(a.dw.p) + first * a.dw.stride * (dw_type == kF32 ? 4 : 2);
-      pa.sum = nullptr;
-      pa.add = false;
-      pa.last = true;
-      pa.ni = n;
-      pa.nc = t_padded;
-      pa.ni_padded = n_padded;
-      if (dw_type == kF32) run_product<true, kF32>(pa, st);
-      else run_product<true, kBF16>(pa, st);
+      ProductArgs& q = both.w;
+      q.g[0] = g.gw[0];
+      q.g[1] = g.gw[1];
+      q.q = g.x;
+      q.unit = g.unit;
+      q.unit_rows = unit_rows;
+      q.out = a.dw;
+      q.out.p = static_cast<char*>(a.dw.p) + first * a.dw.stride * (dw_type == kF32 ? 4 : 2);
+      q.last = true;
+      q.ni = n;
+      q.nc = t_padded;
+      q.ni_padded = n_padded;
+      q.partial = g.partial + partial_x(plan, a.tokens, a.inputs) / 4;
     }
+    const auto products = two_x ? (two_w ? run_products<kF32, kF32> : run_products<kF32, kBF16>) : (two_w ? run_products<kBF16, kF32> : run_products<kBF16, kBF16>);
+    products(both, plan, st);
   }
   return hipGetLastError();
 }
