@@ -27,13 +27,6 @@ __device__ __forceinline__ uint32_t factor_exponent(uint32_t most) {
 }
 [[maybe_unused]] __device__ __forceinline__ float power(uint32_t exponent) { return u2f(exponent << 23); }  // 1 to 254
 
-[[maybe_unused]] __device__ __forceinline__ void store_piece16(_Float16* p, const Piece& v) { __builtin_memcpy(as_global(p), &v, 16); }
-[[maybe_unused]] __device__ __forceinline__ v8h load_half8(const _Float16* p) {  // from LDS
-  v8h r;
-  __builtin_memcpy(&r, p, 16);
-  return r;
-}
-
 // What the tiles of the logits need of a token.
 struct Token {
   float lse2;       // log-sum times log2 e
@@ -46,51 +39,43 @@ struct GradWork {  // parts of the workspace
   float* scale;      // [tokens, padded]: of the codes, or 0 for a token that takes no part
   float* most;       // [tokens, padded]: a bound on |g| of the row
   uint32_t* most_w;  // the largest of the classes' scales (bits)
-  _Float16* x;       // [inputs][tokens, padded]: codes, zeros beyond the tokens
-  _Float16* w;       // [inputs][classes of a piece, padded]
+  _Float16* x;       // [tokens, padded][inputs, padded]: codes, zeros beyond the matrix
+  _Float16* w;       // [classes of a piece, padded][inputs, padded]
   _Float16* gx[2];   // [tokens, padded][classes of a piece, padded]: factors of dx, one or two terms
-  _Float16* gw[2];   // [classes of a piece, padded][tokens, padded]: factors of dw
+  _Float16* gw[2];   // the same: factors of dw
   uint8_t* unit;     // [tiles of tokens][classes of a piece, padded]: exponents of the powers of two that go with gw
   float* sum;        // [tokens][inputs]: of dx, where there are several pieces
   float* partial;    // parts of a product that is taken in several
 };
 
 // ---------------------------------------------------------------------------------------------- preparation
-// Codes as fp16 and transposed, [inputs][rows], with zeros beyond the rows' end up to a multiple of 128: the products' sums run along rows, and what a
-// matrix instruction takes then lies together.  128 rows of 64 columns to a workgroup.
+// Codes as fp16, eight to a thread, into rows of `cols` (a multiple of eight) with zeros beyond the matrix.
+constexpr uint32_t kConvert = 4;  // vectors of a thread
 struct Convert {
   Mat from;
   _Float16* to;
-  uint32_t rows, inputs;
-  uint32_t rows_padded, apart;  // the result's rows, and how far they lie apart
-  uint32_t groups_c;     // of the columns
-  __device__ __forceinline__ uint64_t groups() const { return static_cast<uint64_t>(rows_padded / 128) * groups_c; }
-  __device__ __forceinline__ void operator()(uint64_t group, int8_t* box) const {  // box: 128 x 68
-    const uint32_t r0 = static_cast<uint32_t>(group / groups_c) * 128, c0 = static_cast<uint32_t>(group % groups_c) * 64;
-    const int8_t* const p = static_cast<const int8_t*>(from.p);
+  uint32_t rows, inputs, cols;
+  uint64_t vectors;  // of the padded matrix
+  __device__ __forceinline__ void operator()(uint64_t group) const {
+    const uint32_t per_row = cols / 8;
+    const uint64_t first = group * (256 * kConvert), row0 = first / per_row;
+    const uint32_t in_row = static_cast<uint32_t>(first % per_row) + threadIdx.x;
 #pragma unroll
-    for (uint32_t k = 0; k < 4; ++k) {
-      const uint32_t v = k * 256 + threadIdx.x, row = v / 8, col = v % 8 * 8;
-      Packed<int8_t> q{};
-      if (r0 + row < rows && c0 + col < inputs) q = load_ending(p + (static_cast<uint64_t>(r0) + row) * from.stride, c0 + col, inputs);
-      __builtin_memcpy(box + row * 68 + col, &q.w[0], 4);
-      __builtin_memcpy(box + row * 68 + col + 4, &q.w[1], 4);
-    }
-    __syncthreads();
+    for (uint32_t k = 0; k < kConvert; ++k) {
+      const uint32_t v = in_row + 256 * k, row_in = v / per_row, col = (v - row_in * per_row) * 8;
+      const uint64_t row = row0 + row_in;
+      if (first + threadIdx.x + 256 * k >= vectors) return;
+      v8h h{};
+      if (row < rows) {
+        const Packed<int8_t> q = load_ending(static_cast<const int8_t*>(from.p) + row * from.stride, col, inputs);
 #pragma unroll
-    for (uint32_t k = 0; k < 4; ++k) {
-      const uint32_t v = k * 256 + threadIdx.x, col = v / 16, row = v % 16 * 8;
-      v8h h;
-#pragma unroll
-      for (uint32_t e = 0; e < 8; ++e) h[e] = static_cast<_Float16>(static_cast<float>(box[(row + e) * 68 + col]));
-      if (c0 + col < inputs) __builtin_memcpy(as_global(to) + (static_cast<uint64_t>(c0) + col) * apart + r0 + row, &h, 16);
+        for (uint32_t e = 0; e < 8; ++e) h[e] = static_cast<_Float16>(q.at(e));
+      }
+      __builtin_memcpy(as_global(to) + row * cols + col, &h, 16);
     }
   }
 };
-__global__ __launch_bounds__(256) void convert_kernel(const Convert w) {
-  __shared__ __align__(16) int8_t box[128 * 68];
-  if (group_number() < w.groups()) w(group_number(), box);
-}
+__global__ __launch_bounds__(256) void convert_kernel(const Convert w) { w(group_number()); }
 
 // In one launch what is there before the first piece: the tokens' data, the largest scale of a class, x and the first piece of w in fp16.
 struct Prepare {
@@ -99,9 +84,9 @@ struct Prepare {
   Convert x, w;
   uint32_t tokens_padded;
   uint32_t groups_t;
+  uint64_t groups_x;
 };
 __global__ __launch_bounds__(256) void prepare_kernel(const Prepare p) {
-  __shared__ __align__(16) int8_t box[128 * 68];
   const LossGradArgs& a = p.a;
   uint64_t group = group_number();
   if (group == 0) {
@@ -141,10 +126,10 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Prepare p) {
     p.g.token[token] = t;
     p.g.scale[token] = scale;
     p.g.most[token] = most;
-  } else if ((group -= p.groups_t) < p.x.groups()) {
-    p.x(group, box);
-  } else if ((group -= p.x.groups()) < p.w.groups()) {
-    p.w(group, box);
+  } else if ((group -= p.groups_t) < p.groups_x) {
+    p.x(group);
+  } else if ((group -= p.groups_x) * (256 * kConvert) < p.w.vectors) {
+    p.w(group);
   }
 }
 
@@ -153,43 +138,10 @@ struct LogitGrads {
   GradWork g;
   uint32_t first;                    // class of the piece
   uint32_t tokens_padded, n_padded;  // rows and columns that are written, zeros beyond the matrices
-  uint32_t apart_x, apart_w;         // how far rows of gx and of gw lie apart
 };
 __device__ __forceinline__ float grad_of(float z, const Token& t) { return t.c * __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, -t.lse2)); }
 template <int TERMS>
 __device__ __forceinline__ float term(float x, int k) { return TERMS == 2 && k ? x - static_cast<float>(static_cast<_Float16>(x)) : x; }
-
-// store_tile of fp16, into an output whose rows are the tile's columns (`cols` of them, `apart` elements from one to the next): out of LDS transposed, eight rows of a column to a lane, 32 rows of sixteen columns together.
-template <uint32_t FI, uint32_t FJ, class F>
-__device__ __forceinline__ void store_transposed(_Float16* out, uint32_t apart, uint32_t rows, uint32_t row0, uint32_t col0, uint32_t cols, char* box, uint32_t lane, F value) {
-  constexpr uint32_t kRow = FJ * 64, kPieces = kRow / 16, kShift = kRow == 128 ? 1 : 2;
-  const auto place = [&](uint32_t row, uint32_t piece) { return row * kRow + ((piece ^ (row >> kShift)) & (kPieces - 1)) * 16; };
-#pragma unroll
-  for (uint32_t i = 0; i < FI; ++i) {
-#pragma unroll
-    for (uint32_t j = 0; j < FJ; ++j)
-#pragma unroll
-      for (uint32_t p = 0; p < 4; ++p) {
-        float v[4];
-#pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) v[e] = value(i, j, p, e);
-        pack4<kF16>(v, box + place(lane & 31, j * 4 + p) + (lane >> 5) * 8);
-      }
-    lanes_meet();
-    const uint32_t from = (lane >> 4) * 8 + ((lane & 15) >> 2), token = row0 + i * 32 + (lane >> 4) * 8;
-#pragma unroll
-    for (uint32_t q = 0; q < FJ * 2; ++q) {
-      const uint32_t piece = q * 2 + (lane & 3) / 2, in = (lane & 1) * 8, col = col0 + q * 16 + (lane & 15);
-      Piece v;
-      const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((STQ_LDS v4s*)(box + place(from, piece) + in));
-      const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((STQ_LDS v4s*)(box + place(from + 4, piece) + in));
-      __builtin_memcpy(&v.w[0], &lo, 8);
-      __builtin_memcpy(&v.w[2], &hi, 8);
-      if (col < cols && token < rows) store_piece16(out + static_cast<uint64_t>(col) * apart + token, v);
-    }
-    lanes_meet();
-  }
-}
 
 // a.a.s: the scales of GradWork, a.b and a.n: of the piece.
 template <int TX, int TW, int TM, int TN, int WM, int WN, bool PIECES>
@@ -231,7 +183,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grad_tile_kernel(const MatmulArg
     const auto g = [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return u2f(static_cast<uint32_t>(acc[i][j][p * 4 + e])); };
 #pragma unroll
     for (int k = 0; k < TX; ++k)
-      store_tile<kF16, FM, FN>(Mat{l.g.gx[k], nullptr, l.apart_x, 0, 0}, t.m0 + t.wm, t.n0 + t.wn, l.tokens_padded, l.n_padded, t.box, t.lane,
+      store_tile<kF16, FM, FN>(Mat{l.g.gx[k], nullptr, l.n_padded, 0, 0}, t.m0 + t.wm, t.n0 + t.wn, l.tokens_padded, l.n_padded, t.box, t.lane,
                                [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return term<TX>(g(i, j, p, e) * sn[j * 32 + p * 8 + e] * times[i], k); });
     // g * scale, the largest of each of the tile's columns (by way of LDS; a NaN stays one with any power of two) and the powers of two that follow
     float* const held = reinterpret_cast<float*>(t.spare);  // [2 WM][TN]: of sixteen lanes each
@@ -267,7 +219,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grad_tile_kernel(const MatmulArg
     const float* const pn = powers + t.wn + 4 * half;
 #pragma unroll
     for (int k = 0; k < TW; ++k)
-      store_transposed<FM, FN>(l.g.gw[k], l.apart_w, l.tokens_padded, t.m0 + t.wm, t.n0 + t.wn, l.n_padded, t.box, t.lane,
+      store_tile<kF16, FM, FN>(Mat{l.g.gw[k], nullptr, l.n_padded, 0, 0}, t.m0 + t.wm, t.n0 + t.wn, l.tokens_padded, l.n_padded, t.box, t.lane,
                                [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return term<TW>(g(i, j, p, e) * pn[j * 32 + p * 8 + e], k); });
     if constexpr (TM < 128) {  // rows and columns of zeros that no tile covers
       const uint32_t row_end = t.m0 + TM, col_end = t.n0 + TN;
@@ -275,11 +227,11 @@ __global__ __launch_bounds__(WM * WN * 64) void grad_tile_kernel(const MatmulArg
       for (uint32_t k = threadIdx.x; k < TM * TN; k += WM * WN * 64) {
         const uint32_t r = k / TN, c = k % TN;
         if (last_row && row_end + r < l.tokens_padded && t.n0 + c < l.n_padded) {
-          for (int i = 0; i < TW; ++i) l.g.gw[i][static_cast<uint64_t>(t.n0 + c) * l.apart_w + row_end + r] = static_cast<_Float16>(0.0f);
+          for (int i = 0; i < TW; ++i) l.g.gw[i][static_cast<uint64_t>(row_end + r) * l.n_padded + t.n0 + c] = static_cast<_Float16>(0.0f);
           if (r == 0) l.g.unit[static_cast<uint64_t>(row_end / TM) * l.n_padded + t.n0 + c] = 253;
         }
         if (last_col && col_end + c < l.n_padded && t.m0 + r < l.tokens_padded)
-          for (int i = 0; i < TX; ++i) l.g.gx[i][static_cast<uint64_t>(t.m0 + r) * l.apart_x + col_end + c] = static_cast<_Float16>(0.0f);
+          for (int i = 0; i < TX; ++i) l.g.gx[i][static_cast<uint64_t>(t.m0 + r) * l.n_padded + col_end + c] = static_cast<_Float16>(0.0f);
       }
     }
   });
@@ -307,10 +259,11 @@ __global__ __launch_bounds__(256) void grad_each_kernel(const MatmulArgs a, cons
       const uint32_t token = from + r;
       const bool in = token < a.m && c < a.n;
       const float g = grad(token), gx = in ? g * a.b.s[c] * power(factor_exponent(f2u(l.g.most[token] * most_w))) : 0.0f, gw = in ? g * a.a.s[token] * power(e) : 0.0f;
+      const uint64_t at = static_cast<uint64_t>(token) * l.n_padded + c;
 #pragma unroll
-      for (int k = 0; k < TX; ++k) l.g.gx[k][static_cast<uint64_t>(token) * l.apart_x + c] = static_cast<_Float16>(term<TX>(gx, k));
+      for (int k = 0; k < TX; ++k) l.g.gx[k][at] = static_cast<_Float16>(term<TX>(gx, k));
 #pragma unroll
-      for (int k = 0; k < TW; ++k) l.g.gw[k][static_cast<uint64_t>(c) * l.apart_w + token] = static_cast<_Float16>(term<TW>(gw, k));
+      for (int k = 0; k < TW; ++k) l.g.gw[k][at] = static_cast<_Float16>(term<TW>(gw, k));
     }
   }
 }
@@ -319,8 +272,9 @@ __global__ __launch_bounds__(256) void grad_each_kernel(const MatmulArgs a, cons
 // out[i][j] = sum over c of g(i, c) * q(c, j): with respect to x (WEIGHT false) i is the token and c the class, with respect to w i is the
 // class and c the token.
 struct ProductArgs {
-  const _Float16* g[2];   // [ni, padded][nc]
-  const _Float16* q;      // [nj][nc]
+  const _Float16* g[2];   // [ni, padded][nc], with respect to w [nc][ni, padded]
+  const _Float16* q;      // [nc][nj, padded]
+  uint64_t g_stride;
   const float* most;      // with respect to x: [ni], and the classes' largest scale (bits), as the tiles had them
   const uint32_t* most_w;
   const uint8_t* unit;    // with respect to w: [nc / unit_rows][ni, padded]
@@ -328,9 +282,8 @@ struct ProductArgs {
   Mat out;
   float* sum;             // [ni][nj]: what is added (with `add`), and where the result goes that is not the last part
   bool add, last;
-  uint32_t apart;         // of g's and q's rows
   uint32_t ni, nj, nc;    // sizes of the sum; nc is a multiple of two steps
-  uint32_t ni_padded;
+  uint32_t ni_padded, nj_padded;
   uint32_t tiles_i, tiles_j;
   uint32_t splits, each;  // parts of c, and their length (a multiple of two steps)
   float* partial;         // [splits][ni][nj] where there are several
@@ -340,10 +293,26 @@ struct Products {  // those with respect to x, of which there are groups_x workg
   uint64_t groups_x, groups;
 };
 
-// A tile in LDS has 32 or 64 (C) elements of the sum in a row, in pieces of eight which lie at the places that their number and the row's give
-// by exclusive or, so that reads of one piece of 32 rows meet every bank once.
+// A [c][x] tile in LDS: rows of X elements, of which pieces of eight lie at the places that their number and the row's give by exclusive or, so
+// that the four rows of a transposed read meet every bank once.
+template <uint32_t X>
+__device__ __forceinline__ uint32_t swizzle_x(uint32_t row) { return X >= 128 ? (row & 3) << 2 : (row >> 1 & 1) << 2; }
+// An [i][c] tile of C elements a row, 32 or 64, for reads of one piece of 32 rows.
 template <uint32_t C>
-__device__ __forceinline__ uint32_t swizzle(uint32_t row) { return C == 32 ? row >> 2 & 3 : row >> 1 & 7; }
+__device__ __forceinline__ uint32_t swizzle_c(uint32_t row) { return C == 32 ? row >> 2 & 3 : row >> 1 & 7; }
+
+// The fragment of columns x0 .. x0+31 and rows c0 .. c0+15 of a [c][x] tile: eight neighbouring rows of one column to a lane.
+template <uint32_t X>
+__device__ __forceinline__ v8h transposed(const _Float16* tile, uint32_t c0, uint32_t x0, uint32_t lane) {
+  const uint32_t row = c0 + (lane >> 5) * 8 + ((lane & 15) >> 2), piece = (x0 / 8 ^ swizzle_x<X>((lane & 15) >> 2)) + (lane & 16) / 8 + (lane & 3) / 2;
+  const _Float16* p = tile + row * X + piece * 8 + (lane & 1) * 4;
+  const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((STQ_LDS v4s*)(p));
+  const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((STQ_LDS v4s*)(p + 4 * X));
+  v8h r;
+  __builtin_memcpy(&r, &lo, 8);
+  __builtin_memcpy(reinterpret_cast<char*>(&r) + 8, &hi, 8);
+  return r;
+}
 
 [[maybe_unused]] __device__ __forceinline__ void store_floats(float* p, const float (&v)[4]) { __builtin_memcpy(as_global(p), v, 16); }
 
@@ -426,26 +395,32 @@ __device__ __forceinline__ void product(const ProductArgs& a, uint32_t group, _F
   const uint32_t first = part * a.each, end = min(a.nc, first + a.each);
   // load i of a wave fills 64 pieces of LDS, in lane order, from (i * waves + wave) * 64 on
   uint32_t ob[LB], oa[LA];
-  const auto offset = [&](uint32_t i, uint32_t from, uint32_t rows) {
-    const uint32_t n = (i * (kThreads / 64) + wave) * 64 + lane, row = n / (STEP / 8), piece = n % (STEP / 8) ^ swizzle<STEP>(row);
-    return (min(from + row, rows - 1) - from) * a.apart * 2 + piece * 16;
-  };
 #pragma unroll
-  for (uint32_t i = 0; i < LB; ++i) ob[i] = offset(i, j0, a.nj);
+  for (uint32_t i = 0; i < LB; ++i) {
+    const uint32_t n = (i * (kThreads / 64) + wave) * 64 + lane, row = n / (TJ / 8), piece = (n % (TJ / 8)) ^ swizzle_x<TJ>(row);
+    ob[i] = (row * a.nj_padded + min(j0 + piece * 8, a.nj_padded - 8)) * 2;
+  }
 #pragma unroll
-  for (uint32_t i = 0; i < LA; ++i) oa[i] = offset(i, i0, a.ni_padded);
-  const auto load = [&](uint32_t c, _Float16* to_a, _Float16* to_b) __attribute__((always_inline)) {
+  for (uint32_t i = 0; i < LA; ++i) {
+    const uint32_t n = (i * (kThreads / 64) + wave) * 64 + lane, row = n / (WEIGHT ? TI / 8 : STEP / 8), slot = n % (WEIGHT ? TI / 8 : STEP / 8);
+    if (WEIGHT) oa[i] = (row * static_cast<uint32_t>(a.g_stride) + min(i0 + (slot ^ swizzle_x<TI>(row)) * 8, a.ni_padded - 8)) * 2;
+    else oa[i] = (min(i0 + row, a.ni_padded - 1) - i0) * static_cast<uint32_t>(a.g_stride) * 2 + (slot ^ swizzle_c<STEP>(row)) * 16;
+  }
+  const auto load_b = [&](uint32_t c, _Float16* to) __attribute__((always_inline)) {
     if (c >= end) return;
-    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(a.q) + static_cast<uint64_t>(j0) * a.apart + c, 0, 0x7FFFFFFF, 0x00020000);
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(a.q) + static_cast<uint64_t>(c) * a.nj_padded, 0, 0x7FFFFFFF, 0x00020000);
 #pragma unroll
     for (uint32_t i = 0; i < LB; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (STQ_LDS void*)(to_b + (i * (kThreads / 64) + wave) * 512), 16, ob[i], 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (STQ_LDS void*)(to + (i * (kThreads / 64) + wave) * 512), 16, ob[i], 0, 0, 0);
+  };
+  const auto load_a = [&](uint32_t c, _Float16* to) __attribute__((always_inline)) {
+    if (c >= end) return;
 #pragma unroll
     for (int k = 0; k < TERMS; ++k) {
-      const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(a.g[k]) + static_cast<uint64_t>(i0) * a.apart + c, 0, 0x7FFFFFFF, 0x00020000);
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(a.g[k]) + (WEIGHT ? c * a.g_stride : i0 * a.g_stride + c), 0, 0x7FFFFFFF, 0x00020000);
 #pragma unroll
       for (uint32_t i = 0; i < LA; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (STQ_LDS void*)(to_a + k * kSizeA + (i * (kThreads / 64) + wave) * 512), 16, oa[i], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (STQ_LDS void*)(to + k * kSizeA + (i * (kThreads / 64) + wave) * 512), 16, oa[i], 0, 0, 0);
     }
   };
   v16f acc[FI][FJ] = {};
@@ -457,14 +432,15 @@ __device__ __forceinline__ void product(const ProductArgs& a, uint32_t group, _F
   v8h fa[kAhead], fb[2][FJ];
   const auto read = [&](uint32_t u, const _Float16* ta, const _Float16* tb) __attribute__((always_inline)) {
     const uint32_t s = u / (TERMS * FI), k = u / FI % TERMS, i = u % FI;
-    const auto fragment = [&](const _Float16* tile, uint32_t from) __attribute__((always_inline)) {
-      const uint32_t row = from + (lane & 31);
-      return load_half8(tile + row * STEP + ((s * 2 + (lane >> 5)) ^ swizzle<STEP>(lane & 31)) * 8);
-    };
-    fa[u % kAhead] = fragment(ta + k * kSizeA, wi + i * 32);
+    if constexpr (WEIGHT) {
+      fa[u % kAhead] = transposed<TI>(ta + k * kSizeA, s * 16, wi + i * 32, lane);
+    } else {
+      const uint32_t row = wi + i * 32 + (lane & 31);
+      __builtin_memcpy(&fa[u % kAhead], &ta[k * kSizeA + row * STEP + ((s * 2 + (lane >> 5)) ^ swizzle_c<STEP>(row)) * 8], 16);
+    }
     if (u % (TERMS * FI)) return;
 #pragma unroll
-    for (uint32_t j = 0; j < FJ; ++j) fb[s & 1][j] = fragment(tb, wj + j * 32);
+    for (uint32_t j = 0; j < FJ; ++j) fb[s & 1][j] = transposed<TJ>(tb, s * 16, wj + j * 32, lane);
   };
   // dw: the sums are in units of 2^-unit, those of the factors at work.  A tile of factors 2^64 and more below the largest so far is taken as
   // if it were 2^64 below, so that the sums stay within fp32: it adds nothing to them either way.  What a change multiplies the sums by is
@@ -499,7 +475,8 @@ __device__ __forceinline__ void product(const ProductArgs& a, uint32_t group, _F
       if (u == kUnits - kAhead) {
         __syncthreads();
         if constexpr (WEIGHT) next_units(c + STEP);
-        load(c + 2 * STEP, ta, tb);
+        load_b(c + 2 * STEP, tb);
+        load_a(c + 2 * STEP, ta);
       }
       if constexpr (WEIGHT)
         if (u == 0 && c != first) change_unit(c, FI - 1);
@@ -513,7 +490,8 @@ __device__ __forceinline__ void product(const ProductArgs& a, uint32_t group, _F
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  load(first, a0, b0);
+  load_b(first, b0);
+  load_a(first, a0);
   if constexpr (WEIGHT) {
     load_units(first);
 #pragma unroll
@@ -521,7 +499,8 @@ __device__ __forceinline__ void product(const ProductArgs& a, uint32_t group, _F
     load_units(first / a.unit_rows * a.unit_rows + a.unit_rows);
   }
   __syncthreads();
-  load(first + STEP, a1, b1);
+  load_b(first + STEP, b1);
+  load_a(first + STEP, a1);
 #pragma unroll
   for (uint32_t u = 0; u < kAhead; ++u) read(u, a0, b0);
   // (what the last step reads ahead is not used)
@@ -591,9 +570,6 @@ constexpr uint32_t kCus = 256;  // for sizes that must not depend on the device
 
 uint64_t padded(uint64_t n) { return (n + 127) / 128 * 128; }  // to two steps of a product
 
-// How far rows of n factors or codes lie apart: an odd number of 256 bytes, so that a tile's rows do not all lie in one channel of the L2.
-uint64_t apart_of(uint64_t n) { return n % 256 ? n : n + 128; }
-
 // Classes of a piece, of one size: of as many logits as have their factors in 1 GiB, twice 2 bytes each, or 4 for results in fp32.  (8192 x 32000 x
 // 4096 in 64 MiB of logits' factors 4758 us, in 256 MiB 4586, in 512 MiB 4475, in 1 GiB 4552.)
 constexpr uint64_t kPieceLogits = 1ull << 28, kLeastPiece = 2048, kMostPiece = 1ull << 20;
@@ -605,11 +581,12 @@ uint64_t piece_of(uint64_t tokens, uint64_t classes, bool fp32) {
 }
 
 // How the products of a piece are taken: tiles of t x t, and each sum in parts, so that no workgroup has more than half of what a CU has to do
-// (sums of 512 at least).
+// (but sums of kLeastSum at least: 601 x 5003 x 768 in fp32, in parts of 512 55 us with their joining, of 1024 42, of 2560 62).
 struct Plan {
   uint32_t t;
   uint32_t splits_x, each_x, splits_w, each_w;
 };
+constexpr uint64_t kLeastSum = 1024;
 uint64_t tiles(uint64_t a, uint64_t b, uint64_t t) { return ((a + t - 1) / t) * ((b + t - 1) / t); }
 Plan plan_of(uint64_t tokens, uint64_t n, uint64_t inputs) {
   const uint64_t kx = padded(n), kw = padded(tokens);
@@ -619,7 +596,7 @@ Plan plan_of(uint64_t tokens, uint64_t n, uint64_t inputs) {
   p.t = work(256) >= 512 * kCus && work(256) * 3 <= work(128) ? 256 : (work(128) >= 512 * kCus && work(128) * 2 <= work(64) ? 128 : 64);
   const uint64_t at_once = p.t == 256 ? kCus : (p.t == 128 ? 2 * kCus : 4 * kCus), half = work(p.t) / at_once / 2;
   const auto split = [&](uint64_t k, uint32_t* splits, uint32_t* each) {
-    const uint64_t s = (k + (half > 512 ? half : 512) - 1) / (half > 512 ? half : 512);
+    const uint64_t s = (k + (half > kLeastSum ? half : kLeastSum) - 1) / (half > kLeastSum ? half : kLeastSum);
     *each = static_cast<uint32_t>(padded((k + s - 1) / s));
     *splits = static_cast<uint32_t>((k + *each - 1) / *each);
   };
@@ -687,13 +664,14 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(const Mat out, uint64_t 
 
 namespace {
 struct Need {  // of a workspace
-  uint64_t piece, t, c, partial, bytes;
+  uint64_t piece, t, c, d, partial, bytes;
 };
 Need need_of(uint64_t tokens, uint64_t classes, uint64_t inputs, bool fp32) {
   Need n;
   n.piece = piece_of(tokens, classes, fp32);
   n.t = padded(tokens);
   n.c = padded(n.piece);
+  n.d = (inputs + 7) / 8 * 8;
   n.partial = 0;
   for (const uint64_t k : {n.piece, classes % n.piece ? classes % n.piece : n.piece}) {  // (the last piece may be taken in more parts)
     const Plan p = plan_of(tokens, k, inputs);
@@ -701,7 +679,7 @@ Need need_of(uint64_t tokens, uint64_t classes, uint64_t inputs, bool fp32) {
     n.partial = b > n.partial ? b : n.partial;
   }
   const uint64_t t = n.t, c = n.c;
-  n.bytes = whole(16 * t) + 2 * whole(4 * t) + whole(4) + whole(2 * apart_of(t) * inputs) + whole(2 * apart_of(c) * inputs) + (fp32 ? 2 : 1) * (whole(2 * t * apart_of(c)) + whole(2 * c * apart_of(t))) + whole((t + 63) / 64 * c) +
+  n.bytes = whole(16 * t) + 2 * whole(4 * t) + whole(4) + whole(2 * t * n.d) + whole(2 * c * n.d) + (fp32 ? 4 : 2) * whole(2 * t * c) + whole((t + 63) / 64 * c) +
             (n.piece < classes ? whole(4 * tokens * inputs) : 0) + n.partial;
   return n;
 }
@@ -723,7 +701,7 @@ int launch_loss_grad(const LossGradArgs& a, uint32_t dx_type, uint32_t dw_type, 
   }
   const bool two_x = a.dx.p && dx_type == kF32, two_w = a.dw.p && dw_type == kF32;
   const Need need = need_of(a.tokens, a.classes, a.inputs, two_x || two_w);
-  const uint32_t piece = static_cast<uint32_t>(need.piece), parts = tiles_of(a.classes, piece);
+  const uint32_t piece = static_cast<uint32_t>(need.piece), parts = tiles_of(a.classes, piece), d = static_cast<uint32_t>(need.d);
   const uint64_t t = need.t, c = need.c;
   Arena arena{static_cast<char*>(workspace)};
   GradWork g;
@@ -731,11 +709,11 @@ int launch_loss_grad(const LossGradArgs& a, uint32_t dx_type, uint32_t dw_type, 
   g.scale = arena.take<float>(t);
   g.most = arena.take<float>(t);
   g.most_w = arena.take<uint32_t>(1);
-  g.x = arena.take<_Float16>(apart_of(t) * a.inputs);
-  g.w = arena.take<_Float16>(apart_of(c) * a.inputs);
+  g.x = arena.take<_Float16>(t * d);
+  g.w = arena.take<_Float16>(c * d);
   for (int k = 0; k < (two_x || two_w ? 2 : 1); ++k) {
-    g.gx[k] = arena.take<_Float16>(t * apart_of(c));
-    g.gw[k] = arena.take<_Float16>(c * apart_of(t));
+    g.gx[k] = arena.take<_Float16>(t * c);
+    g.gw[k] = arena.take<_Float16>(t * c);
   }
   g.unit = arena.take<uint8_t>((t + 63) / 64 * c);
   g.sum = parts > 1 ? arena.take<float>(static_cast<uint64_t>(a.tokens) * a.inputs) : nullptr;
@@ -746,24 +724,26 @@ int launch_loss_grad(const LossGradArgs& a, uint32_t dx_type, uint32_t dw_type, 
     Mat w = a.w;
     w.p = static_cast<int8_t*>(a.w.p) + first * a.w.stride;
     w.s = a.w.s + first;
-    const uint32_t apart_x = static_cast<uint32_t>(apart_of(n_padded)), apart_w = static_cast<uint32_t>(apart_of(t));
-    const Convert cw{w, g.w, n, a.inputs, n_padded, apart_x, tiles_of(a.inputs, 64)};
-    const uint64_t groups_w = static_cast<uint64_t>(n_padded / 128) * cw.groups_c;
+    const Convert cw{w, g.w, n, a.inputs, d, static_cast<uint64_t>(n_padded) * (d / 8)};
+    const uint64_t groups_w = (cw.vectors + 256 * kConvert - 1) / (256 * kConvert);
     if (p == 0) {
-      const Prepare q{a, g, Convert{a.x, g.x, a.tokens, a.inputs, t_padded, apart_w, cw.groups_c}, cw, t_padded, tiles_of(t_padded, 256)};
-      prepare_kernel<<<in_layers(1 + q.groups_t + static_cast<uint64_t>(t_padded / 128) * cw.groups_c + groups_w), 256, 0, st>>>(q);
+      Prepare q{a, g, Convert{a.x, g.x, a.tokens, a.inputs, d, t * (d / 8)}, cw, t_padded, tiles_of(t_padded, 256), 0};
+      q.groups_x = (q.x.vectors + 256 * kConvert - 1) / (256 * kConvert);
+      prepare_kernel<<<in_layers(1 + q.groups_t + q.groups_x + groups_w), 256, 0, st>>>(q);
     } else {
       convert_kernel<<<in_layers(groups_w), 256, 0, st>>>(cw);
     }
     MatmulArgs m{a.x, w, Mat{}, a.tokens, n, a.inputs};
     m.a.s = g.scale;
-    const LogitGrads l{g, first, t_padded, n_padded, apart_x, apart_w};
+    const LogitGrads l{g, first, t_padded, n_padded};
     const auto grads = two_x ? (two_w ? run_grads<2, 2> : run_grads<2, 1>) : (two_w ? run_grads<1, 2> : run_grads<1, 1>);
     const uint32_t unit_rows = grads(m, l, n_cu, st);
     Products both{};
     const Plan plan = plan_of(a.tokens, n, a.inputs);
     for (ProductArgs* q : {&both.x, &both.w}) {
+      q->g_stride = n_padded;
       q->nj = a.inputs;
+      q->nj_padded = d;
     }
     if (a.dx.p) {
       ProductArgs& q = both.x;
@@ -778,7 +758,6 @@ int launch_loss_grad(const LossGradArgs& a, uint32_t dx_type, uint32_t dw_type, 
       q.last = p + 1 == parts;
       q.ni = a.tokens;
       q.nc = n_padded;
-      q.apart = apart_x;
       q.ni_padded = t_padded;
       q.partial = g.partial;
     }
@@ -794,7 +773,6 @@ int launch_loss_grad(const LossGradArgs& a, uint32_t dx_type, uint32_t dw_type, 
       q.last = true;
       q.ni = n;
       q.nc = t_padded;
-      q.apart = apart_w;
       q.ni_padded = n_padded;
       q.partial = g.partial + partial_x(plan, a.tokens, a.inputs) / 4;
     }
