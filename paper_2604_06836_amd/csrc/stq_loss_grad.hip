@@ -4,7 +4,7 @@
 // written twice in fp16: times the classes' scales as the factors of dx, times the tokens' as those of dw.  Results in bf16 take one term of 11
 // bits, results in fp32 two, 22 bits.  A power of two goes with them that brings the largest into [2^14, 2^15): what lies 2^-29 below it loses
 // bits, and what lies 2^-39 below it counts as 0.  For dx it is one for each token, whose largest has a bound that is known beforehand
-// (|g| <= |dloss + dlse| (1 - p) but at the target); for dw it is one for each class and tile of tokens, and the sums change their unit
+// (|g| <= |dloss + dlse| (1 - p) but at the target, with 1 - p taken as 2^-20 (1 + |lse|) at least); for dw it is one for each class and tile of tokens, and the sums change their unit
 // from tile to tile.  Codes are exact in fp16.
 #include <hip/hip_runtime.h>
 
@@ -29,7 +29,7 @@ __device__ __forceinline__ uint32_t factor_exponent(uint32_t most) {
 
 // What the tiles of the logits need of a token.
 struct Token {
-  float lse2;       // log-sum times log2 e
+  float lse;
   float c;          // dloss + dlse
   float at_target;  // the gradient of the target's logit
   uint32_t target;  // its class, or kNoTarget
@@ -118,9 +118,11 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Prepare p) {
       const float dlse = a.dlse ? as_global(a.dlse)[token] : 0.0f, dloss = beyond ? NAN : (target == kNoTarget ? 0.0f : as_global(a.dloss)[token]);
       if (!(dlse == 0.0f && dloss == 0.0f)) {
         const float loss = as_global(a.loss)[token], others = target == kNoTarget ? 1.0f : -expm1f(-loss);  // probability of the other classes
-        t = Token{as_global(a.lse)[token] * kLog2e, dloss + dlse, dlse * expf(-loss) - dloss * others, target};
+        t = Token{as_global(a.lse)[token], dloss + dlse, dlse * expf(-loss) - dloss * others, target};
         scale = as_global(a.x.s)[token];
-        most = u2f(max(f2u(t.c * others) & 0x7FFFFFFFu, target == kNoTarget ? 0u : f2u(t.at_target) & 0x7FFFFFFFu));
+        // (A loss that is next to 0 may be no more than a difference of two fp32 numbers of lse's size: the other classes' gradients, from lse and
+        // the logits, are then not bounded by it.)
+        most = u2f(max(f2u(t.c * fmaxf(others, 0x1p-20f * (1.0f + fabsf(t.lse)))) & 0x7FFFFFFFu, target == kNoTarget ? 0u : f2u(t.at_target) & 0x7FFFFFFFu));
       }
     }
     p.g.token[token] = t;
@@ -139,7 +141,7 @@ struct LogitGrads {
   uint32_t first;                    // class of the piece
   uint32_t tokens_padded, n_padded;  // rows and columns that are written, zeros beyond the matrices
 };
-__device__ __forceinline__ float grad_of(float z, const Token& t) { return t.c * __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, -t.lse2)); }
+__device__ __forceinline__ float grad_of(float z, const Token& t) { return t.c * __builtin_amdgcn_exp2f((z - t.lse) * kLog2e); }
 template <int TERMS>
 __device__ __forceinline__ float term(float x, int k) { return TERMS == 2 && k ? x - static_cast<float>(static_cast<_Float16>(x)) : x; }
 

@@ -6,7 +6,8 @@ reference and of a difference and a product, its value by two units in the last 
 is longer than n / 64 + 64.  Factors of the gradients' products enter with 11 significant bits (half a step: 2^-11) for results in
 bf16 and with 22 (2^-22) for results in fp32.  They are fp16 numbers, whose steps are 2^-24 at least (half of one: 2^-25), after a power of two
 that brings the largest of the result's row to 2^14 or above: 2^-39 of that largest is what any of them may be off absolutely.  The largest
-of a row of dx is what a token's own loss bounds it by, max(|dloss + dlse| (1 - p), |g at the target|), with the largest of the classes' scales."""
+of a row of dx is what a token's own loss bounds it by, max(|dloss + dlse| (1 - p), |g at the target|) with 1 - p as 2^-20 (1 + |lse|) at least,
+times the largest of the classes' scales."""
 import math
 
 import pytest
@@ -114,7 +115,7 @@ def check_backward(p, dx, dw, dlse=None):
         + 8 * U * (dl.abs()[there] * sure + dloss.abs()[there] * (1 - sure))
     g_off += 2.0 ** -148
     w, x = p.w.value(), p.x.value()
-    largest = torch.where(there, (dloss + dl).abs() * -torch.expm1(-loss), dl.abs())
+    largest = (dloss + dl).abs() * torch.where(there, torch.maximum(-torch.expm1(-loss), 2.0 ** -20 * (1 + lse.abs())), torch.maximum(torch.ones_like(lse), 2.0 ** -20 * (1 + lse.abs())))
     largest[rows] = torch.maximum(largest[rows], g[rows, p.target[there]].abs())
     largest = largest[:, None] * p.w.s.double().max()
     largest_of_class = (g.t().abs() * p.x.s.double().view(1, -1)).amax(1, keepdim=True)
@@ -284,6 +285,36 @@ def test_rows_of_very_different_size(ctx):
         dx, dw = Buffer(t, n, TYPES[kind]), Buffer(v, n, TYPES[kind])
         p.backward(ctx, dx.mat(), dw.mat())
         check_backward(p, dx, dw)
+
+
+@pytest.mark.parametrize("t,v,n", [(40, 300, 64), (300, 1001, 256), (513, 3001, 768)])
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+def test_losses_that_are_differences(ctx, t, v, n, kind):
+    """Losses from elsewhere: fp32 log-sums less fp32 logits, 0 or slightly wrong for tokens predicted with certainty.  Nothing overflows, and the
+    gradients are off by no more than the losses are: two roundings of numbers of lse's size, and the logit's own three."""
+    p = Problem(t, v, n, seed=16)
+    z, lse, loss, off, off_loss = p.exact()
+    there = p.target >= 0
+    at = p.target.clamp_min(0)[:, None]
+    p.lse = lse.float()
+    p.loss = torch.where(there, p.lse - z.float().gather(1, at)[:, 0], 0.0)
+    assert (p.loss[there] == 0).any()
+    dx, dw = Buffer(t, n, TYPES[kind]), Buffer(v, n, TYPES[kind])
+    p.backward(ctx, dx.mat(), dw.mat())
+    g = torch.exp(z - lse[:, None]) * torch.where(there, p.dloss.double(), 0.0)[:, None]
+    g_off = g.abs() * (2 * off[:, None] + U * (2 * (z - lse[:, None]).abs() + 9)) + 2.0 ** -126 * p.dloss.abs().double()[:, None]
+    rows = torch.arange(t, device="cuda")[there]
+    g[rows, p.target[there]] = (p.dloss.double() * torch.expm1(-loss))[there]
+    g_off[rows, p.target[there]] = (p.dloss.double().abs() * (off + U * 4 * lse.abs()))[there]
+    w, x = p.w.value(), p.x.value()
+    largest = p.dloss.abs().double() * torch.where(there, torch.maximum(-torch.expm1(-loss) + U * 4 * lse.abs(), 2.0 ** -20 * (1 + lse.abs())), 0.0)
+    for out, f, f_off, m, scale, k, most in ((dx, g, g_off, w, p.w.s, v, largest[:, None] * p.w.s.double().max()),
+                                             (dw, g.t(), g_off.t(), x, p.x.s, t, ((g.t().abs() + g_off.t()) * p.x.s.double().view(1, -1)).amax(1, keepdim=True))):
+        bf16 = out.t.dtype == torch.bfloat16
+        want = f @ m
+        bound = f_off @ m.abs() + ((2.0 ** -11 if bf16 else 2.0 ** -22) + (k + 8) * U) * (f.abs() @ m.abs()) + (B * want.abs() * (1 + B) if bf16 else 0.0) \
+            + most * 2.0 ** -39 * (1 + B) * m.div(scale.double()).abs().sum(0, keepdim=True) + 2.0 ** -126
+        assert ((out.t.double() - want).abs() <= bound).all()
 
 
 def test_gradients_against_differences(ctx):
