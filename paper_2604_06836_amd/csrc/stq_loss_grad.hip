@@ -429,8 +429,9 @@ __device__ __forceinline__ void product(const ProductArgs& a, uint32_t group, _F
   const uint32_t wi = wave / WJ * (TI / WI), wj = wave % WJ * (TJ / WJ);
   // A step out of ta, tb, in units of one fragment of g.  A unit's fragments are read kAhead units ahead, so that those of the last kAhead are
   // there when the workgroup meets: from then on the next step's buffers are full and this step's are free.
-  constexpr uint32_t kUnits = STEP / 16 * TERMS * FI, kAhead = FI < 4 || TERMS == 2 ? 2 : 4;
+  constexpr uint32_t kUnits = STEP / 16 * TERMS * FI, kAhead = FI < 4 ? 2 : 4;
   static_assert(kUnits > kAhead, "units in front of the meeting");
+  static_assert(kAhead + 1 >= FI, "changes of units are known when the first sums are done");
   v8h fa[kAhead], fb[2][FJ];
   const auto read = [&](uint32_t u, const _Float16* ta, const _Float16* tb) __attribute__((always_inline)) {
     const uint32_t s = u / (TERMS * FI), k = u / FI % TERMS, i = u % FI;

@@ -161,6 +161,19 @@ def test_gradients(ctx, t, v, n, kinds, pad, with_dlse):
         assert (dx.t[2] == 0).all()
 
 
+# Results of large, ordinary and small tiles behind logits of each tile, sums in parts and not, and sizes that no tile divides.
+@pytest.mark.parametrize("t,v,n", [(192, 27392, 645), (1024, 8192, 1024), (2048, 8192, 512), (2500, 9000, 500), (640, 5003, 768), (128, 20000, 128), (3000, 600, 1000),
+                                   (1500, 2500, 130), (257, 40000, 40)])
+@pytest.mark.parametrize("kinds", [("fp32", "fp32"), ("bf16", "bf16"), ("fp32", "bf16"), ("bf16", "fp32")])
+def test_every_tile(ctx, t, v, n, kinds):
+    p = Problem(t, v, n, seed=17)
+    p.dloss *= torch.exp(4 * torch.randn(t, device="cuda", generator=torch.Generator("cuda").manual_seed(3)))  # units that change from tile to tile
+    p.forward(ctx)
+    dx, dw = Buffer(t, n, TYPES[kinds[0]]), Buffer(v, n, TYPES[kinds[1]])
+    p.backward(ctx, dx.mat(), dw.mat())
+    check_backward(p, dx, dw)
+
+
 @pytest.mark.parametrize("t,v,n", [(4099, 20001, 64), (70001, 1500, 16)])
 @pytest.mark.parametrize("kind", ["fp32", "bf16"])
 def test_several_pieces(ctx, t, v, n, kind):
