@@ -235,7 +235,8 @@ int stq_grad_stats(stq_ctx* ctx, const stq_tensor* tensors, uint32_t n, uint32_t
 /* A gradient of stq_grad_norm and stq_clip_grads. */
 typedef struct {
   const void* grad; /* device, fp32[numel] or bf16[numel], aligned to its elements (16 bytes are faster); NULL if numel is 0 */
-  void* out;        /* where stq_clip_grads writes it: grad itself or NULL (in place), or memory that overlaps no gradient */
+  void* out;        /* where stq_clip_grads writes it: grad itself or NULL (in place), or memory that overlaps no gradient and no
+                       other's out; then no two gradients may overlap either                      */
   uint64_t numel;   /* 0 is possible                                                              */
   uint32_t dtype;   /* 0 = fp32, 1 = bf16: of each tensor by itself                               */
 } stq_grad;

@@ -137,7 +137,7 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* part, const flo
                                                    float* loss, float* lse) {
   constexpr uint32_t kTokens = 256 / Q;
   __shared__ float2 held[256];
-  const uint32_t turn = threadIdx.x / kTokens, token = blockIdx.x * kTokens + threadIdx.x % kTokens;
+  const uint32_t turn = threadIdx.x / kTokens, token = group_number() * kTokens + threadIdx.x % kTokens;
   if (token < tokens && turn < parts) held[threadIdx.x] = joined(part + static_cast<uint64_t>(turn) * tokens + token, static_cast<uint64_t>(Q) * tokens, (parts - turn + Q - 1) / Q);
   else held[threadIdx.x] = make_float2(-INFINITY, 0.0f);
   __syncthreads();
@@ -208,7 +208,7 @@ int launch_loss(const LossArgs& l, void* workspace, uint32_t n_cu, void* stream)
   }
   // Threads for a token: as many as there are parts for, and no more than fill the card.
   if (l.tokens <= 1024 && parts > 64) join_kernel<256><<<l.tokens, 256, 0, st>>>(part, at_target, parts, l.tokens, l.classes, l.targets, l.loss, l.lse);
-  else join_kernel<8><<<tiles_of(l.tokens, 32), 256, 0, st>>>(part, at_target, parts, l.tokens, l.classes, l.targets, l.loss, l.lse);
+  else join_kernel<8><<<in_layers(tiles_of(l.tokens, 32)), 256, 0, st>>>(part, at_target, parts, l.tokens, l.classes, l.targets, l.loss, l.lse);
   return hipGetLastError();
 }
 

@@ -552,7 +552,19 @@ __device__ __forceinline__ void join_four(const ProductArgs& a, uint64_t t) {
     }
   };
   if (a.add) add(a.sum + at);
-  for (uint32_t k = 0; k < a.splits; ++k) add(a.partial + k * size + at);
+  uint32_t k = 0;
+  if (n == 4) {  // eight at a time under way, added in their order
+    for (; k + 8 <= a.splits; k += 8) {
+      v4i w[8];
+#pragma unroll
+      for (uint32_t i = 0; i < 8; ++i) w[i] = load_fragment(reinterpret_cast<const int8_t*>(a.partial + (k + i) * size + at));
+#pragma unroll
+      for (uint32_t i = 0; i < 8; ++i)
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) v[e] += u2f(static_cast<uint32_t>(w[i][e]));
+    }
+  }
+  for (; k < a.splits; ++k) add(a.partial + k * size + at);
   if (a.last) store4<TO>(a.out, row, col, a.nj, v);
   else if (n == 4) store_floats(a.sum + at, v);
   else
