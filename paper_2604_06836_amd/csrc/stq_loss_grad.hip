@@ -27,6 +27,8 @@ __device__ __forceinline__ uint32_t factor_exponent(uint32_t most) {
 }
 [[maybe_unused]] __device__ __forceinline__ float power(uint32_t exponent) { return u2f(exponent << 23); }  // 1 to 254
 
+[[maybe_unused]] __device__ __forceinline__ void store_piece16(_Float16* p, const Piece& v) { __builtin_memcpy(as_global(p), &v, 16); }
+
 // What the tiles of the logits need of a token.
 struct Token {
   float lse;
@@ -145,6 +147,35 @@ __device__ __forceinline__ float grad_of(float z, const Token& t) { return t.c *
 template <int TERMS>
 __device__ __forceinline__ float term(float x, int k) { return TERMS == 2 && k ? x - static_cast<float>(static_cast<_Float16>(x)) : x; }
 
+// store_tile of factors, whose rows and columns are padded to whole pieces.
+template <uint32_t FI, uint32_t FJ, class F>
+__device__ __forceinline__ void store_factors(_Float16* out, uint32_t row0, uint32_t col0, uint32_t rows, uint32_t cols, char* box, uint32_t lane, F value) {
+  constexpr uint32_t kRow = FJ * 64, kPieces = kRow / 16, kShift = kRow == 128 ? 1 : 2;
+  const auto place = [&](uint32_t row, uint32_t piece) { return row * kRow + ((piece ^ (row >> kShift)) & (kPieces - 1)) * 16; };
+  const uint32_t row_of = lane / kPieces, piece = lane % kPieces, col = col0 + piece * 8;
+#pragma unroll
+  for (uint32_t i = 0; i < FI; ++i) {
+#pragma unroll
+    for (uint32_t j = 0; j < FJ; ++j)
+#pragma unroll
+      for (uint32_t p = 0; p < 4; ++p) {
+        float v[4];
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) v[e] = value(i, j, p, e);
+        pack4<kF16>(v, box + place(lane & 31, j * 4 + p) + (lane >> 5) * 8);
+      }
+    lanes_meet();
+#pragma unroll
+    for (uint32_t h = 0; h < 32 * kPieces / 64; ++h) {
+      const uint32_t row = h * (64 / kPieces) + row_of, r = row0 + i * 32 + row;
+      Piece v;
+      __builtin_memcpy(&v, box + place(row, piece), 16);
+      if (r < rows && col < cols) store_piece16(out + static_cast<uint64_t>(r) * cols + col, v);
+    }
+    lanes_meet();
+  }
+}
+
 // a.a.s: the scales of GradWork, a.b and a.n: of the piece.
 template <int TX, int TW, int TM, int TN, int WM, int WN, bool PIECES>
 __global__ __launch_bounds__(WM * WN * 64) void grad_tile_kernel(const MatmulArgs a, const LogitGrads l, uint32_t tiles_m, uint32_t tiles_n) {
@@ -185,7 +216,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grad_tile_kernel(const MatmulArg
     const auto g = [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return u2f(static_cast<uint32_t>(acc[i][j][p * 4 + e])); };
 #pragma unroll
     for (int k = 0; k < TX; ++k)
-      store_tile<kF16, FM, FN>(Mat{l.g.gx[k], nullptr, l.n_padded, 0, 0}, t.m0 + t.wm, t.n0 + t.wn, l.tokens_padded, l.n_padded, t.box, t.lane,
+      store_factors<FM, FN>(l.g.gx[k], t.m0 + t.wm, t.n0 + t.wn, l.tokens_padded, l.n_padded, t.box, t.lane,
                                [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return term<TX>(g(i, j, p, e) * sn[j * 32 + p * 8 + e] * times[i], k); });
     // g * scale, the largest of each of the tile's columns (by way of LDS; a NaN stays one with any power of two) and the powers of two that follow
     float* const held = reinterpret_cast<float*>(t.spare);  // [2 WM][TN]: of sixteen lanes each
@@ -221,7 +252,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grad_tile_kernel(const MatmulArg
     const float* const pn = powers + t.wn + 4 * half;
 #pragma unroll
     for (int k = 0; k < TW; ++k)
-      store_tile<kF16, FM, FN>(Mat{l.g.gw[k], nullptr, l.n_padded, 0, 0}, t.m0 + t.wm, t.n0 + t.wn, l.tokens_padded, l.n_padded, t.box, t.lane,
+      store_factors<FM, FN>(l.g.gw[k], t.m0 + t.wm, t.n0 + t.wn, l.tokens_padded, l.n_padded, t.box, t.lane,
                                [&](uint32_t i, uint32_t j, uint32_t p, uint32_t e) { return term<TW>(g(i, j, p, e) * pn[j * 32 + p * 8 + e], k); });
     if constexpr (TM < 128) {  // rows and columns of zeros that no tile covers
       const uint32_t row_end = t.m0 + TM, col_end = t.n0 + TN;
@@ -318,13 +349,22 @@ __device__ __forceinline__ v8h transposed(const _Float16* tile, uint32_t c0, uin
 
 [[maybe_unused]] __device__ __forceinline__ void store_floats(float* p, const float (&v)[4]) { __builtin_memcpy(as_global(p), v, 16); }
 
+template <uint32_t TO>
+__device__ __forceinline__ void store_four(const Mat& out, uint32_t row, uint32_t col, const float (&v)[4]) {
+  using T = typename Elem<TO>::type;
+  STQ_GLOBAL T* p = as_global(static_cast<T*>(out.p)) + row * out.stride + col;
+  Piece o;
+  pack4<TO>(v, &o);
+  __builtin_memcpy(p, &o, TO == kF32 ? 16 : 8);
+}
+
 // A wave's sums, by way of LDS (`box`, 32 rows in fp32), to where they go, with what is added to them.
 template <uint32_t TO, uint32_t FI, uint32_t FJ, class F>
 __device__ __forceinline__ void store_sums(const ProductArgs& a, uint32_t part, uint32_t row0, uint32_t col0, char* box, uint32_t lane, F value) {
   constexpr uint32_t kRow = FJ * 128, kPieces = kRow / 16, kShift = kRow == 256 ? 0 : 1;
   const auto place = [&](uint32_t row, uint32_t piece) { return row * kRow + ((piece ^ (row >> kShift)) & (kPieces - 1)) * 16; };
   float* const to = a.splits > 1 ? a.partial + static_cast<uint64_t>(part) * a.ni * a.nj : a.sum;
-  const bool last = a.last && a.splits == 1, add = a.add && a.splits == 1;
+  const bool last = a.last && a.splits == 1, add = a.add && a.splits == 1, whole = row0 + FI * 32 <= a.ni && col0 + FJ * 32 <= a.nj;
 #pragma unroll
   for (uint32_t i = 0; i < FI; ++i) {
 #pragma unroll
@@ -337,43 +377,30 @@ __device__ __forceinline__ void store_sums(const ProductArgs& a, uint32_t part, 
         __builtin_memcpy(box + place(lane & 31, j * 8 + p * 2 + (lane >> 5)), v, 16);
       }
     lanes_meet();
-#pragma unroll
+    // (Loops that stay loops: what is run once for each tile costs its way from memory into the instruction cache more than its cycles.)
+#pragma unroll 2
     for (uint32_t h = 0; h < 32 * kPieces / 64; ++h) {
       const uint32_t row = h * (64 / kPieces) + lane / kPieces, piece = lane % kPieces;
       float v[4];
       __builtin_memcpy(v, box + place(row, piece), 16);
       const uint32_t r = row0 + i * 32 + row, c = col0 + piece * 4;
-      if (r >= a.ni || c >= a.nj) continue;
       const uint64_t at = static_cast<uint64_t>(r) * a.nj + c;
-      if (add) {
-        if (c + 4 <= a.nj) {
+      if (whole) {
+        if (add) {
           const v4i w = load_fragment(reinterpret_cast<const int8_t*>(a.sum + at));
 #pragma unroll
           for (uint32_t e = 0; e < 4; ++e) v[e] += u2f(static_cast<uint32_t>(w[e]));
-        } else {
-#pragma unroll
-          for (uint32_t e = 0; e < 4; ++e)
-            if (c + e < a.nj) v[e] += as_global(a.sum)[at + e];
         }
-      }
-      if (last) {
-        using T = typename Elem<TO>::type;
-        STQ_GLOBAL T* p = as_global(static_cast<T*>(a.out.p)) + r * a.out.stride + c;
-        if (c + 4 <= a.nj) {
-          Piece o;
-          pack4<TO>(v, &o);
-          __builtin_memcpy(p, &o, TO == kF32 ? 16 : 8);
-        } else {
-#pragma unroll
-          for (uint32_t e = 0; e < 4; ++e)
-            if (c + e < a.nj) p[e] = static_cast<T>(v[e]);
+        if (last) store_four<TO>(a.out, r, c, v);
+        else store_floats(to + at, v);
+      } else if (r < a.ni) {
+        for (uint32_t e = 0; e < 4 && c + e < a.nj; ++e) {
+          float x = e == 0 ? v[0] : (e == 1 ? v[1] : (e == 2 ? v[2] : v[3]));
+          if (add) x += as_global(a.sum)[at + e];
+          using T = typename Elem<TO>::type;
+          if (last) as_global(static_cast<T*>(a.out.p))[r * a.out.stride + c + e] = static_cast<T>(x);
+          else as_global(to)[at + e] = x;
         }
-      } else if (c + 4 <= a.nj) {
-        store_floats(to + at, v);
-      } else {
-#pragma unroll
-        for (uint32_t e = 0; e < 4; ++e)
-          if (c + e < a.nj) as_global(to)[at + e] = v[e];
       }
     }
     lanes_meet();
@@ -391,8 +418,11 @@ __device__ __forceinline__ void product(const ProductArgs& a, uint32_t group, _F
   constexpr uint32_t LA = kSizeA / 8 / kThreads, LB = kSizeB / 8 / kThreads;  // pieces of eight of a thread
   static_assert(LA * kThreads * 8 == kSizeA && LB * kThreads * 8 == kSizeB, "whole loads");
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t tiles = a.tiles_i * a.tiles_j, part = group / tiles;
-  const TileAt at = tile_at(group - part * tiles, a.tiles_i, a.tiles_j);
+  // A sum in a multiple of eight parts: each part's tiles on one of the card's dies, whose L2 then has that part of both factors to itself.
+  const uint32_t tiles = a.tiles_i * a.tiles_j;
+  const bool by_die = a.splits % kDies == 0;
+  const uint32_t part = by_die ? group % a.splits : group / tiles, tile = by_die ? group / a.splits : group - part * tiles;
+  const TileAt at = by_die ? TileAt{tile / a.tiles_j, tile % a.tiles_j} : tile_at(tile, a.tiles_i, a.tiles_j);
   const uint32_t i0 = at.row * TI, j0 = at.col * TJ;
   const uint32_t first = part * a.each, end = min(a.nc, first + a.each);
   // load i of a wave fills 64 pieces of LDS, in lane order, from (i * waves + wave) * 64 on
@@ -611,7 +641,8 @@ Plan plan_of(uint64_t tokens, uint64_t n, uint64_t inputs) {
   p.t = work(256) >= 512 * kCus && work(256) * 3 <= work(128) ? 256 : (work(128) >= 512 * kCus && work(128) * 2 <= work(64) ? 128 : 64);
   const uint64_t at_once = p.t == 256 ? kCus : (p.t == 128 ? 2 * kCus : 4 * kCus), half = work(p.t) / at_once / 2;
   const auto split = [&](uint64_t k, uint32_t* splits, uint32_t* each) {
-    const uint64_t s = (k + (half > kLeastSum ? half : kLeastSum) - 1) / (half > kLeastSum ? half : kLeastSum);
+    uint64_t s = (k + (half > kLeastSum ? half : kLeastSum) - 1) / (half > kLeastSum ? half : kLeastSum);
+    if (s > 5) s = (s + 2) / 8 * 8 ? (s + 2) / 8 * 8 : 8;
     *each = static_cast<uint32_t>(padded((k + s - 1) / s));
     *splits = static_cast<uint32_t>((k + *each - 1) / *each);
   };
