@@ -51,12 +51,16 @@ __global__ __launch_bounds__(WM * WN * 64) void loss_tile_kernel(const MatmulArg
           if (first + k / 16 * 32 + k % 16 / 4 * 8 + k % 4 >= a.n) z[k] = -INFINITY;
       }
       if (__builtin_amdgcn_ballot_w64(at < FN * 32)) {
+        float it = 0.0f;
+        bool here = false;
 #pragma unroll
-        for (uint32_t k = 0; k < FN * 16; ++k)
-          if (at == k / 16 * 32 + k % 16 / 4 * 8 + k % 4) {
-            if (token < a.m) at_target[token] = z[k];
-            z[k] = -INFINITY;
-          }
+        for (uint32_t k = 0; k < FN * 16; ++k) {
+          const bool is = at == k / 16 * 32 + k % 16 / 4 * 8 + k % 4;
+          it = is ? z[k] : it;
+          here |= is;
+          z[k] = is ? -INFINITY : z[k];
+        }
+        if (here && token < a.m) at_target[token] = it;
       }
       float most = z[0];
 #pragma unroll
