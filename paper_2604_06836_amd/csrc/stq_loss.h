@@ -10,7 +10,7 @@ namespace stq {
 namespace {
 
 constexpr uint32_t kNoTarget = 0xFFFFFFFFu;
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLog2e = 1.44269504088896340736f;
 
 // The class of a token's target, or kNoTarget; one beyond the classes comes out as no class either, and is told apart by `beyond`.
 __device__ __forceinline__ uint32_t target_of(const int64_t* targets, uint32_t token, uint32_t classes, bool* beyond) {
