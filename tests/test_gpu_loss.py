@@ -185,6 +185,23 @@ def test_several_pieces(ctx, t, v, n, kind):
     check_backward(p, dx, dw)
 
 
+@pytest.mark.parametrize("t,v,n", [(70001, 5003, 16), (16411, 20001, 64), (16411, 20001, 301), (1, 3 * 2 ** 20 + 5, 16), (17, 2200007, 24)])
+@pytest.mark.parametrize("kinds", [("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "fp32")])
+def test_classes_that_do_not_fit_one_piece(ctx, t, v, n, kinds):
+    # Factors of all classes at once, two of at least two bytes each, would not fit the workspace: so there are several pieces, for either type.
+    assert stq.cross_entropy_grad_bytes(t, v, n) < 4 * ((t + 127) // 128 * 128) * v
+    p = Problem(t, v, n, seed=12)
+    p.forward(ctx)
+    check_forward(p)
+    dx, dw = Buffer(t, n, TYPES[kinds[0]]), Buffer(v, n, TYPES[kinds[1]])
+    p.backward(ctx, dx.mat(), dw.mat())
+    check_backward(p, dx, dw)
+    one = Buffer(t, n, TYPES[kinds[0]])
+    if kinds[0] == kinds[1]:  # (with dw in fp32 the pieces would be others than without it)
+        p.backward(ctx, one.mat(), None)
+        assert torch.equal(one.t, dx.t)
+
+
 @pytest.mark.parametrize("kind", ["fp32", "bf16"])
 def test_one_gradient_alone(ctx, kind):
     p = Problem(300, 1001, 100, seed=3)
