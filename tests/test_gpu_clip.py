@@ -270,3 +270,26 @@ def test_refusals(ctx):
         assert code_of(lambda: ctx.clip_grads(one(), norm.data_ptr(), most, s)) == EINVAL
     torch.cuda.synchronize()
     assert (g == 1).all() and (norm == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_tensor_of_more_than_32_bits_of_elements(ctx, dtype):
+    n = 2 ** 32 + 2051
+    t = torch.zeros(n, dtype=dtype, device="cuda")
+    at = torch.tensor([0, 2 ** 31 - 1, 2 ** 31, 2 ** 32 - 1, 2 ** 32, 2 ** 32 + 2047, n - 1], device="cuda")
+    t[at] = torch.tensor([1.0, 2.0, 3.0, 4.0, 5.0, 6.0, 8.0], device="cuda").to(t.dtype)
+    norm = torch.zeros(2, dtype=torch.float64, device="cuda")
+    grads = stq.make_grads([dict(grad=t.data_ptr(), numel=n, dtype=KIND[dtype])])
+    s = torch.cuda.current_stream().cuda_stream
+    ctx.grad_norm(grads, norm.data_ptr(), s)
+    assert norm[0].item() == 155.0  # exact in fp64
+    before = t[at].double()
+    ctx.clip_grads(grads, norm.data_ptr(), 1.0, s)
+    c = 1.0 / (math.sqrt(155.0) + 1e-6)
+    # the factor and the product each rounded to fp32, and to bf16
+    off = 2.0 ** -24 * 2.01 + (2.0 ** -8 * 1.01 if dtype == BF16 else 0.0)
+    assert ((t[at].double() - before * c).abs() <= off * before * c).all()
+    t[at] = 0
+    assert not any(part.any().item() for part in t.split(2 ** 28))
+    del t
+    torch.cuda.empty_cache()

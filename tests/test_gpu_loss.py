@@ -202,6 +202,27 @@ def test_classes_that_do_not_fit_one_piece(ctx, t, v, n, kinds):
         assert torch.equal(one.t, dx.t)
 
 
+# Rows so far apart that the last of the classes' lie beyond 2^32 bytes and (of dw) 2^31 elements; at 2^22 codes and more the kernels are others.
+@pytest.mark.parametrize("t,v,stride", [(3, 2200, 1 << 21), (300, 2200, 1 << 21), (300, 2200, (1 << 21) + 5), (5, 1100, 1 << 22), (70, 1100, 1 << 22)])
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+def test_rows_far_apart(ctx, t, v, stride, kind):
+    n = 64
+    p = Problem(t, v, n, seed=13)
+    x, w = p.x, p.w
+    p.x, p.w = Codes(t, n, pad=stride - n), Codes(v, n, pad=stride - n)
+    for to, of in ((p.x, x), (p.w, w)):
+        if stride % 16 == 0:  # rows that begin at 16 bytes
+            to.q.at, to.q.t = 0, to.q.whole[:, :n]
+            to.mat = to.q.mat(to.s)
+        to.q.t.copy_(of.q.t)
+        to.s.copy_(of.s)
+    p.forward(ctx)
+    check_forward(p)
+    dx, dw = Buffer(t, n, TYPES[kind], pad=(1 << 20) - n), Buffer(v, n, TYPES[kind], pad=(1 << 20) - n)
+    p.backward(ctx, dx.mat(), dw.mat())
+    check_backward(p, dx, dw)
+
+
 @pytest.mark.parametrize("kind", ["fp32", "bf16"])
 def test_one_gradient_alone(ctx, kind):
     p = Problem(300, 1001, 100, seed=3)
